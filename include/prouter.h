@@ -460,6 +460,195 @@ pr_status pr_stream_reset_slots(pr_stream* state, const int32_t* slots, int32_t 
 /* Frees the state (synchronises the device first). NULL is ignored. */
 void pr_stream_destroy(pr_stream* state);
 
+/* ------------------------------------------------------------------------
+ * Training the small model on what the routing saw: losses over the same
+ * logit rows, with their gradients in the logits, and the optimizer's step.
+ * ------------------------------------------------------------------------ */
+
+/* Per-row flags of the losses, besides the PR_FLAG_* above. */
+#define PR_FLAG_MASKED 16u  /* weight 0: the row is not read, its outputs and its gradient are 0 */
+#define PR_FLAG_CLIPPED 32u /* the clipped ratio is the smaller gain: no gradient through it */
+
+/* Options of pr_policy_loss. */
+typedef struct pr_policy_params {
+  double clip_low;   /* the ratio is held at or above 1 - clip_low, 0 <= clip_low <= 1 */
+  double clip_high;  /* and at or below 1 + clip_high, >= 0 (+inf: no upper bound) */
+  double kl_coef;    /* beta of the KL term, finite, >= 0 */
+  double grad_scale; /* finite factor of the gradient alone (loss scaling, accumulation) */
+} pr_policy_params;
+
+/* Per-token outputs of pr_policy_loss, each [n_rows]; any may be NULL. */
+typedef struct pr_policy_tokens_t {
+  float* logprob; /* l = log p(y) */
+  float* ratio;   /* exp(l - old_logprob) */
+  float* kl;      /* exp(ref - l) - 1 - (ref - l), 0 without ref_logprob */
+  uint32_t* flags;
+} pr_policy_tokens_t;
+
+/* Fills *params (host pointer): clip_low = clip_high = 0.2, kl_coef = 0, grad_scale = 1. */
+void pr_policy_params_default(pr_policy_params* params);
+
+/*
+ * Clipped policy loss with a KL term over n_rows tokens, and its gradient in
+ * the logits. With u = z / T, l = log softmax(u)[y], ratio = exp(l - old),
+ * A the advantage, d = ref - l:
+ *   gain = min(ratio A, clip(ratio, 1 - clip_low, 1 + clip_high) A)
+ *   kl   = exp(d) - 1 - d
+ *   loss = sum over rows of weight (kl_coef kl - gain)
+ *   dloss/dz_v = weight ((clipped ? 0 : -ratio A) - kl_coef (exp(d) - 1)) / T (delta_vy - softmax(u)_v)
+ * where clipped says that the second product is strictly the smaller.
+ *   logits .. temperature  as for pr_token_features (no top-p).
+ *   weight       float [n_rows]: each row's weight in the sum, mask and
+ *                normaliser in one. A row of weight 0 is not read (its logits
+ *                may hold anything), its outputs and gradient are 0.
+ *   advantage, old_logprob
+ *                float [n_rows].
+ *   ref_logprob  float [n_rows], or NULL: no KL term (kl_coef must be 0).
+ *   loss         float [1].
+ *   out          host pointer to a struct of device arrays, or NULL.
+ *   grad         of the logits' type, row r at element r * grad_stride
+ *                (grad_stride >= vocab), aligned to the element size; times
+ *                grad_scale, rounded to nearest. NULL: not computed. It may be
+ *                the logits themselves (the same pointer and stride); any
+ *                other overlap is rejected.
+ *   workspace    device scratch of at least pr_policy_loss_workspace bytes,
+ *                16-byte aligned; no initialisation needed.
+ * A row with a nonzero weight that is flagged NONFINITE, BAD_TP or BAD_ID has
+ * NaN outputs and gradient, and makes the loss NaN. Sums are held in 64 bits
+ * and taken in a fixed order. n_rows == 0 sets the loss to 0.
+ */
+size_t pr_policy_loss_workspace(pr_dtype dtype, int64_t n_rows, int32_t vocab);
+pr_status pr_policy_loss(const void* logits, pr_dtype dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,
+                         const int32_t* ids, const float* temperature, const float* weight, const float* advantage,
+                         const float* old_logprob, const float* ref_logprob, const pr_policy_params* params,
+                         float* loss, const pr_policy_tokens_t* out, void* grad, int64_t grad_stride,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* Options of pr_preference_loss. */
+typedef struct pr_preference_params {
+  double beta;            /* finite, > 0 */
+  double label_smoothing; /* 0 <= label_smoothing <= 1 */
+  double margin;          /* finite: subtracted from every pair's logit */
+  double grad_scale;      /* finite factor of the gradient alone */
+} pr_preference_params;
+
+/* Outputs of pr_preference_loss; any may be NULL. */
+typedef struct pr_preference_out_t {
+  float* pair_loss;    /* [n_pairs] */
+  float* pair_logit;   /* [n_pairs] h */
+  float* seq_logratio; /* [2 n_pairs] q */
+  float* logprob;      /* [n_rows] l */
+  uint32_t* flags;     /* [n_rows] */
+} pr_preference_out_t;
+
+/* Fills *params (host pointer): beta = 0.1, label_smoothing = margin = 0, grad_scale = 1. */
+void pr_preference_params_default(pr_preference_params* params);
+
+/*
+ * Preference loss over pairs of requests, and its gradient in the logits.
+ * Pair p is request 2p (the chosen answer) and request 2p + 1 (the rejected
+ * one); request i owns rows offsets[i] .. offsets[i+1]-1. With l as above:
+ *   q_i  = sum over the request's rows of weight (l - ref)
+ *   h_p  = beta (q_2p - q_2p+1) - margin
+ *   loss = mean over pairs of -(1 - s) log sigmoid(h) - s log sigmoid(-h), s = label_smoothing
+ *   dloss/dz_v = +-beta weight (sigmoid(h) - 1 + s) / (n_pairs T) (delta_vy - softmax(u)_v)
+ *                (+ in the chosen request, - in the rejected one)
+ * Weights of 1 / (the request's tokens), no ref and a margin give the
+ * length-normalised form without a reference model.
+ *   logits .. weight, loss, grad, workspace  as for pr_policy_loss.
+ *   offsets      int32 [2 n_pairs + 1], device; precondition as for
+ *                pr_feature_sequence. A request may be empty (q = 0).
+ *   ref_logprob  float [n_rows], the reference model's l, or NULL (0).
+ *   out          host pointer to a struct of device arrays, or NULL.
+ * n_pairs == 0 (then n_rows == 0) sets the loss to NaN, a mean over nothing.
+ */
+size_t pr_preference_loss_workspace(pr_dtype dtype, int64_t n_rows, int32_t vocab, int32_t n_pairs);
+pr_status pr_preference_loss(const void* logits, pr_dtype dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,
+                             const int32_t* ids, const float* temperature, const float* weight,
+                             const int32_t* offsets, int32_t n_pairs, const float* ref_logprob,
+                             const pr_preference_params* params, float* loss, const pr_preference_out_t* out,
+                             void* grad, int64_t grad_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One tensor of an AdamW step. Pointers are device pointers, aligned to their
+ * element size. */
+typedef struct pr_adamw_tensor {
+  void* param;      /* [n], of the optimizer's param_dtype */
+  const void* grad; /* [n], of its grad_dtype; NULL: given at each step */
+  void* copy;       /* bfloat16 [n]: receives the float32 parameter rounded to nearest; or NULL */
+  void* m;          /* [n]: float (32-bit states) or uint8_t codes */
+  void* v;          /* [n]: likewise */
+  uint8_t* m_exp;   /* [ceil(n / 256)] exponents (8-bit states), else NULL */
+  uint8_t* v_exp;
+  int64_t n;        /* elements, >= 0 */
+} pr_adamw_tensor;
+
+/* A step's hyperparameters. */
+typedef struct pr_adamw_params {
+  double lr, beta1, beta2, eps, weight_decay; /* finite; 0 <= beta < 1, eps >= 0 */
+  double grad_scale;                          /* finite factor of the gradients */
+  int64_t step;                               /* counted from 1 */
+} pr_adamw_params;
+
+typedef struct pr_adamw pr_adamw;
+
+/* Elements that share an exponent in 8-bit states. */
+#define PR_ADAMW_BLOCK 256
+
+/*
+ * An AdamW step over many tensors at once, in one launch per 448 tensors. For each element, with g = grad_scale grad:
+ *   m' = beta1 m + (1 - beta1) g,  v' = beta2 v + (1 - beta2) g g
+ *   p' = p (1 - lr weight_decay) - lr c1 m' / (c2 sqrt(v') + eps),
+ *   c1 = 1 / (1 - beta1^step),  c2 = 1 / sqrt(1 - beta2^step)
+ * in float32. bfloat16 parameters are rounded stochastically, so that
+ * steps below half their spacing still count on average.
+ *
+ * 8-bit states: the elements i / 256 of a tensor share an exponent byte E.
+ * The code of m is a sign bit and k (7 bits: 4 of exponent, 3 of mantissa),
+ * that of v is k (8 bits: 5 and 3). k = 0 stands for 0, any other k for the
+ * float32 whose bits are (k + 8 (E - 15)) << 20 for m, (k + 8 (E - 31)) << 20
+ * for v. E is the exponent of the block's largest magnitude with its 20 low
+ * bits rounded up, at least 16 (m) or 32 (v), so a state keeps 16 (m) or 31 (v)
+ * octaves below the block's largest; smaller values of m become 0, of
+ * v the smallest positive code. A value is rounded up when its 20 low bits
+ * plus 20 random ones carry: right on average, so that a moving average
+ * moves although each step changes it by less than its spacing. E = 255: the
+ * block holds NaN or an infinity and stands for NaN throughout.
+ *   Random bits: element i of tensor j takes mix(i + mix(j + 1 + K)) mod 2^32
+ *   with K the upper 32 bits of SplitMix64's output for (seed, step) and
+ *     mix(x): x *= 0x9E3779B9; x ^= x >> 15; x *= 0x6A09E667; x ^= x >> 13
+ *   (m takes its 20 low bits, v its 20 high ones, a bfloat16 parameter its
+ *   16 low ones).
+ *
+ * pr_adamw_create: reads the host array `tensors` and keeps a copy on the
+ * current device (the only allocating call). The tensors stay the caller's; no
+ * two of their arrays may overlap, except that a tensor's grad may be in
+ * any memory of its own. param_dtype, grad_dtype: PR_F32 or PR_BF16; copies
+ * need float32 parameters. state_bits: 32 or 8. A first step starts from
+ * states that are all zero bytes (either kind).
+ */
+pr_status pr_adamw_create(const pr_adamw_tensor* tensors, int32_t n_tensors, pr_dtype param_dtype,
+                          pr_dtype grad_dtype, int32_t state_bits, uint64_t seed, pr_adamw** handle);
+
+/*
+ * One step. grads: host array of n_tensors device pointers, read during the
+ * call, or NULL: those of the tensors' descriptors. A NULL entry leaves that
+ * tensor as it is. Steps of a handle share no scratch; those on the same
+ * tensors must be ordered.
+ */
+pr_status pr_adamw_step(pr_adamw* handle, const void* const* grads, const pr_adamw_params* params, void* stream);
+
+/*
+ * The values that 8-bit states stand for, as bfloat16 (which holds every one
+ * exactly): tensor j's element i at element 256 * (blocks of the tensors
+ * before it) + i of m and of v, where a tensor has ceil(n / 256) blocks.
+ * Entries between tensors are left as they are. PR_ERR_UNSUPPORTED for 32-bit
+ * states.
+ */
+pr_status pr_adamw_moments(pr_adamw* handle, void* m, void* v, void* stream);
+
+/* Frees the handle (synchronises its device first). NULL is ignored. */
+void pr_adamw_destroy(pr_adamw* handle);
+
 #ifdef __cplusplus
 }
 #endif

@@ -13,6 +13,10 @@ The paper's own verifier input, the per-token tuples (l, m, h, rho) with the
 top-K entropy (Sec. 3.1, Eq. 3): :func:`feature_sequence`.
 
 Streaming decode: :class:`StreamState`.
+
+Training the small model on what the routing saw: :func:`policy_loss` and
+:func:`preference_loss` over the same logit rows, with their gradients, and
+:class:`AdamW`.
 """
 
 from __future__ import annotations
@@ -22,11 +26,11 @@ import ctypes as C
 import torch
 
 from . import _abi
-from ._abi import (FLAG_BAD_ID, FLAG_BAD_TP, FLAG_NONFINITE, FLAG_OUTSIDE_NUCLEUS,  # noqa: F401
-                   ProuterError)
+from ._abi import (FLAG_BAD_ID, FLAG_BAD_TP, FLAG_CLIPPED, FLAG_MASKED, FLAG_NONFINITE,  # noqa: F401
+                   FLAG_OUTSIDE_NUCLEUS, ProuterError)
 
 __all__ = ["token_features", "token_features_noalloc", "feature_sequence", "sample_features", "verifier_head", "request_aggregate", "route", "calibrate_threshold",
-           "validate_offsets", "StreamState",
+           "validate_offsets", "StreamState", "policy_loss", "preference_loss", "AdamW",
            "token_features_workspace", "ProuterError", "FEATURE_FLOATS", "FEATURE_INTS", "PAPER_TOP_K"]
 
 PAPER_TOP_K = 20  # K of the paper's top-K entropy (Sec. 3.1)
@@ -448,6 +452,317 @@ class StreamState:
     def close(self) -> None:
         if self._h:
             _abi.lib().pr_stream_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ---------------------------------------------------------------------------
+# Training: losses over logit rows, and the optimizer's step.
+
+def _check_current(device, what: str):
+    """Launches go to the current device's stream: the tensors have to be there."""
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} must be on the current CUDA device, got {device}")
+
+
+def _check_row_floats(device, n: int, **tensors):
+    for name, t in tensors.items():
+        if t is not None and (t.dtype != torch.float32 or t.device != device or t.shape != (n,) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous float32 [{n}] tensor on {device}")
+
+
+def _check_loss(logits, ids, temperature, weight, grad):
+    """Checks of a loss's rows; returns them with the temperature as a tensor, and the gradient to write or None."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be a 2-D CUDA tensor with unit stride along the vocabulary")
+    n, V = logits.shape
+    _dtype_code(logits)
+    _check_current(logits.device, "logits")
+    temperature = _as_row_tensor(temperature, n, logits.device)
+    if logits.stride(1) != 1 or (n > 1 and logits.stride(0) < V):
+        raise ValueError("logits must be a 2-D CUDA tensor with unit stride along the vocabulary and rows apart")
+    _check_index_tensor(ids, "ids", logits.device, n)
+    _check_row_floats(logits.device, n, temperature=temperature, weight=weight)
+    if grad is True:
+        grad = torch.empty(n, V, dtype=logits.dtype, device=logits.device)
+    elif grad is False or grad is None:
+        grad = None
+    elif (grad.dtype != logits.dtype or grad.shape != logits.shape or grad.device != logits.device
+          or grad.stride(1) != 1 or (n > 1 and grad.stride(0) < V)):
+        raise ValueError(f"grad must be a {logits.dtype} {list(logits.shape)} tensor on {logits.device} with unit "
+                         "stride along the vocabulary and rows apart")
+    return temperature, grad
+
+
+def _row_stride(t) -> int:
+    """Elements from row to row (a single row may come with any stride)."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _scratch(workspace, need: int, device):
+    """The caller's workspace where it serves, else one of this call; and its bytes."""
+    _check_workspace(workspace, device)
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if need and (size < need or workspace.data_ptr() % 16):
+        workspace, size = torch.empty(need, dtype=torch.uint8, device=device), need
+    return workspace, size
+
+
+def policy_loss(logits: torch.Tensor, ids: torch.Tensor, temperature, weight: torch.Tensor, advantage: torch.Tensor,
+                old_logprob: torch.Tensor, ref_logprob: torch.Tensor | None = None, clip_low: float = 0.2,
+                clip_high: float = 0.2, kl_coef: float = 0.0, grad=True, grad_scale: float = 1.0,
+                workspace: torch.Tensor | None = None) -> dict:
+    """Clipped policy loss with a KL term, and its gradient (``pr_policy_loss``).
+
+    ``logits`` [n_rows, V] float32/bfloat16, ``ids`` int32 [n_rows] (the
+    tokens that were generated), ``temperature`` float32 [n_rows] or a Python
+    float, ``weight`` float32 [n_rows]: a row's weight in the sum, 0 for rows
+    that do not count (they are not read). ``advantage``, ``old_logprob``,
+    ``ref_logprob`` float32 [n_rows]; without ``ref_logprob`` there is no KL
+    term. The loss is the sum over rows of
+    weight (kl_coef kl - min(ratio A, clip(ratio, 1 - clip_low, 1 + clip_high) A)),
+    ratio = exp(logprob - old_logprob).
+
+    ``grad``: True for a gradient in the logits (of their type, times
+    ``grad_scale``), False for none, or the tensor that receives it, which may
+    be ``logits``. Returns a dict with ``loss`` (float32 [1]), ``logprob``,
+    ``ratio``, ``kl``, ``flags`` ([n_rows]) and, when wanted, ``grad``.
+    ``workspace``: optional device scratch of this call, not shared with one
+    that may overlap.
+    """
+    temperature, grad = _check_loss(logits, ids, temperature, weight, grad)
+    n, V = logits.shape
+    _check_row_floats(logits.device, n, advantage=advantage, old_logprob=old_logprob, ref_logprob=ref_logprob)
+    L = _abi.lib()
+    code = _dtype_code(logits)
+    need = L.pr_policy_loss_workspace(code, n, V)
+    workspace, ws_bytes = _scratch(workspace, need, logits.device)
+    out = dict(zip(("logprob", "ratio", "kl"), _outputs(3, n, torch.float32, logits.device)))
+    out["flags"] = torch.empty(n, dtype=torch.int32, device=logits.device)
+    out["loss"] = torch.empty(1, dtype=torch.float32, device=logits.device)
+    params = _abi.PolicyParams(float(clip_low), float(clip_high), float(kl_coef), float(grad_scale))
+    tokens = _abi.PolicyTokens(*[out[k].data_ptr() for k in _abi.POLICY_FIELDS])
+    st = L.pr_policy_loss(_ptr(logits), code, n, V, _row_stride(logits), _ptr(ids), _ptr(temperature), _ptr(weight),
+                          _ptr(advantage), _ptr(old_logprob), _ptr(ref_logprob), C.byref(params), _ptr(out["loss"]),
+                          C.byref(tokens), _ptr(grad), 0 if grad is None else _row_stride(grad), _ptr(workspace),
+                          ws_bytes, _stream_handle())
+    _abi.check("pr_policy_loss", st)
+    if grad is not None:
+        out["grad"] = grad
+    return out
+
+
+def preference_loss(logits: torch.Tensor, ids: torch.Tensor, temperature, weight: torch.Tensor, offsets: torch.Tensor,
+                    ref_logprob: torch.Tensor | None = None, beta: float = 0.1, label_smoothing: float = 0.0,
+                    margin: float = 0.0, grad=True, grad_scale: float = 1.0,
+                    workspace: torch.Tensor | None = None) -> dict:
+    """Preference loss over pairs of requests, and its gradient (``pr_preference_loss``).
+
+    ``logits``, ``ids``, ``temperature``, ``weight``, ``grad``, ``workspace``
+    as for :func:`policy_loss`. ``offsets`` int32 [2 n_pairs + 1]: request i
+    owns rows ``offsets[i]:offsets[i+1]``; requests 2p and 2p + 1 are the
+    chosen and the rejected answer of pair p. With q the sum over a request's
+    rows of weight (logprob - ref_logprob) and
+    h = beta (q_chosen - q_rejected) - margin, the loss is the mean over pairs
+    of -(1 - label_smoothing) log sigmoid(h) - label_smoothing log sigmoid(-h).
+
+    Returns a dict with ``loss`` (float32 [1]), ``pair_loss``, ``pair_logit``
+    (h) [n_pairs], ``seq_logratio`` (q) [2 n_pairs], ``logprob``, ``flags``
+    [n_rows] and, when wanted, ``grad``.
+    """
+    temperature, grad = _check_loss(logits, ids, temperature, weight, grad)
+    n, V = logits.shape
+    _check_row_floats(logits.device, n, ref_logprob=ref_logprob)
+    _check_index_tensor(offsets, "offsets", logits.device)
+    if offsets.shape[0] % 2 == 0:
+        raise ValueError("offsets must have 2 n_pairs + 1 entries")
+    n_pairs = offsets.shape[0] // 2
+    L = _abi.lib()
+    code = _dtype_code(logits)
+    need = L.pr_preference_loss_workspace(code, n, V, n_pairs)
+    workspace, ws_bytes = _scratch(workspace, need, logits.device)
+    out = dict(zip(("pair_loss", "pair_logit"), _outputs(2, n_pairs, torch.float32, logits.device)))
+    out["seq_logratio"] = torch.empty(2 * n_pairs, dtype=torch.float32, device=logits.device)
+    out["logprob"] = torch.empty(n, dtype=torch.float32, device=logits.device)
+    out["flags"] = torch.empty(n, dtype=torch.int32, device=logits.device)
+    out["loss"] = torch.empty(1, dtype=torch.float32, device=logits.device)
+    params = _abi.PreferenceParams(float(beta), float(label_smoothing), float(margin), float(grad_scale))
+    values = _abi.PreferenceOut(*[out[k].data_ptr() for k in _abi.PREFERENCE_FIELDS])
+    st = L.pr_preference_loss(_ptr(logits), code, n, V, _row_stride(logits), _ptr(ids), _ptr(temperature), _ptr(weight),
+                              _ptr(offsets), n_pairs, _ptr(ref_logprob), C.byref(params), _ptr(out["loss"]),
+                              C.byref(values), _ptr(grad), 0 if grad is None else _row_stride(grad), _ptr(workspace),
+                              ws_bytes, _stream_handle())
+    _abi.check("pr_preference_loss", st)
+    if grad is not None:
+        out["grad"] = grad
+    return out
+
+
+class AdamW:
+    """AdamW over many tensors at once (``pr_adamw_*``), states in 32 or 8 bits.
+
+    ``params``: contiguous CUDA tensors, all float32 or all bfloat16 (then
+    rounded stochastically). ``grads``: their gradients, when these stay in
+    the same memory from step to step; otherwise :meth:`step` takes them.
+    ``copies``: bfloat16 tensors that receive float32 parameters rounded to
+    nearest. ``states``: a dict per tensor with ``m`` and ``v`` (float32 like
+    the parameter; with ``state_bits=8`` uint8 codes, and uint8 ``m_exp`` and
+    ``v_exp`` of one entry per 256 elements), as :attr:`states` holds them; by
+    default zeros. ``steps``: steps taken so far. ``seed``: of the stochastic
+    rounding.
+
+    The tensors given and made here are kept, not copied: a step changes them
+    in place, and they must stay where they are.
+    """
+
+    def __init__(self, params, grads=None, copies=None, state_bits: int = 32, states=None, seed: int = 0,
+                 steps: int = 0):
+        self._h = C.c_void_p()
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("params must hold at least one tensor")
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        self.device = self.params[0].device
+        _check_current(self.device, "params")
+        self.state_bits, self.steps = state_bits, int(steps)
+        n = len(self.params)
+        self._dtype = self.params[0].dtype
+        _dtype_code(self.params[0])
+        for p in self.params:
+            self._check(p, "params", self._dtype, None)
+        self._sizes = [p.numel() for p in self.params]
+        self.grads = self._list(grads, "grads", None)
+        self._grad_dtype = self.grads[0].dtype if self.grads else None
+        self.copies = self._list(copies, "copies", torch.bfloat16)
+        if self.copies and self._dtype != torch.float32:
+            raise ValueError("copies need float32 params")
+        blocks = [-(-k // _abi.PR_ADAMW_BLOCK) for k in self._sizes]
+        self._blocks = blocks
+        if states is None:
+            states = [self._zeros(k, b) for k, b in zip(self._sizes, blocks)]
+        self.states = list(states)
+        if len(self.states) != n:
+            raise ValueError(f"states must have {n} entries")
+        kind = torch.float32 if state_bits == 32 else torch.uint8
+        for s, k, b in zip(self.states, self._sizes, blocks):
+            for name, size in (("m", k), ("v", k)) + ((("m_exp", b), ("v_exp", b)) if state_bits == 8 else ()):
+                if name not in s:
+                    raise ValueError(f"a state of {state_bits} bits needs '{name}'")
+                self._check(s[name], f"states' {name}", kind, size)
+        self._seed = int(seed) & 0xFFFFFFFFFFFFFFFF
+        if self._grad_dtype is not None:
+            self._create()
+
+    def _check(self, t, what, dtype, size):
+        if t.dtype != dtype or t.device != self.device or not t.is_contiguous() or (size is not None and t.numel() != size):
+            count = "" if size is None else f" of {size} elements"
+            raise ValueError(f"{what} must be contiguous {dtype} tensors{count} on {self.device}")
+
+    def _list(self, tensors, what, dtype):
+        """A list that matches the parameters, or None."""
+        if tensors is None:
+            return None
+        tensors = list(tensors)
+        if len(tensors) != len(self.params):
+            raise ValueError(f"{what} must have {len(self.params)} entries")
+        if dtype is None:
+            dtype = next((t.dtype for t in tensors if t is not None), None)
+            if dtype not in (torch.float32, torch.bfloat16):
+                raise ValueError(f"{what} must be float32 or bfloat16 tensors")
+        for t, size in zip(tensors, self._sizes):
+            if t is not None:
+                self._check(t, what, dtype, size)
+            elif what != "step's grads":
+                raise ValueError(f"{what} must have a tensor for every parameter")
+        return tensors
+
+    def _zeros(self, n, blocks):
+        kind = torch.float32 if self.state_bits == 32 else torch.uint8
+        sizes = {"m": n, "v": n}
+        if self.state_bits == 8:
+            sizes.update(m_exp=blocks, v_exp=blocks)
+        return {k: torch.zeros(size, dtype=kind, device=self.device) for k, size in sizes.items()}
+
+    def _create(self):
+        self.close()
+        T = (_abi.AdamWTensor * len(self.params))()
+        for i, (t, p, s) in enumerate(zip(T, self.params, self.states)):
+            t.param, t.n = p.data_ptr(), p.numel()
+            t.grad = self.grads[i].data_ptr() if self.grads else None
+            t.copy = self.copies[i].data_ptr() if self.copies else None
+            t.m, t.v = s["m"].data_ptr(), s["v"].data_ptr()
+            if self.state_bits == 8:
+                t.m_exp, t.v_exp = s["m_exp"].data_ptr(), s["v_exp"].data_ptr()
+        code = {torch.float32: _abi.PR_F32, torch.bfloat16: _abi.PR_BF16}
+        st = _abi.lib().pr_adamw_create(T, len(T), code[self._dtype], code[self._grad_dtype], self.state_bits,
+                                        self._seed, C.byref(self._h))
+        _abi.check("pr_adamw_create", st)
+
+    def step(self, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
+             grad_scale: float = 1.0, grads=None) -> None:
+        """One step (``pr_adamw_step``) with the gradients given here or at construction; a None among those given
+        here leaves its tensor as it is."""
+        pointers = None
+        if grads is not None:
+            grads = self._list(grads, "step's grads", None)
+            dtype = next(t.dtype for t in grads if t is not None)
+            if self._grad_dtype is None:
+                self._grad_dtype = dtype
+                self._create()
+            elif dtype != self._grad_dtype:
+                raise ValueError(f"step's grads must be {self._grad_dtype} tensors")
+            pointers = (C.c_void_p * len(grads))(*[None if t is None else t.data_ptr() for t in grads])
+        elif self.grads is None:
+            raise ValueError("step needs grads: none were given at construction")
+        _check_current(self.device, "the optimizer's tensors")
+        p = _abi.AdamWParams(float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), float(grad_scale),
+                             self.steps + 1)
+        _abi.check("pr_adamw_step", _abi.lib().pr_adamw_step(self._h, pointers, C.byref(p), _stream_handle()))
+        self.steps += 1
+
+    def moments(self, out=None):
+        """The values of the states, a list of m and a list of v, each shaped like its parameter.
+
+        32-bit states are returned themselves. 8-bit ones are decoded
+        (``pr_adamw_moments``) to bfloat16, which holds them exactly.
+        ``out``: two bfloat16 buffers of 256 entries per block of 256
+        elements, which receive the values and are returned instead; tensor j
+        starts at 256 times the blocks of the tensors before it, and entries
+        between tensors are left as they are."""
+        if self.state_bits == 32:
+            return tuple([s[k].view(p.shape) for s, p in zip(self.states, self.params)] for k in ("m", "v"))
+        if not self._h:
+            self._grad_dtype = self._dtype  # nothing is stepped yet: any type of gradient will do
+            self._create()
+            self._grad_dtype = None
+        total = _abi.PR_ADAMW_BLOCK * sum(self._blocks)
+        given = out is not None
+        if not given:
+            out = tuple(torch.zeros(total, dtype=torch.bfloat16, device=self.device) for _ in range(2))
+        for t in out:
+            self._check(t, "out", torch.bfloat16, total)
+        _check_current(self.device, "the optimizer's tensors")
+        _abi.check("pr_adamw_moments",
+                   _abi.lib().pr_adamw_moments(self._h, _ptr(out[0]), _ptr(out[1]), _stream_handle()))
+        if given:
+            return out
+        lists = ([], [])
+        at = 0
+        for p, size, blocks in zip(self.params, self._sizes, self._blocks):
+            for flat, views in zip(out, lists):
+                views.append(flat[at:at + size].view(p.shape))
+            at += _abi.PR_ADAMW_BLOCK * blocks
+        return lists
+
+    def close(self) -> None:
+        if self._h:
+            _abi.lib().pr_adamw_destroy(self._h)
             self._h = C.c_void_p()
 
     def __del__(self):

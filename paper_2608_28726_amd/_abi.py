@@ -16,6 +16,8 @@ FLAG_NONFINITE = 1
 FLAG_BAD_ID = 2
 FLAG_BAD_TP = 4
 FLAG_OUTSIDE_NUCLEUS = 8
+FLAG_MASKED = 16
+FLAG_CLIPPED = 32
 
 FEATURE_FIELDS = ("max_logit", "lse", "entropy", "logprob", "maxprob", "margin", "rank", "argmax",
                   "cutoff", "flags")
@@ -30,11 +32,16 @@ EXPORTED = (
     "pr_feature_sequence_workspace", "pr_feature_sequence_ws", "pr_sample_features_workspace",
     "pr_sample_features_ws", "pr_verifier_head_workspace_full",
     "pr_token_features_workspace_full", "pr_stream_step_workspace", "pr_stream_step_ws", "pr_token_features_ws",
+    "pr_policy_params_default", "pr_policy_loss_workspace", "pr_policy_loss", "pr_preference_params_default",
+    "pr_preference_loss_workspace", "pr_preference_loss", "pr_adamw_create", "pr_adamw_step", "pr_adamw_moments",
+    "pr_adamw_destroy",
 )
 
 PR_HEAD_WEIGHTS = 67329
 
 PR_MAX_TOP_K = 32
+
+PR_ADAMW_BLOCK = 256
 
 
 class TokenFeatures(C.Structure):
@@ -47,6 +54,35 @@ class AggParams(C.Structure):
 
 class RequestAgg(C.Structure):
     _fields_ = [(name, C.c_void_p) for name in AGG_FIELDS]
+
+
+POLICY_FIELDS = ("logprob", "ratio", "kl", "flags")
+PREFERENCE_FIELDS = ("pair_loss", "pair_logit", "seq_logratio", "logprob", "flags")
+
+
+class PolicyParams(C.Structure):
+    _fields_ = [(name, C.c_double) for name in ("clip_low", "clip_high", "kl_coef", "grad_scale")]
+
+
+class PolicyTokens(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in POLICY_FIELDS]
+
+
+class PreferenceParams(C.Structure):
+    _fields_ = [(name, C.c_double) for name in ("beta", "label_smoothing", "margin", "grad_scale")]
+
+
+class PreferenceOut(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in PREFERENCE_FIELDS]
+
+
+class AdamWTensor(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("param", "grad", "copy", "m", "v", "m_exp", "v_exp")] + [("n", C.c_int64)]
+
+
+class AdamWParams(C.Structure):
+    _fields_ = [(name, C.c_double) for name in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale")] + [
+        ("step", C.c_int64)]
 
 
 class ProuterError(RuntimeError):
@@ -131,6 +167,28 @@ def lib() -> C.CDLL:
     L.pr_stream_reset_slots.restype = C.c_int
     L.pr_stream_destroy.argtypes = [vp]
     L.pr_stream_destroy.restype = None
+    L.pr_policy_params_default.argtypes = [C.POINTER(PolicyParams)]
+    L.pr_policy_params_default.restype = None
+    L.pr_policy_loss_workspace.argtypes = [C.c_int, i64, i32]
+    L.pr_policy_loss_workspace.restype = sz
+    L.pr_policy_loss.argtypes = [vp, C.c_int, i64, i32, i64, vp, vp, vp, vp, vp, vp, C.POINTER(PolicyParams), vp,
+                                 C.POINTER(PolicyTokens), vp, i64, vp, sz, vp]
+    L.pr_policy_loss.restype = C.c_int
+    L.pr_preference_params_default.argtypes = [C.POINTER(PreferenceParams)]
+    L.pr_preference_params_default.restype = None
+    L.pr_preference_loss_workspace.argtypes = [C.c_int, i64, i32, i32]
+    L.pr_preference_loss_workspace.restype = sz
+    L.pr_preference_loss.argtypes = [vp, C.c_int, i64, i32, i64, vp, vp, vp, vp, i32, vp, C.POINTER(PreferenceParams),
+                                     vp, C.POINTER(PreferenceOut), vp, i64, vp, sz, vp]
+    L.pr_preference_loss.restype = C.c_int
+    L.pr_adamw_create.argtypes = [C.POINTER(AdamWTensor), i32, C.c_int, C.c_int, i32, C.c_uint64, C.POINTER(vp)]
+    L.pr_adamw_create.restype = C.c_int
+    L.pr_adamw_step.argtypes = [vp, C.POINTER(vp), C.POINTER(AdamWParams), vp]
+    L.pr_adamw_step.restype = C.c_int
+    L.pr_adamw_moments.argtypes = [vp, vp, vp, vp]
+    L.pr_adamw_moments.restype = C.c_int
+    L.pr_adamw_destroy.argtypes = [vp]
+    L.pr_adamw_destroy.restype = None
     _LIB = L
     return L
 

@@ -1,12 +1,16 @@
 // C ABI of the verifier library: argument checks, launch-shape selection and
 // the streaming state object. Every compute step runs in the kernels of
 // row_features.hip, topp.hip and aggregate.hip.
+#include <cmath>
 #include <mutex>
 #include <new>
+#include <vector>
 
+#include "adamw.h"
 #include "aggregate.h"
 #include "calibrate.h"
 #include "head.h"
+#include "loss.h"
 #include "topp.h"
 
 using namespace pr;
@@ -24,6 +28,15 @@ struct pr_stream {
   pr_agg_params params;
   Partial* ws;  // split-row workspace for up to max_slots rows of kStreamMaxSplit workgroups
   void* block;  // single allocation backing everything above
+};
+
+struct pr_adamw {
+  int device;
+  AdamPlan plan;
+  std::vector<int64_t> chunk_begin;  // [n_tensors + 1] first chunk of each tensor
+  bool has_grads;                    // every tensor of the plan has a gradient of its own
+  uint64_t seed;                     // of the stochastic rounding
+  void* block;                       // single allocation backing the plan's arrays
 };
 
 namespace {
@@ -99,6 +112,51 @@ pr_status noalloc_scratch(hipStream_t stream, void** out) {
   }
   *out = g_scratch_ptr[dev];
   return PR_OK;
+}
+
+// What a loss needs of its rows and its gradient, checked on the host.
+pr_status check_loss(const void* logits, pr_dtype dtype, int64_t n_rows, int32_t V, int64_t row_stride,
+                     const int32_t* ids, const float* temps, const float* weight, const float* loss, const void* grad,
+                     int64_t grad_stride) {
+  const pr_status st = check_rows(logits, dtype, n_rows, V, row_stride, ids, temps);
+  if (st != PR_OK) return st;
+  if (!loss || (n_rows > 0 && !weight)) return PR_ERR_INVALID_ARG;
+  if (!grad || n_rows == 0) return PR_OK;
+  if (grad_stride < V || !aligned(grad, dtype_size(dtype))) return PR_ERR_INVALID_ARG;
+  if (grad == logits && grad_stride == row_stride) return PR_OK;
+  // Rows of at most 2^31 elements, at most 2^26 of them: strides beyond 2^34
+  // would overflow the byte offsets below and address no memory there is.
+  constexpr int64_t kMostStride = int64_t{1} << 34;
+  if (row_stride > kMostStride || grad_stride > kMostStride) return PR_ERR_INVALID_ARG;
+  const uintptr_t item = dtype_size(dtype), n = static_cast<uintptr_t>(n_rows) - 1, v = static_cast<uintptr_t>(V);
+  const uintptr_t z0 = reinterpret_cast<uintptr_t>(logits), g0 = reinterpret_cast<uintptr_t>(grad);
+  const uintptr_t z1 = z0 + (n * static_cast<uintptr_t>(row_stride) + v) * item;
+  const uintptr_t g1 = g0 + (n * static_cast<uintptr_t>(grad_stride) + v) * item;
+  return z0 < g1 && g0 < z1 ? PR_ERR_INVALID_ARG : PR_OK;
+}
+
+LossRows loss_rows(const void* logits, int64_t n_rows, int32_t V, int64_t row_stride, const int32_t* ids,
+                   const float* temps, const float* weight, void* grad, int64_t grad_stride) {
+  LossRows a{};
+  a.logits = logits;
+  a.n_rows = n_rows;
+  a.V = V;
+  a.row_stride = row_stride;
+  a.ids = ids;
+  a.temperature = temps;
+  a.weight = weight;
+  a.grad = grad;
+  a.grad_stride = grad_stride;
+  return a;
+}
+
+// Upper 32 bits of SplitMix64's output (Steele, Lea and Flood, OOPSLA 2014)
+// for a step: the key of its random numbers.
+uint32_t step_key(uint64_t seed, int64_t step) {
+  uint64_t x = seed + static_cast<uint64_t>(step) * 0x9E3779B97F4A7C15ull;
+  x = (x ^ (x >> 30)) * 0xBF58476D1CE4E5B9ull;
+  x = (x ^ (x >> 27)) * 0x94D049BB133111EBull;
+  return static_cast<uint32_t>((x ^ (x >> 31)) >> 32);
 }
 
 bool params_ok(const pr_agg_params& p) {
@@ -501,6 +559,215 @@ void pr_stream_destroy(pr_stream* state) {
   (void)hipFree(state->block);
   (void)hipSetDevice(prev);
   delete state;
+}
+
+void pr_policy_params_default(pr_policy_params* params) {
+  if (params) *params = pr_policy_params{0.2, 0.2, 0.0, 1.0};
+}
+
+size_t pr_policy_loss_workspace(pr_dtype, int64_t n_rows, int32_t) { return policy_workspace_bytes(n_rows); }
+
+pr_status pr_policy_loss(const void* logits, pr_dtype dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,
+                         const int32_t* ids, const float* temperature, const float* weight, const float* advantage,
+                         const float* old_logprob, const float* ref_logprob, const pr_policy_params* params,
+                         float* loss, const pr_policy_tokens_t* out, void* grad, int64_t grad_stride,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  const pr_status st =
+      check_loss(logits, dtype, n_rows, vocab, row_stride, ids, temperature, weight, loss, grad, grad_stride);
+  if (st != PR_OK) return st;
+  if (n_rows > 0 && (!advantage || !old_logprob)) return PR_ERR_INVALID_ARG;
+  pr_policy_params p;
+  pr_policy_params_default(&p);
+  if (params) p = *params;
+  if (!(p.clip_low >= 0.0 && p.clip_low <= 1.0) || !(p.clip_high >= 0.0) || !(p.kl_coef >= 0.0) ||
+      !std::isfinite(p.kl_coef) || !std::isfinite(p.grad_scale) || (p.kl_coef > 0.0 && !ref_logprob && n_rows > 0))
+    return PR_ERR_INVALID_ARG;
+  const size_t need = policy_workspace_bytes(n_rows);
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return PR_ERR_INVALID_ARG;
+  PolicyArgs a{};
+  a.rows = loss_rows(logits, n_rows, vocab, row_stride, ids, temperature, weight, grad, grad_stride);
+  a.advantage = advantage;
+  a.old_logprob = old_logprob;
+  a.ref_logprob = ref_logprob;
+  a.clip_lo = 1.0 - p.clip_low;
+  a.clip_hi = 1.0 + p.clip_high;
+  a.kl_coef = p.kl_coef;
+  a.grad_scale = p.grad_scale;
+  a.loss = loss;
+  if (out) a.out = *out;
+  a.row_loss = static_cast<double*>(workspace);
+  return hip_status(launch_policy(a, dtype, as_stream(stream)));
+}
+
+void pr_preference_params_default(pr_preference_params* params) {
+  if (params) *params = pr_preference_params{0.1, 0.0, 0.0, 1.0};
+}
+
+size_t pr_preference_loss_workspace(pr_dtype dtype, int64_t n_rows, int32_t vocab, int32_t n_pairs) {
+  return preference_workspace_bytes(n_rows, n_pairs, preference_split(n_rows, vocab, dtype));
+}
+
+pr_status pr_preference_loss(const void* logits, pr_dtype dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,
+                             const int32_t* ids, const float* temperature, const float* weight,
+                             const int32_t* offsets, int32_t n_pairs, const float* ref_logprob,
+                             const pr_preference_params* params, float* loss, const pr_preference_out_t* out,
+                             void* grad, int64_t grad_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  const pr_status st =
+      check_loss(logits, dtype, n_rows, vocab, row_stride, ids, temperature, weight, loss, grad, grad_stride);
+  if (st != PR_OK) return st;
+  if (n_pairs < 0 || (n_pairs > 0 && !offsets) || (n_pairs == 0 && n_rows > 0)) return PR_ERR_INVALID_ARG;
+  if (n_pairs > (1 << 30) - 1) return PR_ERR_UNSUPPORTED;  // 2 n_pairs + 1 offsets are counted in 32 bits
+  pr_preference_params p;
+  pr_preference_params_default(&p);
+  if (params) p = *params;
+  if (!(p.beta > 0.0) || !std::isfinite(p.beta) || !(p.label_smoothing >= 0.0 && p.label_smoothing <= 1.0) ||
+      !std::isfinite(p.margin) || !std::isfinite(p.grad_scale))
+    return PR_ERR_INVALID_ARG;
+  const size_t need = pr_preference_loss_workspace(dtype, n_rows, vocab, n_pairs);
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return PR_ERR_INVALID_ARG;
+  PreferenceArgs a{};
+  a.rows = loss_rows(logits, n_rows, vocab, row_stride, ids, temperature, weight, grad, grad_stride);
+  a.offsets = offsets;
+  a.n_pairs = n_pairs;
+  a.ref_logprob = ref_logprob;
+  a.beta = p.beta;
+  a.label_smoothing = p.label_smoothing;
+  a.margin = p.margin;
+  a.grad_scale = p.grad_scale;
+  a.loss = loss;
+  if (out) a.out = *out;
+  a.G = preference_split(n_rows, vocab, dtype);
+  a.ws = workspace;
+  return hip_status(launch_preference(a, dtype, as_stream(stream)));
+}
+
+pr_status pr_adamw_create(const pr_adamw_tensor* tensors, int32_t n_tensors, pr_dtype param_dtype,
+                          pr_dtype grad_dtype, int32_t state_bits, uint64_t seed, pr_adamw** handle) {
+  if (!handle) return PR_ERR_INVALID_ARG;
+  *handle = nullptr;
+  if (n_tensors < 0 || (n_tensors > 0 && !tensors)) return PR_ERR_INVALID_ARG;
+  if ((param_dtype != PR_F32 && param_dtype != PR_BF16) || (grad_dtype != PR_F32 && grad_dtype != PR_BF16) ||
+      (state_bits != 8 && state_bits != 32))
+    return PR_ERR_INVALID_ARG;
+  const size_t state = state_bits == 8 ? 1 : 4;
+  for (int32_t j = 0; j < n_tensors; ++j) {
+    const pr_adamw_tensor& t = tensors[j];
+    if (t.n < 0 || t.n > (int64_t{1} << 42)) return PR_ERR_INVALID_ARG;
+    if (t.n == 0) continue;
+    if (!t.param || !t.m || !t.v || !aligned(t.param, dtype_size(param_dtype)) || !aligned(t.m, state) ||
+        !aligned(t.v, state) || (t.grad && !aligned(t.grad, dtype_size(grad_dtype))))
+      return PR_ERR_INVALID_ARG;
+    if (state_bits == 8 && (!t.m_exp || !t.v_exp)) return PR_ERR_INVALID_ARG;
+    if (t.copy && (param_dtype != PR_F32 || !aligned(t.copy, 2))) return PR_ERR_INVALID_ARG;
+  }
+  try {
+    pr_adamw* h = new pr_adamw();
+    h->block = nullptr;
+    h->has_grads = true;
+    std::vector<AdamTensor> plan(static_cast<size_t>(n_tensors));
+    std::vector<AdamChunk> chunks;
+    hipError_t e = hipSuccess;
+    try {
+      h->chunk_begin.resize(static_cast<size_t>(n_tensors) + 1);
+      int64_t block = 0, total = 0;
+      for (int32_t j = 0; j < n_tensors; ++j) total += (tensors[j].n + kAdamChunk - 1) / kAdamChunk;
+      chunks.reserve(static_cast<size_t>(total));
+      for (int32_t j = 0; j < n_tensors; ++j) {
+        const pr_adamw_tensor& t = tensors[j];
+        h->chunk_begin[static_cast<size_t>(j)] = static_cast<int64_t>(chunks.size());
+        plan[static_cast<size_t>(j)] = AdamTensor{t.param, t.grad, static_cast<uint16_t*>(t.copy), t.m, t.v,
+                                                  t.m_exp, t.v_exp, t.n, block};
+        if (t.n > 0 && !t.grad) h->has_grads = false;
+        block += (t.n + kAdamBlock - 1) / kAdamBlock;
+        for (int32_t k = 0; static_cast<int64_t>(k) * kAdamChunk < t.n; ++k) chunks.push_back(AdamChunk{j, k});
+      }
+      h->chunk_begin[static_cast<size_t>(n_tensors)] = static_cast<int64_t>(chunks.size());
+      const size_t b_plan = plan.size() * sizeof(AdamTensor), b_chunks = chunks.size() * sizeof(AdamChunk);
+      e = hipGetDevice(&h->device);
+      if (e == hipSuccess && b_plan > 0) {
+        e = hipMalloc(&h->block, b_plan + b_chunks);
+        char* b = static_cast<char*>(h->block);
+        if (e == hipSuccess) e = hipMemcpy(b, plan.data(), b_plan, hipMemcpyHostToDevice);
+        if (e == hipSuccess && b_chunks > 0) e = hipMemcpy(b + b_plan, chunks.data(), b_chunks, hipMemcpyHostToDevice);
+        h->plan.tensors = reinterpret_cast<const AdamTensor*>(b);
+        h->plan.chunks = reinterpret_cast<const AdamChunk*>(b + b_plan);
+      }
+    } catch (...) {
+      delete h;
+      throw;
+    }
+    if (e != hipSuccess) {
+      if (h->block) (void)hipFree(h->block);
+      delete h;
+      return hip_status(e);
+    }
+    h->plan.param_dtype = param_dtype;
+    h->plan.grad_dtype = grad_dtype;
+    h->plan.state_bits = state_bits;
+    h->seed = seed;
+    *handle = h;
+    return PR_OK;
+  } catch (...) {
+    return PR_ERR_NO_MEMORY;
+  }
+}
+
+pr_status pr_adamw_step(pr_adamw* handle, const void* const* grads, const pr_adamw_params* params, void* stream) {
+  if (!handle || !params) return PR_ERR_INVALID_ARG;
+  const pr_adamw_params& p = *params;
+  for (const double v : {p.lr, p.beta1, p.beta2, p.eps, p.weight_decay, p.grad_scale})
+    if (!std::isfinite(v)) return PR_ERR_INVALID_ARG;
+  if (!(p.beta1 >= 0.0 && p.beta1 < 1.0) || !(p.beta2 >= 0.0 && p.beta2 < 1.0) || !(p.eps >= 0.0) || p.step < 1)
+    return PR_ERR_INVALID_ARG;
+  if (!grads && !handle->has_grads) return PR_ERR_INVALID_ARG;
+  AdamScalars s{};
+  s.beta1 = static_cast<float>(p.beta1);
+  s.one_minus_beta1 = static_cast<float>(1.0 - p.beta1);
+  s.beta2 = static_cast<float>(p.beta2);
+  s.one_minus_beta2 = static_cast<float>(1.0 - p.beta2);
+  s.decay = static_cast<float>(1.0 - p.lr * p.weight_decay);
+  s.rate = static_cast<float>(p.lr / (1.0 - std::pow(p.beta1, static_cast<double>(p.step))));
+  s.c2 = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(p.beta2, static_cast<double>(p.step))));
+  s.eps = static_cast<float>(p.eps);
+  s.grad_scale = static_cast<float>(p.grad_scale);
+  s.key = step_key(handle->seed, p.step);
+  const int32_t n = static_cast<int32_t>(handle->chunk_begin.size()) - 1;
+  if (!grads)
+    return hip_status(launch_adamw(handle->plan, 0, handle->chunk_begin[static_cast<size_t>(n)], s, nullptr, 0,
+                                   as_stream(stream)));
+  const size_t item = dtype_size(handle->plan.grad_dtype);
+  for (int32_t j = 0; j < n; ++j)
+    if (grads[j] && !aligned(grads[j], item)) return PR_ERR_INVALID_ARG;
+  for (int32_t j = 0; j < n; j += kAdamGrads) {
+    const int32_t to = n - j < kAdamGrads ? n : j + kAdamGrads;
+    AdamGrads g{};
+    for (int32_t i = j; i < to; ++i) g.p[i - j] = grads[i];
+    const hipError_t e = launch_adamw(handle->plan, handle->chunk_begin[static_cast<size_t>(j)],
+                                      handle->chunk_begin[static_cast<size_t>(to)], s, &g, j, as_stream(stream));
+    if (e != hipSuccess) return hip_status(e);
+  }
+  return PR_OK;
+}
+
+pr_status pr_adamw_moments(pr_adamw* handle, void* m, void* v, void* stream) {
+  if (!handle) return PR_ERR_INVALID_ARG;
+  if (handle->plan.state_bits != 8) return PR_ERR_UNSUPPORTED;
+  const int64_t chunks = handle->chunk_begin.back();
+  if (chunks == 0) return PR_OK;
+  if (!m || !v || !aligned(m, 2) || !aligned(v, 2)) return PR_ERR_INVALID_ARG;
+  return hip_status(launch_adamw_moments(handle->plan, chunks, static_cast<uint16_t*>(m), static_cast<uint16_t*>(v),
+                                         as_stream(stream)));
+}
+
+void pr_adamw_destroy(pr_adamw* handle) {
+  if (!handle) return;
+  int prev = 0;
+  (void)hipGetDevice(&prev);
+  (void)hipSetDevice(handle->device);
+  (void)hipDeviceSynchronize();
+  (void)hipFree(handle->block);
+  (void)hipSetDevice(prev);
+  delete handle;
 }
 
 }  // extern "C"
