@@ -464,39 +464,47 @@ class StreamState:
 # ---------------------------------------------------------------------------
 # Training: losses over logit rows, and the optimizer's step.
 
-def _check_current(device, what: str):
-    """Launches go to the current device's stream: the tensors have to be there."""
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
+def _check_current(device, what: str) -> int:
+    """Launches go to the current device's stream: the tensors have to be there. Returns that stream."""
+    current = torch.cuda.current_device()
+    if device.type != "cuda" or device.index != current:
         raise ValueError(f"{what} must be on the current CUDA device, got {device}")
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(current)
 
 
 def _check_row_floats(device, n: int, **tensors):
     for name, t in tensors.items():
-        if t is not None and (t.dtype != torch.float32 or t.device != device or t.shape != (n,) or not t.is_contiguous()):
+        if t is not None and (t.dtype != torch.float32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous()
+                              or t.device != device):
             raise ValueError(f"{name} must be a contiguous float32 [{n}] tensor on {device}")
 
 
-def _check_loss(logits, ids, temperature, weight, grad):
-    """Checks of a loss's rows; returns them with the temperature as a tensor, and the gradient to write or None."""
+def _rows_apart(t, V: int) -> bool:
+    """Whether a 2-D tensor's rows are contiguous and do not overlap."""
+    return t.stride(1) == 1 and (t.shape[0] <= 1 or t.stride(0) >= V)
+
+
+def _check_loss(logits, ids, temperature, grad):
+    """Checks of a loss's rows. Returns the stream, the device, the type's code, the temperature as a tensor, and the
+    gradient to write or None."""
     if logits.dim() != 2:
         raise ValueError("logits must be a 2-D CUDA tensor with unit stride along the vocabulary")
     n, V = logits.shape
-    _dtype_code(logits)
-    _check_current(logits.device, "logits")
-    temperature = _as_row_tensor(temperature, n, logits.device)
-    if logits.stride(1) != 1 or (n > 1 and logits.stride(0) < V):
+    device = logits.device
+    code = _dtype_code(logits)
+    stream = _check_current(device, "logits")
+    if not _rows_apart(logits, V):
         raise ValueError("logits must be a 2-D CUDA tensor with unit stride along the vocabulary and rows apart")
-    _check_index_tensor(ids, "ids", logits.device, n)
-    _check_row_floats(logits.device, n, temperature=temperature, weight=weight)
+    _check_index_tensor(ids, "ids", device, n)
     if grad is True:
-        grad = torch.empty(n, V, dtype=logits.dtype, device=logits.device)
+        grad = torch.empty((n, V), dtype=logits.dtype, device=device)
     elif grad is False or grad is None:
         grad = None
-    elif (grad.dtype != logits.dtype or grad.shape != logits.shape or grad.device != logits.device
-          or grad.stride(1) != 1 or (n > 1 and grad.stride(0) < V)):
-        raise ValueError(f"grad must be a {logits.dtype} {list(logits.shape)} tensor on {logits.device} with unit "
-                         "stride along the vocabulary and rows apart")
-    return temperature, grad
+    elif (grad.dtype != logits.dtype or grad.shape != logits.shape or grad.device != device
+          or not _rows_apart(grad, V)):
+        raise ValueError(f"grad must be a {logits.dtype} {list(logits.shape)} tensor on {device} with unit stride along "
+                         "the vocabulary and rows apart")
+    return stream, device, code, _as_row_tensor(temperature, n, device), grad
 
 
 def _row_stride(t) -> int:
@@ -504,13 +512,22 @@ def _row_stride(t) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
 
 
-def _scratch(workspace, need: int, device):
-    """The caller's workspace where it serves, else one of this call; and its bytes."""
-    _check_workspace(workspace, device)
-    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    if need and (size < need or workspace.data_ptr() % 16):
-        workspace, size = torch.empty(need, dtype=torch.uint8, device=device), need
-    return workspace, size
+def _loss_outputs(sizes, workspace, need: int, device):
+    """Float32 outputs of these sizes and the scratch of a call, from one allocation (see _outputs): the caller's
+    workspace where it serves, else a part of it. Returns the outputs, the workspace's address and its bytes."""
+    if workspace is not None:
+        _check_workspace(workspace, device)
+        have = workspace.numel() * workspace.element_size()
+        if have >= need and workspace.data_ptr() % 16 == 0:
+            return _split_floats(sizes, device), workspace.data_ptr(), have
+    *out, scratch = _split_floats([*sizes, (need + 3) // 4], device)
+    return out, scratch.data_ptr(), need
+
+
+def _split_floats(sizes, device):
+    """Float32 tensors of these sizes, each 16-byte aligned, from one allocation (see _outputs)."""
+    parts = [p for k in sizes for p in (k, -k % 4)]
+    return torch.empty(sum(parts), dtype=torch.float32, device=device).unsafe_split_with_sizes(parts)[::2]
 
 
 def policy_loss(logits: torch.Tensor, ids: torch.Tensor, temperature, weight: torch.Tensor, advantage: torch.Tensor,
@@ -535,23 +552,22 @@ def policy_loss(logits: torch.Tensor, ids: torch.Tensor, temperature, weight: to
     ``workspace``: optional device scratch of this call, not shared with one
     that may overlap.
     """
-    temperature, grad = _check_loss(logits, ids, temperature, weight, grad)
+    stream, device, code, temperature, grad = _check_loss(logits, ids, temperature, grad)
     n, V = logits.shape
-    _check_row_floats(logits.device, n, advantage=advantage, old_logprob=old_logprob, ref_logprob=ref_logprob)
+    _check_row_floats(device, n, temperature=temperature, weight=weight, advantage=advantage, old_logprob=old_logprob,
+                      ref_logprob=ref_logprob)
     L = _abi.lib()
-    code = _dtype_code(logits)
-    need = L.pr_policy_loss_workspace(code, n, V)
-    workspace, ws_bytes = _scratch(workspace, need, logits.device)
-    out = dict(zip(("logprob", "ratio", "kl"), _outputs(3, n, torch.float32, logits.device)))
-    out["flags"] = torch.empty(n, dtype=torch.int32, device=logits.device)
-    out["loss"] = torch.empty(1, dtype=torch.float32, device=logits.device)
-    params = _abi.PolicyParams(float(clip_low), float(clip_high), float(kl_coef), float(grad_scale))
-    tokens = _abi.PolicyTokens(*[out[k].data_ptr() for k in _abi.POLICY_FIELDS])
-    st = L.pr_policy_loss(_ptr(logits), code, n, V, _row_stride(logits), _ptr(ids), _ptr(temperature), _ptr(weight),
-                          _ptr(advantage), _ptr(old_logprob), _ptr(ref_logprob), C.byref(params), _ptr(out["loss"]),
-                          C.byref(tokens), _ptr(grad), 0 if grad is None else _row_stride(grad), _ptr(workspace),
-                          ws_bytes, _stream_handle())
+    (logprob, ratio, kl, loss), ws, ws_bytes = _loss_outputs((n, n, n, 1), workspace,
+                                                             L.pr_policy_loss_workspace(code, n, V), device)
+    flags = torch.empty(n, dtype=torch.int32, device=device)
+    params = _abi.PolicyParams(clip_low, clip_high, kl_coef, grad_scale)
+    tokens = _abi.PolicyTokens(logprob.data_ptr(), ratio.data_ptr(), kl.data_ptr(), flags.data_ptr())
+    st = L.pr_policy_loss(logits.data_ptr(), code, n, V, _row_stride(logits), ids.data_ptr(), temperature.data_ptr(),
+                          weight.data_ptr(), advantage.data_ptr(), old_logprob.data_ptr(), _ptr(ref_logprob),
+                          C.byref(params), loss.data_ptr(), C.byref(tokens), _ptr(grad),
+                          0 if grad is None else _row_stride(grad), ws, ws_bytes, stream)
     _abi.check("pr_policy_loss", st)
+    out = {"loss": loss, "logprob": logprob, "ratio": ratio, "kl": kl, "flags": flags}
     if grad is not None:
         out["grad"] = grad
     return out
@@ -575,29 +591,25 @@ def preference_loss(logits: torch.Tensor, ids: torch.Tensor, temperature, weight
     (h) [n_pairs], ``seq_logratio`` (q) [2 n_pairs], ``logprob``, ``flags``
     [n_rows] and, when wanted, ``grad``.
     """
-    temperature, grad = _check_loss(logits, ids, temperature, weight, grad)
+    stream, device, code, temperature, grad = _check_loss(logits, ids, temperature, grad)
     n, V = logits.shape
-    _check_row_floats(logits.device, n, ref_logprob=ref_logprob)
-    _check_index_tensor(offsets, "offsets", logits.device)
+    _check_row_floats(device, n, temperature=temperature, weight=weight, ref_logprob=ref_logprob)
+    _check_index_tensor(offsets, "offsets", device)
     if offsets.shape[0] % 2 == 0:
         raise ValueError("offsets must have 2 n_pairs + 1 entries")
     n_pairs = offsets.shape[0] // 2
     L = _abi.lib()
-    code = _dtype_code(logits)
-    need = L.pr_preference_loss_workspace(code, n, V, n_pairs)
-    workspace, ws_bytes = _scratch(workspace, need, logits.device)
-    out = dict(zip(("pair_loss", "pair_logit"), _outputs(2, n_pairs, torch.float32, logits.device)))
-    out["seq_logratio"] = torch.empty(2 * n_pairs, dtype=torch.float32, device=logits.device)
-    out["logprob"] = torch.empty(n, dtype=torch.float32, device=logits.device)
-    out["flags"] = torch.empty(n, dtype=torch.int32, device=logits.device)
-    out["loss"] = torch.empty(1, dtype=torch.float32, device=logits.device)
-    params = _abi.PreferenceParams(float(beta), float(label_smoothing), float(margin), float(grad_scale))
-    values = _abi.PreferenceOut(*[out[k].data_ptr() for k in _abi.PREFERENCE_FIELDS])
-    st = L.pr_preference_loss(_ptr(logits), code, n, V, _row_stride(logits), _ptr(ids), _ptr(temperature), _ptr(weight),
-                              _ptr(offsets), n_pairs, _ptr(ref_logprob), C.byref(params), _ptr(out["loss"]),
-                              C.byref(values), _ptr(grad), 0 if grad is None else _row_stride(grad), _ptr(workspace),
-                              ws_bytes, _stream_handle())
+    (logprob, q, pair, h, loss), ws, ws_bytes = _loss_outputs(
+        (n, 2 * n_pairs, n_pairs, n_pairs, 1), workspace, L.pr_preference_loss_workspace(code, n, V, n_pairs), device)
+    flags = torch.empty(n, dtype=torch.int32, device=device)
+    params = _abi.PreferenceParams(beta, label_smoothing, margin, grad_scale)
+    values = _abi.PreferenceOut(pair.data_ptr(), h.data_ptr(), q.data_ptr(), logprob.data_ptr(), flags.data_ptr())
+    st = L.pr_preference_loss(logits.data_ptr(), code, n, V, _row_stride(logits), ids.data_ptr(),
+                              temperature.data_ptr(), weight.data_ptr(), offsets.data_ptr(), n_pairs,
+                              _ptr(ref_logprob), C.byref(params), loss.data_ptr(), C.byref(values), _ptr(grad),
+                              0 if grad is None else _row_stride(grad), ws, ws_bytes, stream)
     _abi.check("pr_preference_loss", st)
+    out = {"loss": loss, "pair_loss": pair, "pair_logit": h, "seq_logratio": q, "logprob": logprob, "flags": flags}
     if grad is not None:
         out["grad"] = grad
     return out
@@ -720,10 +732,10 @@ class AdamW:
             pointers = (C.c_void_p * len(grads))(*[None if t is None else t.data_ptr() for t in grads])
         elif self.grads is None:
             raise ValueError("step needs grads: none were given at construction")
-        _check_current(self.device, "the optimizer's tensors")
+        stream = _check_current(self.device, "the optimizer's tensors")
         p = _abi.AdamWParams(float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), float(grad_scale),
                              self.steps + 1)
-        _abi.check("pr_adamw_step", _abi.lib().pr_adamw_step(self._h, pointers, C.byref(p), _stream_handle()))
+        _abi.check("pr_adamw_step", _abi.lib().pr_adamw_step(self._h, pointers, C.byref(p), stream))
         self.steps += 1
 
     def moments(self, out=None):
@@ -747,9 +759,8 @@ class AdamW:
             out = tuple(torch.zeros(total, dtype=torch.bfloat16, device=self.device) for _ in range(2))
         for t in out:
             self._check(t, "out", torch.bfloat16, total)
-        _check_current(self.device, "the optimizer's tensors")
-        _abi.check("pr_adamw_moments",
-                   _abi.lib().pr_adamw_moments(self._h, _ptr(out[0]), _ptr(out[1]), _stream_handle()))
+        stream = _check_current(self.device, "the optimizer's tensors")
+        _abi.check("pr_adamw_moments", _abi.lib().pr_adamw_moments(self._h, _ptr(out[0]), _ptr(out[1]), stream))
         if given:
             return out
         lists = ([], [])

@@ -20,8 +20,9 @@ namespace {
 using scan::head_elems;
 using scan::neg_inf_vec;
 
+constexpr int kCUs = 256;  // compute units of the device
 constexpr int kStatsBlock = 256;
-constexpr int kGradBlock = 256;
+constexpr int kGradBlock = 512;
 constexpr int kSumBlock = 1024;
 
 // What the gradient pass needs of a row: dz_v = k 2^fma(z_v, c, -A) for every
@@ -97,8 +98,8 @@ struct RowValue {
   uint32_t flags;  // 0 or the reasons why l is NaN
 };
 
-// l of a row from its sum of exps. The exact residual of A = round(m c) moves
-// S to the exact reference, so that the largest logit contributes exactly 1.
+// l of a row from its sum of exps, in 64 bits. S is relative to A = round(m c),
+// whose exact residual goes off its logarithm.
 __device__ __forceinline__ RowValue row_value(const RowSum& p, float T, float c, int32_t y, int32_t V, float zy) {
   RowValue v;
   v.A = p.m * c;
@@ -112,7 +113,7 @@ __device__ __forceinline__ RowValue row_value(const RowSum& p, float T, float c,
     return v;
   }
   const double delta = static_cast<double>(fmaf(p.m, c, -v.A));
-  const double lnS = ln_sum(static_cast<double>(p.S) * exp2(-delta));
+  const double lnS = log(static_cast<double>(p.S)) - delta * 0.69314718055994530942;
   v.l = (static_cast<double>(zy) - static_cast<double>(p.m)) / static_cast<double>(T) - lnS;
   return v;
 }
@@ -125,7 +126,7 @@ __device__ __forceinline__ RowGrad row_grad(double coef, double l, float A, floa
     const float nan = __uint_as_float(0x7fc00000u);
     return RowGrad{0.0f, 0.0f, nan, nan};
   }
-  return RowGrad{A, c, static_cast<float>(-coef / static_cast<double>(S)), static_cast<float>(-coef * expm1(l))};
+  return RowGrad{A, c, static_cast<float>(-coef / static_cast<double>(S)), static_cast<float>(-coef) * expm1f(static_cast<float>(l))};
 }
 
 template <typename Tin>
@@ -141,7 +142,7 @@ __device__ __forceinline__ float token_logit(const LossRows& a, int64_t r, int32
 // The policy loss of one row: outputs, its term of the loss and its gradient's factors.
 __device__ __forceinline__ RowGrad policy_row(const PolicyArgs& a, int64_t r, const RowValue& v, float T, float c,
                                               float S, float w) {
-  const double A = a.advantage[r], ratio = exp(v.l - static_cast<double>(a.old_logprob[r]));
+  const double A = a.advantage[r], ratio = expf(static_cast<float>(v.l - static_cast<double>(a.old_logprob[r])));
   const double free = ratio * A, held = fmin(fmax(ratio, a.clip_lo), a.clip_hi) * A;
   const bool clipped = free > held;
   double kl = 0.0, rise = 0.0;
@@ -182,9 +183,10 @@ __device__ __forceinline__ double block_sum(const double* v, int64_t n) {
   return t;
 }
 
-__global__ __launch_bounds__(kSumBlock) void loss_sum_kernel(const double* v, int64_t n, double factor, float* loss) {
+// loss = (sum of v) / over
+__global__ __launch_bounds__(kSumBlock) void loss_sum_kernel(const double* v, int64_t n, double over, float* loss) {
   const double s = block_sum(v, n);
-  if (threadIdx.x == 0) loss[0] = static_cast<float>(s * factor);
+  if (threadIdx.x == 0) loss[0] = static_cast<float>(s / over);
 }
 
 // The sum of exps of a stretch of a row (the whole row when G = 1).
@@ -240,9 +242,7 @@ template <typename Tin>
 struct GradVec;
 template <>
 struct GradVec<float> {
-  struct __attribute__((packed, aligned(4))) Store {
-    vec4u v;
-  };
+  typedef uint32_t Store __attribute__((ext_vector_type(4), aligned(4)));
   __device__ __forceinline__ static vec4u pack(const float (&g)[4]) {
     return vec4u{__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3])};
   }
@@ -258,9 +258,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {  // round to
 
 template <>
 struct GradVec<uint16_t> {
-  struct __attribute__((packed, aligned(2))) Store {
-    vec4u v;
-  };
+  typedef uint32_t Store __attribute__((ext_vector_type(4), aligned(2)));
   __device__ __forceinline__ static vec4u pack(const float (&g)[8]) {
     return vec4u{pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[4], g[5]), pack_bf16(g[6], g[7])};
   }
@@ -271,69 +269,332 @@ struct GradVec<uint16_t> {
 
 template <typename Tin>
 __device__ __forceinline__ void store_grad(Tin* at, const vec4u& v) {
-  reinterpret_cast<typename GradVec<Tin>::Store*>(at)->v = v;
+  *reinterpret_cast<typename GradVec<Tin>::Store*>(at) = v;
+}
+// The same past the caches.
+template <typename Tin>
+__device__ __forceinline__ void stream_grad(Tin* at, const vec4u& v) {
+  typedef typename GradVec<Tin>::Store Store;
+  __builtin_nontemporal_store(static_cast<Store>(v), reinterpret_cast<Store*>(at));
 }
 
 __device__ __forceinline__ float grad_of(float z, const RowGrad& q) { return q.k * fast_exp2(fmaf(z, q.c, -q.A)); }
 
-// The gradient of a stretch of a row. Each element is read and written by one
-// thread, so the gradient may take the logits' place.
-template <typename Tin>
-__global__ __launch_bounds__(kGradBlock) void grad_kernel(LossRows a, const RowGrad* rg, int32_t segs) {
+// Vectors per thread of a workgroup of the gradient pass.
+constexpr int kGradPer = 1;
+
+// The gradient of a stretch of a row (blockIdx.x) of the rows from `first` on
+// (blockIdx.y). Each element is read and written by one thread, so the
+// gradient may take the logits' place.
+//
+// SUM: the first workgroup also takes the loss that waits for the kernel
+// before this one, the mean of `sum`'s values. (Only small grids do that: it
+// saves a launch, but costs every workgroup about 10 %.)
+template <typename Tin, bool SUM>
+__global__ __launch_bounds__(kGradBlock) void grad_kernel(LossRows a, const RowGrad* rg, int64_t first,
+                                                          const double* sum, int32_t n_sum, float* loss) {
   constexpr int VEC = Elem<Tin>::kVec;
-  const int64_t r = blockIdx.x / segs;
-  const int seg = blockIdx.x % segs;
+  if (SUM && blockIdx.x == 0 && blockIdx.y == 0) {
+    const double s = block_sum(sum, n_sum);
+    if (threadIdx.x == 0) loss[0] = static_cast<float>(s / n_sum);
+  }
+  const int64_t r = first + blockIdx.y;
   const RowGrad q = rg[r];
   const Tin* row = row_ptr<Tin>(a, r);
   Tin* out = static_cast<Tin*>(a.grad) + r * a.grad_stride;
-  const int64_t h = head_elems<Tin>(row, a.V), nvec = (a.V - h) / VEC;
-  const int64_t vb = nvec * seg / segs, ve = nvec * (seg + 1) / segs;
+  const int32_t h = static_cast<int32_t>(head_elems<Tin>(row, a.V)), nvec = (a.V - h) / VEC, tail = h + nvec * VEC;
   const int t = threadIdx.x;
   const int32_t y = a.ids[r];
   const bool zero = q.k == 0.0f && q.gy == 0.0f;
-  const int64_t tail = h + nvec * VEC;
-  if (seg == 0 && t < h)
-    GradVec<Tin>::store1(out, t, zero ? 0.0f : t == y ? q.gy : grad_of(Elem<Tin>::load1(row, t), q));
-  if (seg == segs - 1 && tail + t < a.V)
-    GradVec<Tin>::store1(out, tail + t,
-                         zero ? 0.0f : tail + t == y ? q.gy : grad_of(Elem<Tin>::load1(row, tail + t), q));
-  if (zero) {
-    for (int64_t j = vb + t; j < ve; j += kGradBlock) store_grad(out + h + j * VEC, vec4u{0, 0, 0, 0});
-    return;
+  if (blockIdx.x == 0 && t < 16) {
+    const int32_t e = t < 8 ? (t < h ? t : a.V) : tail + t - 8;  // the thread's scalar element
+    if (e < a.V) GradVec<Tin>::store1(out, e, zero ? 0.0f : e == y ? q.gy : grad_of(Elem<Tin>::load1(row, e), q));
   }
   const vec4u* vp = reinterpret_cast<const vec4u*>(row + h);
-  for (int64_t j = vb + t; j < ve; j += kGradBlock) {
-    float z[VEC];
-    Elem<Tin>::unpack(vp[j], z);
+  const int32_t j0 = blockIdx.x * (kGradBlock * kGradPer) + t;
+  vec4u v[kGradPer];
+  if (!zero) {
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) z[k] = grad_of(z[k], q);
-    const int64_t at = y - (h + j * VEC);
-    if (at >= 0 && at < VEC) {
+    for (int u = 0; u < kGradPer; ++u)
+      if (j0 + u * kGradBlock < nvec) v[u] = __builtin_nontemporal_load(vp + j0 + u * kGradBlock);
+  }
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) z[k] = k == at ? q.gy : z[k];
+  for (int u = 0; u < kGradPer; ++u) {
+    const int32_t j = j0 + u * kGradBlock;
+    if (j >= nvec) return;
+    vec4u g{0, 0, 0, 0};
+    if (!zero) {
+      float z[VEC];
+      Elem<Tin>::unpack(v[u], z);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) z[k] = grad_of(z[k], q);
+      const int32_t at = y - (h + j * VEC);
+      if (at >= 0 && at < VEC) {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) z[k] = k == at ? q.gy : z[k];
+      }
+      g = GradVec<Tin>::pack(z);
     }
-    store_grad(out + h + j * VEC, GradVec<Tin>::pack(z));
+    stream_grad(out + h + static_cast<int64_t>(j) * VEC, g);
   }
 }
 
-// Vectors of a row that one workgroup of the gradient pass takes.
-constexpr int64_t kGradSegment = 8 * kGradBlock;
+// Makes the compiler forget what it knows of a vector, so that it unpacks it
+// anew in each pass instead of keeping 8 floats of each through all of them.
+__device__ __forceinline__ void forget(vec4u& v) { asm volatile("" : "+v"(v)); }
+
+// 16 bytes of each lane from memory into LDS: lane i's go to slots[i]
+// (`slots` is the wave's).
+__device__ __forceinline__ void load_to_lds(const vec4u* from, vec4u* slots) {
+  __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void*)slots, 16, 0, 0);
+}
+
+// A row as the fused kernel sees it: its vectors start at the first 16-byte
+// boundary, h elements in; up to 2 x 7 elements before and after are scalars.
+template <typename Tin>
+struct RowView {
+  const Tin* row;
+  Tin* out;
+  int32_t h, nvec;
+
+  __device__ __forceinline__ RowView(const LossRows& a, int64_t r) {
+    row = row_ptr<Tin>(a, r);
+    out = static_cast<Tin*>(a.grad) + r * a.grad_stride;
+    h = static_cast<int32_t>(head_elems<Tin>(row, a.V));
+    nvec = (a.V - h) / Elem<Tin>::kVec;
+  }
+  __device__ __forceinline__ int32_t tail() const { return h + nvec * Elem<Tin>::kVec; }
+  // Vector at + t of the row and of its gradient: a place that the wave shares
+  // plus 16 t, so that an address takes one register of a lane.
+  __device__ __forceinline__ const vec4u* in(int32_t at, uint32_t t) const {
+    return reinterpret_cast<const vec4u*>(reinterpret_cast<const char*>(row + h) + static_cast<int64_t>(at) * 16 +
+                                          t * 16u);
+  }
+  __device__ __forceinline__ Tin* to(int32_t at, uint32_t t) const {
+    return reinterpret_cast<Tin*>(reinterpret_cast<char*>(out + h) + static_cast<int64_t>(at) * 16 + t * 16u);
+  }
+};
+
+// Vectors of the rows that policy_row_kernel holds, by its two sizes.
+constexpr int64_t kSmallRowVectors = 19 * 7 * kWave, kRowVectors = 20 * 15 * kWave;
+
+// Most rows whose order policy_row_kernel works out for itself.
+constexpr int64_t kListedRows = 65536;
+constexpr int kListed = kListedRows / kCUs + 1;
+
+// The policy loss of a row and its gradient in one read of the row.
+//
+// A workgroup keeps the row on the chip between its sum and its gradient: its
+// first DW waves hold NR vectors per thread in registers and NL in LDS (which
+// the loads fill without passing through registers). One more wave takes what
+// is scalar in a row (its inputs, the elements outside the vectors, the loss
+// in 64 bits): the registers for that are not taken from those that hold the
+// row.
+//
+// The grid is the workgroups that run at once. Memory serves loads and stores
+// best when they do not mix, and workgroups that start together and do the
+// same stay together: so the rows that count are dealt out by their rank
+// among those that do, and the zero gradients of the others are written last.
+template <typename Tin, int DW, int NR, int NL>
+__global__ __launch_bounds__((DW + 1) * kWave) void policy_row_kernel(PolicyArgs a) {
+  constexpr int VEC = Elem<Tin>::kVec, NT = DW * kWave;
+  __shared__ vec4u held[NL * NT];
+  __shared__ float sh_m[DW + 1], sh_s[DW + 1];
+  __shared__ RowGrad sh_q;
+  __shared__ int32_t rows_on[kListed], rows_off[kListed];
+  __shared__ uint32_t sh_n[DW + 1];
+  static_assert(DW < kWave, "one wave merges the waves");
+  const int lane = threadIdx.x % kWave;
+  // As a scalar, so that what follows branches by wave and not by lane: both
+  // branches pass the same barriers.
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+  const int32_t V = a.rows.V;
+  const int64_t n = a.rows.n_rows, G = gridDim.x;
+
+  // The workgroup's rows: of the rows that count those of rank b, b + G, ..
+  // (b the workgroup), and likewise of the others. Each thread counts a
+  // stretch of rows; the counts' prefix sums give the ranks.
+  const bool listed = n > G && n <= kListedRows;
+  uint32_t n_on = 0, n_off = 0;
+  if (listed) {
+    const uint32_t per = static_cast<uint32_t>((n + blockDim.x - 1) / blockDim.x);
+    const uint32_t lo = min(static_cast<uint32_t>(n), threadIdx.x * per), hi = min(static_cast<uint32_t>(n), lo + per);
+    uint32_t on = 0;
+    for (uint32_t i = lo; i < hi; ++i) on += a.rows.weight[i] != 0.0f ? 1u : 0u;
+    const uint32_t scan = wave_incl_scan_u(on);
+    if (lane == kWave - 1) sh_n[wave] = scan;
+    __syncthreads();
+    uint32_t rank = scan - on;
+    for (int k = 0; k <= DW; ++k) {
+      if (k < wave) rank += sh_n[k];
+      n_on += sh_n[k];
+    }
+    n_off = static_cast<uint32_t>(n) - n_on;
+    for (uint32_t i = lo; i < hi; ++i) {
+      const bool counts = a.rows.weight[i] != 0.0f;
+      const uint32_t k = counts ? rank : i - rank;
+      if (k % static_cast<uint32_t>(G) == blockIdx.x) (counts ? rows_on : rows_off)[k / G] = static_cast<int32_t>(i);
+      rank += counts ? 1u : 0u;
+    }
+    __syncthreads();
+    const uint32_t b = blockIdx.x, g = static_cast<uint32_t>(G);
+    n_on = n_on > b ? (n_on - b - 1) / g + 1 : 0u;
+    n_off = n_off > b ? (n_off - b - 1) / g + 1 : 0u;
+  }
+  // A row for each workgroup, or too many to list: they are dealt out by row,
+  // and the turn of a row that does not count is passed over.
+  const int64_t turns = listed ? n_on : n > blockIdx.x ? (n - blockIdx.x - 1) / G + 1 : 0;
+  const int64_t turns_off = listed ? n_off : turns;
+  auto row_of = [&](const int32_t* list, int64_t k) -> int64_t {
+    return listed ? static_cast<int64_t>(__builtin_amdgcn_readfirstlane(list[k])) : blockIdx.x + k * G;
+  };
+
+  if (wave == DW) {
+    for (int64_t k = 0; k < turns; ++k) {
+      const int64_t r = row_of(rows_on, k);
+      const RowView<Tin> x(a.rows, r);
+      const float w = a.rows.weight[r];
+      if (w == 0.0f) continue;
+      const int32_t e = lane < 8 ? (lane < x.h ? lane : V) : x.tail() + lane - 8;  // the lane's scalar element
+      const float T = a.rows.temperature[r], c = scale_of(T);
+      const int32_t y = a.rows.ids[r];
+      const float zy = token_logit<Tin>(a.rows, r, y);
+      const float z = e < V ? Elem<Tin>::load1(x.row, e) : -INFINITY;
+      float m = wave_max(z);
+      if (lane == 0) sh_m[DW] = m;
+      __syncthreads();
+      m = wave_max(lane <= DW ? sh_m[lane] : -INFINITY);
+      const float A = fmaxf(m * c, kNegSentinel);
+      const float own = wave_sum(fast_exp2(fmaf(z, c, -A)));
+      __syncthreads();
+      const float S = wave_sum(lane < DW ? sh_s[lane] : lane == DW ? own : 0.0f);
+      const RowGrad q = policy_row(a, r, row_value(RowSum{m, S}, T, c, y, V, zy), T, c, S, w);
+      if (lane == 0) sh_q = q;
+      __syncthreads();
+      if (e < V) GradVec<Tin>::store1(x.out, e, e == y ? q.gy : grad_of(z, q));
+    }
+    for (int64_t k = 0; k < turns_off; ++k) {
+      const int64_t r = row_of(rows_off, k);
+      if (a.rows.weight[r] != 0.0f) continue;
+      const RowView<Tin> x(a.rows, r);
+      const int32_t e = lane < 8 ? (lane < x.h ? lane : V) : x.tail() + lane - 8;
+      if (lane == 0) policy_masked(a, r);
+      if (e < V) GradVec<Tin>::store1(x.out, e, 0.0f);
+    }
+    return;
+  }
+
+  const int t = threadIdx.x;  // below NT
+  for (int64_t k = 0; k < turns; ++k) {
+    const int64_t r = row_of(rows_on, k);
+    if (!listed && a.rows.weight[r] == 0.0f) continue;
+    const RowView<Tin> x(a.rows, r);
+    // The lanes of a wave fill consecutive 16-byte slots of LDS. Only these
+    // lanes read them again, so no barrier is needed, only their arrival (and
+    // that the previous row's have been read).
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int u = 0; u < NL; ++u)
+      if (t < x.nvec - u * NT) load_to_lds(x.in(u * NT, t), held + u * NT + wave * kWave);
+    vec4u v[NR];
+#pragma unroll
+    for (int u = 0; u < NR; ++u)
+      v[u] = t < x.nvec - (NL + u) * NT ? *x.in((NL + u) * NT, t) : neg_inf_vec<Tin>();
+    const float c = scale_of(a.rows.temperature[r]);
+    const int32_t y = a.rows.ids[r];
+
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    auto in_lds = [&](int u) { return t < x.nvec - u * NT ? held[u * NT + t] : neg_inf_vec<Tin>(); };
+
+    float m = -INFINITY;
+    auto top = [&](const vec4u& p) {
+      float z[VEC];
+      Elem<Tin>::unpack(p, z);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) m = fmaxf(m, z[i]);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+#pragma unroll
+    for (int u = 0; u < NL; ++u) top(in_lds(u));
+#pragma unroll
+    for (int u = 0; u < NR; ++u) top(v[u]);
+    m = wave_max(m);
+    if (lane == 0) sh_m[wave] = m;
+    __syncthreads();
+    m = wave_max(lane <= DW ? sh_m[lane] : -INFINITY);
+    const float A = fmaxf(m * c, kNegSentinel);
+    float S = 0.0f;
+    auto sum = [&](const vec4u& p) {
+      float z[VEC];
+      Elem<Tin>::unpack(p, z);
+      float s0 = fast_exp2(fmaf(z[0], c, -A)), s1 = fast_exp2(fmaf(z[1], c, -A));
+#pragma unroll
+      for (int i = 2; i < VEC; i += 2) {
+        s0 += fast_exp2(fmaf(z[i], c, -A));
+        s1 += fast_exp2(fmaf(z[i + 1], c, -A));
+      }
+      S += s0 + s1;
+      __builtin_amdgcn_sched_barrier(0);
+    };
+#pragma unroll
+    for (int u = 0; u < NL; ++u) sum(in_lds(u));
+#pragma unroll
+    for (int u = 0; u < NR; ++u) {
+      forget(v[u]);
+      sum(v[u]);
+    }
+    S = wave_sum(S);
+    if (lane == 0) sh_s[wave] = S;
+    __syncthreads();
+    __syncthreads();
+    const RowGrad q = sh_q;
+    const int32_t jy = y >= x.h && y < x.tail() ? (y - x.h) / VEC : -1, ky = (y - x.h) % VEC;
+    auto put = [&](const vec4u& p, int32_t at) {
+      float z[VEC];
+      Elem<Tin>::unpack(p, z);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) z[i] = grad_of(z[i], q);
+      if (t == jy - at) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) z[i] = i == ky ? q.gy : z[i];
+      }
+      store_grad(x.to(at, t), GradVec<Tin>::pack(z));
+      __builtin_amdgcn_sched_barrier(0);
+    };
+#pragma unroll
+    for (int u = 0; u < NL; ++u)
+      if (t < x.nvec - u * NT) put(held[u * NT + t], u * NT);
+#pragma unroll
+    for (int u = 0; u < NR; ++u) {
+      forget(v[u]);
+      if (t < x.nvec - (NL + u) * NT) put(v[u], (NL + u) * NT);
+    }
+  }
+  for (int64_t k = 0; k < turns_off; ++k) {
+    const int64_t r = row_of(rows_off, k);
+    if (!listed && a.rows.weight[r] != 0.0f) continue;
+    const RowView<Tin> x(a.rows, r);
+    for (int32_t at = 0; at < x.nvec; at += NT)
+      if (t < x.nvec - at) store_grad(x.to(at, t), vec4u{0, 0, 0, 0});
+  }
+}
+
+// Workgroups of the gradient pass along a row.
+template <typename Tin>
+int64_t grad_parts(int32_t V) {
+  constexpr int64_t kPart = kGradBlock * kGradPer;
+  const int64_t nvec = V / Elem<Tin>::kVec;
+  return nvec > 0 ? (nvec + kPart - 1) / kPart : 1;
+}
 
 template <typename Tin>
 hipError_t launch_grad(const LossRows& a, const RowGrad* rg, hipStream_t stream) {
-  const int64_t nvec = a.V / Elem<Tin>::kVec;
-  const int32_t segs = static_cast<int32_t>((nvec + kGradSegment - 1) / kGradSegment);
-  const int32_t s = segs < 1 ? 1 : segs;
-  // Lists of more than 2^31 workgroups take several launches.
-  const int64_t most = (int64_t{1} << 30) / s;
-  for (int64_t at = 0; at < a.n_rows; at += most) {
-    LossRows b = a;
-    b.n_rows = a.n_rows - at < most ? a.n_rows - at : most;
-    b.logits = static_cast<const Tin*>(a.logits) + at * a.row_stride;
-    b.grad = static_cast<Tin*>(a.grad) + at * a.grad_stride;
-    b.ids = a.ids + at;
-    hipLaunchKernelGGL(grad_kernel<Tin>, dim3(static_cast<unsigned>(b.n_rows * s)), dim3(kGradBlock), 0, stream, b,
-                       rg + at, s);
+  constexpr int64_t kMostY = 32768;
+  const int64_t parts = grad_parts<Tin>(a.V);
+  for (int64_t at = 0; at < a.n_rows; at += kMostY) {
+    const int64_t rows = a.n_rows - at < kMostY ? a.n_rows - at : kMostY;
+    hipLaunchKernelGGL((grad_kernel<Tin, false>), dim3(static_cast<unsigned>(parts), static_cast<unsigned>(rows)),
+                       dim3(kGradBlock), 0, stream, a, rg, at, nullptr, 0, nullptr);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -341,13 +602,14 @@ hipError_t launch_grad(const LossRows& a, const RowGrad* rg, hipStream_t stream)
 }
 
 // The preference loss of a row, first part: l and what its gradient needs.
-__device__ __forceinline__ void preference_row(const PreferenceArgs& a, int64_t r, const RowSum& p, float T, float c,
-                                               int32_t y, float zy, double* l, RowGrad* rg) {
+__device__ __forceinline__ double preference_row(const PreferenceArgs& a, int64_t r, const RowSum& p, float T, float c,
+                                                 int32_t y, float zy, double* l, RowGrad* rg) {
   const RowValue v = row_value(p, T, c, y, a.rows.V, zy);
   l[r] = v.l;
   rg[r] = RowGrad{v.A, c, p.S, T};
   if (a.out.logprob) a.out.logprob[r] = static_cast<float>(v.l);
   if (a.out.flags) a.out.flags[r] = v.flags;
+  return v.l;
 }
 
 template <typename Tin>
@@ -375,6 +637,22 @@ __global__ __launch_bounds__(kStatsBlock) void preference_stats_kernel(Preferenc
     preference_row(a, r, p, T, c, y, zy, l, rg);
 }
 
+// The state of a row that was split: its G partial sums, all of them read at once.
+constexpr int kMaxSplit = 16;
+
+__device__ __forceinline__ RowSum merge_parts(const RowSum* part, int G, float c) {
+  RowSum e[kMaxSplit];
+  RowSum s{-INFINITY, 0.0f};
+#pragma unroll
+  for (int g = 0; g < kMaxSplit; ++g) e[g] = g < G ? part[g] : RowSum{-INFINITY, 0.0f};
+#pragma unroll
+  for (int g = 0; g < kMaxSplit; ++g) s.m = fmaxf(s.m, e[g].m);
+#pragma unroll
+  for (int g = 0; g < kMaxSplit; ++g)
+    s.S += e[g].S * (e[g].m == -INFINITY ? 0.0f : fast_exp2(fmaxf(e[g].m * c - s.m * c, -kBig)));
+  return s;
+}
+
 // One workgroup per pair: the sums over both requests, the pair's loss, and
 // the gradient's factors of the pair's rows. Rows that were split finish here.
 constexpr int kPairBlock = 256;
@@ -392,25 +670,25 @@ __global__ __launch_bounds__(kPairBlock) void preference_pair_kernel(PreferenceA
     const int64_t o = a.offsets[2 * p + i];
     off[i] = o < 0 ? 0 : o > a.rows.n_rows ? a.rows.n_rows : o;
   }
+  // The pair's rows, chosen request first.
   double q[2] = {0.0, 0.0};
+  for (int64_t r = off[0] + threadIdx.x; r < off[2]; r += kPairBlock) {
+    const float w = a.rows.weight[r];
+    const float ref = a.ref_logprob ? a.ref_logprob[r] : 0.0f;
+    double lr;
+    if (a.G > 1) {
+      if (w == 0.0f) continue;
+      const int32_t y = a.rows.ids[r];
+      const float T = a.rows.temperature[r], c = scale_of(T), zy = token_logit<Tin>(a.rows, r, y);
+      const RowSum s = merge_parts(part + r * a.G, a.G, c);
+      lr = preference_row(a, r, s, T, c, y, zy, l, rg);
+    } else {
+      lr = l[r];
+    }
+    if (w != 0.0f) q[r < off[1] ? 0 : 1] += static_cast<double>(w) * (lr - static_cast<double>(ref));
+  }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    for (int64_t r = off[i] + threadIdx.x; r < off[i + 1]; r += kPairBlock) {
-      const float w = a.rows.weight[r];
-      if (w == 0.0f) continue;
-      if (a.G > 1) {
-        const float T = a.rows.temperature[r], c = scale_of(T);
-        RowSum s{-INFINITY, 0.0f};
-        for (int g = 0; g < a.G; ++g) s.m = fmaxf(s.m, part[r * a.G + g].m);
-        for (int g = 0; g < a.G; ++g) {
-          const RowSum e = part[r * a.G + g];
-          s.S += e.S * (e.m == -INFINITY ? 0.0f : fast_exp2(fmaxf(e.m * c - s.m * c, -kBig)));
-        }
-        const int32_t y = a.rows.ids[r];
-        preference_row(a, r, s, T, c, y, token_logit<Tin>(a.rows, r, y), l, rg);
-      }
-      q[i] += static_cast<double>(w) * (l[r] - (a.ref_logprob ? static_cast<double>(a.ref_logprob[r]) : 0.0));
-    }
     q[i] = wave_sum_d(q[i]);
     if (threadIdx.x % kWave == 0) sh[i][threadIdx.x / kWave] = q[i];
   }
@@ -424,6 +702,7 @@ __global__ __launch_bounds__(kPairBlock) void preference_pair_kernel(PreferenceA
   if (threadIdx.x == 0) {
     const double loss = (s < 1.0 ? (1.0 - s) * softplus(-h) : 0.0) + (s > 0.0 ? s * softplus(h) : 0.0);
     pair_loss[p] = loss;
+    if (a.n_pairs == 1) a.loss[0] = static_cast<float>(loss);
     if (a.out.pair_loss) a.out.pair_loss[p] = static_cast<float>(loss);
     if (a.out.pair_logit) a.out.pair_logit[p] = static_cast<float>(h);
     if (a.out.seq_logratio) {
@@ -435,15 +714,12 @@ __global__ __launch_bounds__(kPairBlock) void preference_pair_kernel(PreferenceA
   // sigmoid(h) - 1 + s, without the cancellation of sigmoid(h) - 1.
   const double dh = s / (1.0 + exp(-h)) - (1.0 - s) / (1.0 + exp(h));
   const double dq = a.grad_scale * a.beta * dh / static_cast<double>(a.n_pairs);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    for (int64_t r = off[i] + threadIdx.x; r < off[i + 1]; r += kPairBlock) {
-      const float w = a.rows.weight[r];
-      if (w == 0.0f) continue;
-      const RowGrad e = rg[r];
-      const double coef = (i == 0 ? dq : -dq) * static_cast<double>(w) / static_cast<double>(e.gy);
-      rg[r] = row_grad(coef, l[r], e.A, e.c, e.k);
-    }
+  for (int64_t r = off[0] + threadIdx.x; r < off[2]; r += kPairBlock) {
+    const float w = a.rows.weight[r];
+    if (w == 0.0f) continue;
+    const RowGrad e = rg[r];
+    const double coef = (r < off[1] ? dq : -dq) * static_cast<double>(w) / static_cast<double>(e.gy);
+    rg[r] = row_grad(coef, l[r], e.A, e.c, e.k);
   }
 }
 
@@ -453,14 +729,24 @@ template <typename Tin>
 hipError_t policy(const PolicyArgs& a, hipStream_t stream) {
   RowGrad* rg = reinterpret_cast<RowGrad*>(reinterpret_cast<char*>(a.row_loss) +
                                            up16(static_cast<size_t>(a.rows.n_rows) * sizeof(double)));
-  if (a.rows.n_rows > 0) {
-    hipLaunchKernelGGL(policy_stats_kernel<Tin>, dim3(static_cast<unsigned>(a.rows.n_rows)), dim3(kStatsBlock), 0,
-                       stream, a, rg);
-    hipError_t e = hipGetLastError();
+  const int64_t n = a.rows.n_rows, nvec = a.rows.V / Elem<Tin>::kVec;
+  hipError_t e = hipSuccess;
+  if (n > 0 && a.rows.grad && nvec <= kRowVectors) {
+    const bool small = nvec <= kSmallRowVectors;
+    const int64_t most = small ? 2 * kCUs : kCUs;
+    const dim3 grid(static_cast<unsigned>(n < most ? n : most));
+    if (small)
+      hipLaunchKernelGGL((policy_row_kernel<Tin, 7, 11, 8>), grid, dim3(512), 0, stream, a);
+    else
+      hipLaunchKernelGGL((policy_row_kernel<Tin, 15, 12, 8>), grid, dim3(1024), 0, stream, a);
+    e = hipGetLastError();
+  } else if (n > 0) {
+    hipLaunchKernelGGL(policy_stats_kernel<Tin>, dim3(static_cast<unsigned>(n)), dim3(kStatsBlock), 0, stream, a, rg);
+    e = hipGetLastError();
     if (e == hipSuccess && a.rows.grad) e = launch_grad<Tin>(a.rows, rg, stream);
-    if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(kSumBlock), 0, stream, a.row_loss, a.rows.n_rows, 1.0, a.loss);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(kSumBlock), 0, stream, a.row_loss, n, 1.0, a.loss);
   return hipGetLastError();
 }
 
@@ -483,10 +769,20 @@ hipError_t preference(const PreferenceArgs& a, hipStream_t stream) {
                        stream, a, l, rg, part, pair_loss);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && n > 0 && a.rows.grad) e = launch_grad<Tin>(a.rows, rg, stream);
-  if (e != hipSuccess) return e;
+  // The mean over pairs: a single pair's own kernel writes it, that of a small
+  // batch goes beside its gradient.
+  const int64_t parts = grad_parts<Tin>(a.rows.V);
+  if (e == hipSuccess && n > 0 && a.rows.grad) {
+    if (a.n_pairs > 1 && a.rows.n_rows * parts <= 2048 && a.n_pairs <= 4 * kGradBlock) {
+      hipLaunchKernelGGL((grad_kernel<Tin, true>), dim3(static_cast<unsigned>(parts), static_cast<unsigned>(n)),
+                         dim3(kGradBlock), 0, stream, a.rows, rg, int64_t{0}, pair_loss, a.n_pairs, a.loss);
+      return hipGetLastError();
+    }
+    e = launch_grad<Tin>(a.rows, rg, stream);
+  }
+  if (e != hipSuccess || a.n_pairs == 1) return e;
   hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(kSumBlock), 0, stream, pair_loss,
-                     static_cast<int64_t>(a.n_pairs), 1.0 / a.n_pairs, a.loss);
+                     static_cast<int64_t>(a.n_pairs), static_cast<double>(a.n_pairs), a.loss);
   return hipGetLastError();
 }
 
@@ -507,7 +803,7 @@ int preference_split(int64_t n_rows, int32_t V, pr_dtype dtype) {
   if (n_rows <= 0 || n_rows >= 1024) return 1;
   const int64_t want = (2048 + n_rows - 1) / n_rows, most = nvec / 1024;
   const int64_t G = want < most ? want : most;
-  return static_cast<int>(G < 1 ? 1 : G > 64 ? 64 : G);
+  return static_cast<int>(G < 1 ? 1 : G > kMaxSplit ? kMaxSplit : G);
 }
 
 size_t preference_workspace_bytes(int64_t n_rows, int32_t n_pairs, int32_t G) {
