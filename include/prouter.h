@@ -595,7 +595,9 @@ typedef struct pr_adamw pr_adamw;
 #define PR_ADAMW_BLOCK 256
 
 /*
- * An AdamW step over many tensors at once, in one launch per 448 tensors. For each element, with g = grad_scale grad:
+ * An AdamW step over many tensors at once, in one launch (one per 400 tensors
+ * when a step is given its gradients). For each element, with
+ * g = grad_scale grad:
  *   m' = beta1 m + (1 - beta1) g,  v' = beta2 v + (1 - beta2) g g
  *   p' = p (1 - lr weight_decay) - lr c1 m' / (c2 sqrt(v') + eps),
  *   c1 = 1 / (1 - beta1^step),  c2 = 1 / sqrt(1 - beta2^step)

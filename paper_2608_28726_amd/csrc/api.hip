@@ -36,7 +36,7 @@ struct pr_adamw {
   std::vector<int64_t> chunk_begin;  // [n_tensors + 1] first chunk of each tensor
   bool has_grads;                    // every tensor of the plan has a gradient of its own
   uint64_t seed;                     // of the stochastic rounding
-  void* block;                       // single allocation backing the plan's arrays
+  void* block;                       // single allocation backing the plan
 };
 
 namespace {
@@ -646,13 +646,14 @@ pr_status pr_adamw_create(const pr_adamw_tensor* tensors, int32_t n_tensors, pr_
   if (!handle) return PR_ERR_INVALID_ARG;
   *handle = nullptr;
   if (n_tensors < 0 || (n_tensors > 0 && !tensors)) return PR_ERR_INVALID_ARG;
+  if (n_tensors > (1 << 20)) return PR_ERR_UNSUPPORTED;
   if ((param_dtype != PR_F32 && param_dtype != PR_BF16) || (grad_dtype != PR_F32 && grad_dtype != PR_BF16) ||
       (state_bits != 8 && state_bits != 32))
     return PR_ERR_INVALID_ARG;
   const size_t state = state_bits == 8 ? 1 : 4;
   for (int32_t j = 0; j < n_tensors; ++j) {
     const pr_adamw_tensor& t = tensors[j];
-    if (t.n < 0 || t.n > (int64_t{1} << 42)) return PR_ERR_INVALID_ARG;
+    if (t.n < 0 || t.n > (int64_t{1} << 38)) return PR_ERR_INVALID_ARG;  // more than a device holds
     if (t.n == 0) continue;
     if (!t.param || !t.m || !t.v || !aligned(t.param, dtype_size(param_dtype)) || !aligned(t.m, state) ||
         !aligned(t.v, state) || (t.grad && !aligned(t.grad, dtype_size(grad_dtype))))
@@ -664,33 +665,43 @@ pr_status pr_adamw_create(const pr_adamw_tensor* tensors, int32_t n_tensors, pr_
     pr_adamw* h = new pr_adamw();
     h->block = nullptr;
     h->has_grads = true;
-    std::vector<AdamTensor> plan(static_cast<size_t>(n_tensors));
     std::vector<AdamChunk> chunks;
     hipError_t e = hipSuccess;
+    int64_t elements = 0;
+    const int64_t element_bytes = static_cast<int64_t>(dtype_size(param_dtype) + dtype_size(grad_dtype) + 2 * state);
     try {
       h->chunk_begin.resize(static_cast<size_t>(n_tensors) + 1);
       int64_t block = 0, total = 0;
-      for (int32_t j = 0; j < n_tensors; ++j) total += (tensors[j].n + kAdamChunk - 1) / kAdamChunk;
+      for (int32_t j = 0; j < n_tensors; ++j) {
+        total += (tensors[j].n + kAdamChunk - 1) / kAdamChunk;
+        elements += tensors[j].n;
+      }
       chunks.reserve(static_cast<size_t>(total));
+      const int64_t p_item = static_cast<int64_t>(dtype_size(param_dtype)), s_item = static_cast<int64_t>(state);
+      const int64_t g_item = static_cast<int64_t>(dtype_size(grad_dtype));
+      auto past = [](auto* p, int64_t bytes) -> decltype(p) {
+        return p ? (decltype(p))((const char*)p + bytes) : nullptr;
+      };
       for (int32_t j = 0; j < n_tensors; ++j) {
         const pr_adamw_tensor& t = tensors[j];
         h->chunk_begin[static_cast<size_t>(j)] = static_cast<int64_t>(chunks.size());
-        plan[static_cast<size_t>(j)] = AdamTensor{t.param, t.grad, static_cast<uint16_t*>(t.copy), t.m, t.v,
-                                                  t.m_exp, t.v_exp, t.n, block};
         if (t.n > 0 && !t.grad) h->has_grads = false;
+        for (int64_t at = 0; at < t.n; at += kAdamChunk) {
+          const int64_t n = t.n - at < kAdamChunk ? t.n - at : kAdamChunk, k = at / kAdamBlock;
+          chunks.push_back(AdamChunk{past(t.param, at * p_item), past(t.grad, at * g_item),
+                                     past(static_cast<uint16_t*>(t.copy), at * 2), past(t.m, at * s_item),
+                                     past(t.v, at * s_item), past(t.m_exp, k), past(t.v_exp, k), at, block + k,
+                                     static_cast<int32_t>(n), j});
+        }
         block += (t.n + kAdamBlock - 1) / kAdamBlock;
-        for (int32_t k = 0; static_cast<int64_t>(k) * kAdamChunk < t.n; ++k) chunks.push_back(AdamChunk{j, k});
       }
       h->chunk_begin[static_cast<size_t>(n_tensors)] = static_cast<int64_t>(chunks.size());
-      const size_t b_plan = plan.size() * sizeof(AdamTensor), b_chunks = chunks.size() * sizeof(AdamChunk);
+      const size_t bytes = chunks.size() * sizeof(AdamChunk);
       e = hipGetDevice(&h->device);
-      if (e == hipSuccess && b_plan > 0) {
-        e = hipMalloc(&h->block, b_plan + b_chunks);
-        char* b = static_cast<char*>(h->block);
-        if (e == hipSuccess) e = hipMemcpy(b, plan.data(), b_plan, hipMemcpyHostToDevice);
-        if (e == hipSuccess && b_chunks > 0) e = hipMemcpy(b + b_plan, chunks.data(), b_chunks, hipMemcpyHostToDevice);
-        h->plan.tensors = reinterpret_cast<const AdamTensor*>(b);
-        h->plan.chunks = reinterpret_cast<const AdamChunk*>(b + b_plan);
+      if (e == hipSuccess && bytes > 0) {
+        e = hipMalloc(&h->block, bytes);
+        if (e == hipSuccess) e = hipMemcpy(h->block, chunks.data(), bytes, hipMemcpyHostToDevice);
+        h->plan.chunks = static_cast<const AdamChunk*>(h->block);
       }
     } catch (...) {
       delete h;
@@ -704,6 +715,7 @@ pr_status pr_adamw_create(const pr_adamw_tensor* tensors, int32_t n_tensors, pr_
     h->plan.param_dtype = param_dtype;
     h->plan.grad_dtype = grad_dtype;
     h->plan.state_bits = state_bits;
+    h->plan.streamed = elements * element_bytes > kAdamCached;
     h->seed = seed;
     *handle = h;
     return PR_OK;
@@ -730,20 +742,22 @@ pr_status pr_adamw_step(pr_adamw* handle, const void* const* grads, const pr_ada
   s.c2 = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(p.beta2, static_cast<double>(p.step))));
   s.eps = static_cast<float>(p.eps);
   s.grad_scale = static_cast<float>(p.grad_scale);
+  s.tiny_eps = p.eps < 1e-12;
   s.key = step_key(handle->seed, p.step);
   const int32_t n = static_cast<int32_t>(handle->chunk_begin.size()) - 1;
   if (!grads)
-    return hip_status(launch_adamw(handle->plan, 0, handle->chunk_begin[static_cast<size_t>(n)], s, nullptr, 0,
-                                   as_stream(stream)));
+    return hip_status(
+        launch_adamw(handle->plan, 0, handle->chunk_begin[static_cast<size_t>(n)], s, nullptr, as_stream(stream)));
   const size_t item = dtype_size(handle->plan.grad_dtype);
   for (int32_t j = 0; j < n; ++j)
     if (grads[j] && !aligned(grads[j], item)) return PR_ERR_INVALID_ARG;
   for (int32_t j = 0; j < n; j += kAdamGrads) {
     const int32_t to = n - j < kAdamGrads ? n : j + kAdamGrads;
     AdamGrads g{};
+    g.first = j;
     for (int32_t i = j; i < to; ++i) g.p[i - j] = grads[i];
     const hipError_t e = launch_adamw(handle->plan, handle->chunk_begin[static_cast<size_t>(j)],
-                                      handle->chunk_begin[static_cast<size_t>(to)], s, &g, j, as_stream(stream));
+                                      handle->chunk_begin[static_cast<size_t>(to)], s, &g, as_stream(stream));
     if (e != hipSuccess) return hip_status(e);
   }
   return PR_OK;
