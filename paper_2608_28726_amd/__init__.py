@@ -466,8 +466,8 @@ class StreamState:
 
 def _check_current(device, what: str) -> int:
     """Launches go to the current device's stream: the tensors have to be there. Returns that stream."""
-    current = torch.cuda.current_device()
-    if device.type != "cuda" or device.index != current:
+    current = torch.cuda.current_device() if device.type == "cuda" else None
+    if current is None or device.index != current:
         raise ValueError(f"{what} must be on the current CUDA device, got {device}")
     return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(current)
 
