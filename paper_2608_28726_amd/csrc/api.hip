@@ -565,7 +565,9 @@ void pr_policy_params_default(pr_policy_params* params) {
   if (params) *params = pr_policy_params{0.2, 0.2, 0.0, 1.0};
 }
 
-size_t pr_policy_loss_workspace(pr_dtype, int64_t n_rows, int32_t) { return policy_workspace_bytes(n_rows); }
+size_t pr_policy_loss_workspace(pr_dtype dtype, int64_t n_rows, int32_t vocab) {
+  return vocab < 2 ? 0 : policy_workspace_bytes(n_rows, vocab, dtype);
+}
 
 pr_status pr_policy_loss(const void* logits, pr_dtype dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,
                          const int32_t* ids, const float* temperature, const float* weight, const float* advantage,
@@ -582,7 +584,7 @@ pr_status pr_policy_loss(const void* logits, pr_dtype dtype, int64_t n_rows, int
   if (!(p.clip_low >= 0.0 && p.clip_low <= 1.0) || !(p.clip_high >= 0.0) || !(p.kl_coef >= 0.0) ||
       !std::isfinite(p.kl_coef) || !std::isfinite(p.grad_scale) || (p.kl_coef > 0.0 && !ref_logprob && n_rows > 0))
     return PR_ERR_INVALID_ARG;
-  const size_t need = policy_workspace_bytes(n_rows);
+  const size_t need = pr_policy_loss_workspace(dtype, n_rows, vocab);
   if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return PR_ERR_INVALID_ARG;
   PolicyArgs a{};
   a.rows = loss_rows(logits, n_rows, vocab, row_stride, ids, temperature, weight, grad, grad_stride);
@@ -595,6 +597,7 @@ pr_status pr_policy_loss(const void* logits, pr_dtype dtype, int64_t n_rows, int
   a.grad_scale = p.grad_scale;
   a.loss = loss;
   if (out) a.out = *out;
+  a.G = policy_split(n_rows, vocab, dtype, grad != nullptr);
   a.row_loss = static_cast<double*>(workspace);
   return hip_status(launch_policy(a, dtype, as_stream(stream)));
 }
@@ -604,6 +607,7 @@ void pr_preference_params_default(pr_preference_params* params) {
 }
 
 size_t pr_preference_loss_workspace(pr_dtype dtype, int64_t n_rows, int32_t vocab, int32_t n_pairs) {
+  if (vocab < 2) return 0;
   return preference_workspace_bytes(n_rows, n_pairs, preference_split(n_rows, vocab, dtype));
 }
 

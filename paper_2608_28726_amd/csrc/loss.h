@@ -28,7 +28,8 @@ struct PolicyArgs {
   double grad_scale;
   float* loss;
   pr_policy_tokens_t out;
-  double* row_loss;  // workspace [n_rows]
+  int32_t G;         // workgroups per row of the parts (0: rows are not split)
+  double* row_loss;  // the workspace, which starts with the rows' terms of the loss where they are not split
 };
 
 struct PreferenceArgs {
@@ -43,7 +44,10 @@ struct PreferenceArgs {
   void* ws;
 };
 
-size_t policy_workspace_bytes(int64_t n_rows);
+// Workgroups per row for a shape (0: rows are not split), with or without the
+// gradient, and the workspace that either takes.
+int policy_split(int64_t n_rows, int32_t V, pr_dtype dtype, bool grad);
+size_t policy_workspace_bytes(int64_t n_rows, int32_t V, pr_dtype dtype);
 hipError_t launch_policy(const PolicyArgs& a, pr_dtype dtype, hipStream_t stream);
 
 // Workgroups per row for a shape, and the workspace it takes.

@@ -121,7 +121,7 @@ __device__ __forceinline__ RowValue row_value(const RowSum& p, float T, float c,
 // The gradient's factors of a row from coef = dloss/dl / T. 1 - p_y is
 // -expm1(l), which keeps its precision when p_y is near 1.
 __device__ __forceinline__ RowGrad row_grad(double coef, double l, float A, float c, float S) {
-  if (coef == 0.0) return RowGrad{0.0f, 0.0f, 0.0f, 0.0f};
+  if (coef == 0.0) return RowGrad{A, c, 0.0f, 0.0f};
   if (!(coef == coef)) {
     const float nan = __uint_as_float(0x7fc00000u);
     return RowGrad{0.0f, 0.0f, nan, nan};
@@ -139,9 +139,16 @@ __device__ __forceinline__ float token_logit(const LossRows& a, int64_t r, int32
   return y >= 0 && y < a.V ? Elem<Tin>::load1(row_ptr<Tin>(a, r), y) : 0.0f;
 }
 
-// The policy loss of one row: outputs, its term of the loss and its gradient's factors.
-__device__ __forceinline__ RowGrad policy_row(const PolicyArgs& a, int64_t r, const RowValue& v, float T, float c,
-                                              float S, float w) {
+// What the policy loss makes of a row.
+struct PolicyRow {
+  double term;  // of the loss
+  float logprob, ratio, kl;
+  uint32_t flags;
+  RowGrad grad;
+};
+
+__device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, int64_t r, const RowValue& v, float T, float c,
+                                                float S, float w) {
   const double A = a.advantage[r], ratio = expf(static_cast<float>(v.l - static_cast<double>(a.old_logprob[r])));
   const double free = ratio * A, held = fmin(fmax(ratio, a.clip_lo), a.clip_hi) * A;
   const bool clipped = free > held;
@@ -152,28 +159,32 @@ __device__ __forceinline__ RowGrad policy_row(const PolicyArgs& a, int64_t r, co
     kl = d == INFINITY ? d : rise - d;  // a token of probability 0
   }
   const double gain = v.flags ? v.l : (clipped ? held : free);
-  a.row_loss[r] = static_cast<double>(w) * ((a.ref_logprob ? a.kl_coef * kl : 0.0) - gain);
-  if (a.out.logprob) a.out.logprob[r] = static_cast<float>(v.l);
-  if (a.out.ratio) a.out.ratio[r] = static_cast<float>(ratio);
-  if (a.out.kl) a.out.kl[r] = static_cast<float>(kl);
-  if (a.out.flags) a.out.flags[r] = v.flags | (!v.flags && clipped ? PR_FLAG_CLIPPED : 0u);
   const double dl = static_cast<double>(w) * ((clipped ? 0.0 : -free) - (a.ref_logprob ? a.kl_coef * rise : 0.0));
-  return row_grad(v.flags ? v.l : a.grad_scale * dl / static_cast<double>(T), v.l, v.A, c, S);
+  PolicyRow p;
+  p.term = static_cast<double>(w) * ((a.ref_logprob ? a.kl_coef * kl : 0.0) - gain);
+  p.logprob = static_cast<float>(v.l);
+  p.ratio = static_cast<float>(ratio);
+  p.kl = static_cast<float>(kl);
+  p.flags = v.flags | (!v.flags && clipped ? PR_FLAG_CLIPPED : 0u);
+  p.grad = row_grad(v.flags ? v.l : a.grad_scale * dl / static_cast<double>(T), v.l, v.A, c, S);
+  return p;
 }
 
-__device__ __forceinline__ void policy_masked(const PolicyArgs& a, int64_t r) {
-  a.row_loss[r] = 0.0;
-  if (a.out.logprob) a.out.logprob[r] = 0.0f;
-  if (a.out.ratio) a.out.ratio[r] = 0.0f;
-  if (a.out.kl) a.out.kl[r] = 0.0f;
-  if (a.out.flags) a.out.flags[r] = PR_FLAG_MASKED;
+__device__ __forceinline__ PolicyRow policy_masked() {
+  return PolicyRow{0.0, 0.0f, 0.0f, 0.0f, PR_FLAG_MASKED, RowGrad{0.0f, 0.0f, 0.0f, 0.0f}};
 }
 
-// Sum of v[0..n) by one workgroup, in a fixed order (valid in thread 0).
-__device__ __forceinline__ double block_sum(const double* v, int64_t n) {
+__device__ __forceinline__ void policy_write(const PolicyArgs& a, int64_t r, const PolicyRow& p) {
+  if (a.out.logprob) a.out.logprob[r] = p.logprob;
+  if (a.out.ratio) a.out.ratio[r] = p.ratio;
+  if (a.out.kl) a.out.kl[r] = p.kl;
+  if (a.out.flags) a.out.flags[r] = p.flags;
+}
+
+// Sums by one workgroup, in a fixed order (valid in thread 0): of its
+// threads' values, and of v[0..n).
+__device__ __forceinline__ double block_total(double s) {
   __shared__ double sh[kSumBlock / kWave];
-  double s = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += blockDim.x) s += v[i];
   s = wave_sum_d(s);
   if (threadIdx.x % kWave == 0) sh[threadIdx.x / kWave] = s;
   __syncthreads();
@@ -181,6 +192,11 @@ __device__ __forceinline__ double block_sum(const double* v, int64_t n) {
   if (threadIdx.x == 0)
     for (int w = 0; w < static_cast<int>(blockDim.x) / kWave; ++w) t += sh[w];
   return t;
+}
+__device__ __forceinline__ double block_sum(const double* v, int64_t n) {
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < n; i += blockDim.x) s += v[i];
+  return block_total(s);
 }
 
 // loss = (sum of v) / over
@@ -214,25 +230,50 @@ __device__ RowSum stretch_sum(const Tin* row, int32_t V, int g, int G, float c) 
   return merge_block<BLOCK>(L, c);
 }
 
+// The sums of the rows' stretches, G of them a row.
+template <typename Tin>
+__global__ __launch_bounds__(kStatsBlock) void parts_kernel(LossRows a, RowSum* part, int32_t G) {
+  const int64_t r = blockIdx.x / G;
+  const int g = blockIdx.x % G;
+  if (a.weight[r] == 0.0f) return;
+  const RowSum p = stretch_sum<Tin, kStatsBlock>(row_ptr<Tin>(a, r), a.V, g, G, scale_of(a.temperature[r]));
+  if (threadIdx.x == 0) part[r * G + g] = p;
+}
+
+// The state of a row from its G parts, all of them read at once.
+constexpr int kMaxSplit = 16;
+
+__device__ __forceinline__ RowSum merge_parts(const RowSum* part, int G, float c) {
+  RowSum e[kMaxSplit];
+  RowSum s{-INFINITY, 0.0f};
+#pragma unroll
+  for (int g = 0; g < kMaxSplit; ++g) e[g] = g < G ? part[g] : RowSum{-INFINITY, 0.0f};
+#pragma unroll
+  for (int g = 0; g < kMaxSplit; ++g) s.m = fmaxf(s.m, e[g].m);
+#pragma unroll
+  for (int g = 0; g < kMaxSplit; ++g)
+    s.S += e[g].S * (e[g].m == -INFINITY ? 0.0f : fast_exp2(fmaxf(e[g].m * c - s.m * c, -kBig)));
+  return s;
+}
+
 template <typename Tin>
 __global__ __launch_bounds__(kStatsBlock) void policy_stats_kernel(PolicyArgs a, RowGrad* rg) {
   const int64_t r = blockIdx.x;
   const float w = a.rows.weight[r];
-  if (w == 0.0f) {
-    if (threadIdx.x == 0) {
-      policy_masked(a, r);
-      rg[r] = RowGrad{0.0f, 0.0f, 0.0f, 0.0f};
-    }
+  PolicyRow p = policy_masked();
+  if (w != 0.0f) {
+    const float T = a.rows.temperature[r], c = scale_of(T);
+    const int32_t y = a.rows.ids[r];
+    const float zy = token_logit<Tin>(a.rows, r, y);
+    const RowSum s = stretch_sum<Tin, kStatsBlock>(row_ptr<Tin>(a.rows, r), a.rows.V, 0, 1, c);
+    if (threadIdx.x != 0) return;
+    p = policy_row(a, r, row_value(s, T, c, y, a.rows.V, zy), T, c, s.S, w);
+  } else if (threadIdx.x != 0) {
     return;
   }
-  const float T = a.rows.temperature[r], c = scale_of(T);
-  const int32_t y = a.rows.ids[r];
-  const float zy = token_logit<Tin>(a.rows, r, y);
-  const RowSum p = stretch_sum<Tin, kStatsBlock>(row_ptr<Tin>(a.rows, r), a.rows.V, 0, 1, c);
-  if (threadIdx.x == 0) {
-    const RowValue v = row_value(p, T, c, y, a.rows.V, zy);
-    rg[r] = policy_row(a, r, v, T, c, p.S, w);
-  }
+  policy_write(a, r, p);
+  a.row_loss[r] = p.term;
+  rg[r] = p.grad;
 }
 
 // A bfloat16 or float32 vector of gradients. The gradient's rows may sit
@@ -280,63 +321,98 @@ __device__ __forceinline__ void stream_grad(Tin* at, const vec4u& v) {
 
 __device__ __forceinline__ float grad_of(float z, const RowGrad& q) { return q.k * fast_exp2(fmaf(z, q.c, -q.A)); }
 
-// Vectors per thread of a workgroup of the gradient pass.
-constexpr int kGradPer = 1;
-
-// The gradient of a stretch of a row (blockIdx.x) of the rows from `first` on
-// (blockIdx.y). Each element is read and written by one thread, so the
-// gradient may take the logits' place.
-//
-// SUM: the first workgroup also takes the loss that waits for the kernel
-// before this one, the mean of `sum`'s values. (Only small grids do that: it
-// saves a launch, but costs every workgroup about 10 %.)
-template <typename Tin, bool SUM>
-__global__ __launch_bounds__(kGradBlock) void grad_kernel(LossRows a, const RowGrad* rg, int64_t first,
-                                                          const double* sum, int32_t n_sum, float* loss) {
+// The gradient of a stretch of a row, a vector per thread of workgroup `part`:
+// short workgroups in memory order, past the caches, are what reads and
+// writes fastest at once here (6.5 TB/s; four vectors a thread 4.9). Each
+// element is read and written by one thread, so the gradient may take the
+// logits' place.
+template <typename Tin>
+__device__ __forceinline__ void grad_stretch(const LossRows& a, int64_t r, int32_t part, const RowGrad& q) {
   constexpr int VEC = Elem<Tin>::kVec;
-  if (SUM && blockIdx.x == 0 && blockIdx.y == 0) {
-    const double s = block_sum(sum, n_sum);
-    if (threadIdx.x == 0) loss[0] = static_cast<float>(s / n_sum);
-  }
-  const int64_t r = first + blockIdx.y;
-  const RowGrad q = rg[r];
   const Tin* row = row_ptr<Tin>(a, r);
   Tin* out = static_cast<Tin*>(a.grad) + r * a.grad_stride;
   const int32_t h = static_cast<int32_t>(head_elems<Tin>(row, a.V)), nvec = (a.V - h) / VEC, tail = h + nvec * VEC;
   const int t = threadIdx.x;
   const int32_t y = a.ids[r];
   const bool zero = q.k == 0.0f && q.gy == 0.0f;
-  if (blockIdx.x == 0 && t < 16) {
+  if (part == 0 && t < 16) {
     const int32_t e = t < 8 ? (t < h ? t : a.V) : tail + t - 8;  // the thread's scalar element
     if (e < a.V) GradVec<Tin>::store1(out, e, zero ? 0.0f : e == y ? q.gy : grad_of(Elem<Tin>::load1(row, e), q));
   }
-  const vec4u* vp = reinterpret_cast<const vec4u*>(row + h);
-  const int32_t j0 = blockIdx.x * (kGradBlock * kGradPer) + t;
-  vec4u v[kGradPer];
+  const int32_t j = part * kGradBlock + t;
+  if (j >= nvec) return;
+  vec4u g{0, 0, 0, 0};
   if (!zero) {
+    float z[VEC];
+    Elem<Tin>::unpack(__builtin_nontemporal_load(reinterpret_cast<const vec4u*>(row + h) + j), z);
 #pragma unroll
-    for (int u = 0; u < kGradPer; ++u)
-      if (j0 + u * kGradBlock < nvec) v[u] = __builtin_nontemporal_load(vp + j0 + u * kGradBlock);
-  }
+    for (int k = 0; k < VEC; ++k) z[k] = grad_of(z[k], q);
+    const int32_t at = y - (h + j * VEC);
+    if (at >= 0 && at < VEC) {
 #pragma unroll
-  for (int u = 0; u < kGradPer; ++u) {
-    const int32_t j = j0 + u * kGradBlock;
-    if (j >= nvec) return;
-    vec4u g{0, 0, 0, 0};
-    if (!zero) {
-      float z[VEC];
-      Elem<Tin>::unpack(v[u], z);
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) z[k] = grad_of(z[k], q);
-      const int32_t at = y - (h + j * VEC);
-      if (at >= 0 && at < VEC) {
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) z[k] = k == at ? q.gy : z[k];
-      }
-      g = GradVec<Tin>::pack(z);
+      for (int k = 0; k < VEC; ++k) z[k] = k == at ? q.gy : z[k];
     }
-    stream_grad(out + h + static_cast<int64_t>(j) * VEC, g);
+    g = GradVec<Tin>::pack(z);
   }
+  stream_grad(out + h + static_cast<int64_t>(j) * VEC, g);
+}
+
+// The gradients of the rows from `first` on (blockIdx.y).
+// SUM: the first workgroup also takes the loss that waits for the kernel
+// before this one, the mean of `sum`'s values. (Only small grids do that: it
+// saves a launch, but costs every workgroup about 10 %.)
+template <typename Tin, bool SUM>
+__global__ __launch_bounds__(kGradBlock) void grad_kernel(LossRows a, const RowGrad* rg, int64_t first,
+                                                          const double* sum, int32_t n_sum, float* loss) {
+  if (SUM && blockIdx.x == 0 && blockIdx.y == 0) {
+    const double s = block_sum(sum, n_sum);
+    if (threadIdx.x == 0) loss[0] = static_cast<float>(s / n_sum);
+  }
+  const int64_t r = first + blockIdx.y;
+  grad_stretch<Tin>(a, r, blockIdx.x, rg[r]);
+}
+
+// A split row's policy loss from its parts.
+template <typename Tin>
+__device__ __forceinline__ PolicyRow policy_from_parts(const PolicyArgs& a, int64_t r, const RowSum* part) {
+  const float w = a.rows.weight[r];
+  if (w == 0.0f) return policy_masked();
+  const float T = a.rows.temperature[r], c = scale_of(T);
+  const int32_t y = a.rows.ids[r];
+  const float zy = token_logit<Tin>(a.rows, r, y);
+  const RowSum s = merge_parts(part + r * a.G, a.G, c);
+  return policy_row(a, r, row_value(s, T, c, y, a.rows.V, zy), T, c, s.S, w);
+}
+
+// All split rows' outputs, gradient factors (rg NULL: not wanted) and the
+// loss, by one workgroup.
+template <typename Tin>
+__device__ __forceinline__ void policy_finish(const PolicyArgs& a, const RowSum* part, RowGrad* rg) {
+  double sum = 0.0;
+  for (int64_t r = threadIdx.x; r < a.rows.n_rows; r += kGradBlock) {
+    const PolicyRow p = policy_from_parts<Tin>(a, r, part);
+    policy_write(a, r, p);
+    if (rg) rg[r] = p.grad;
+    sum += p.term;
+  }
+  sum = block_total(sum);
+  if (threadIdx.x == 0) a.loss[0] = static_cast<float>(sum);
+}
+
+template <typename Tin>
+__global__ __launch_bounds__(kGradBlock) void policy_finish_kernel(PolicyArgs a, const RowSum* part, RowGrad* rg) {
+  policy_finish<Tin>(a, part, rg);
+}
+
+// The gradients of a few split rows: each workgroup works out its own row's
+// factors instead of waiting for a kernel that does. The first workgroup of
+// the grid's last row finishes the rows.
+template <typename Tin>
+__global__ __launch_bounds__(kGradBlock) void policy_parts_kernel(PolicyArgs a, const RowSum* part) {
+  if (blockIdx.y + 1 < gridDim.y)
+    grad_stretch<Tin>(a.rows, blockIdx.y, blockIdx.x, policy_from_parts<Tin>(a, blockIdx.y, part).grad);
+  else if (blockIdx.x == 0)
+    policy_finish<Tin>(a, part, nullptr);
 }
 
 // Makes the compiler forget what it knows of a vector, so that it unpacks it
@@ -468,9 +544,14 @@ __global__ __launch_bounds__((DW + 1) * kWave) void policy_row_kernel(PolicyArgs
       const float own = wave_sum(fast_exp2(fmaf(z, c, -A)));
       __syncthreads();
       const float S = wave_sum(lane < DW ? sh_s[lane] : lane == DW ? own : 0.0f);
-      const RowGrad q = policy_row(a, r, row_value(RowSum{m, S}, T, c, y, V, zy), T, c, S, w);
+      const PolicyRow p = policy_row(a, r, row_value(RowSum{m, S}, T, c, y, V, zy), T, c, S, w);
+      const RowGrad q = p.grad;
       if (lane == 0) sh_q = q;
       __syncthreads();
+      if (lane == 0) {
+        policy_write(a, r, p);
+        a.row_loss[r] = p.term;
+      }
       if (e < V) GradVec<Tin>::store1(x.out, e, e == y ? q.gy : grad_of(z, q));
     }
     for (int64_t k = 0; k < turns_off; ++k) {
@@ -478,7 +559,10 @@ __global__ __launch_bounds__((DW + 1) * kWave) void policy_row_kernel(PolicyArgs
       if (a.rows.weight[r] != 0.0f) continue;
       const RowView<Tin> x(a.rows, r);
       const int32_t e = lane < 8 ? (lane < x.h ? lane : V) : x.tail() + lane - 8;
-      if (lane == 0) policy_masked(a, r);
+      if (lane == 0) {
+        policy_write(a, r, policy_masked());
+        a.row_loss[r] = 0.0;
+      }
       if (e < V) GradVec<Tin>::store1(x.out, e, 0.0f);
     }
     return;
@@ -582,9 +666,8 @@ __global__ __launch_bounds__((DW + 1) * kWave) void policy_row_kernel(PolicyArgs
 // Workgroups of the gradient pass along a row.
 template <typename Tin>
 int64_t grad_parts(int32_t V) {
-  constexpr int64_t kPart = kGradBlock * kGradPer;
   const int64_t nvec = V / Elem<Tin>::kVec;
-  return nvec > 0 ? (nvec + kPart - 1) / kPart : 1;
+  return nvec > 0 ? (nvec + kGradBlock - 1) / kGradBlock : 1;
 }
 
 template <typename Tin>
@@ -635,22 +718,6 @@ __global__ __launch_bounds__(kStatsBlock) void preference_stats_kernel(Preferenc
     part[r * a.G + g] = p;
   else
     preference_row(a, r, p, T, c, y, zy, l, rg);
-}
-
-// The state of a row that was split: its G partial sums, all of them read at once.
-constexpr int kMaxSplit = 16;
-
-__device__ __forceinline__ RowSum merge_parts(const RowSum* part, int G, float c) {
-  RowSum e[kMaxSplit];
-  RowSum s{-INFINITY, 0.0f};
-#pragma unroll
-  for (int g = 0; g < kMaxSplit; ++g) e[g] = g < G ? part[g] : RowSum{-INFINITY, 0.0f};
-#pragma unroll
-  for (int g = 0; g < kMaxSplit; ++g) s.m = fmaxf(s.m, e[g].m);
-#pragma unroll
-  for (int g = 0; g < kMaxSplit; ++g)
-    s.S += e[g].S * (e[g].m == -INFINITY ? 0.0f : fast_exp2(fmaxf(e[g].m * c - s.m * c, -kBig)));
-  return s;
 }
 
 // One workgroup per pair: the sums over both requests, the pair's loss, and
@@ -723,14 +790,54 @@ __global__ __launch_bounds__(kPairBlock) void preference_pair_kernel(PreferenceA
   }
 }
 
+// Below this many rows a row may be spread over workgroups.
+constexpr int64_t kSplitRows = 1024;
+
+// Workgroups along a row for its sums: about 2,048 in all, each with at least
+// 1,024 vectors.
+int row_parts(int64_t n_rows, int32_t V, pr_dtype dtype) {
+  if (n_rows <= 0 || n_rows >= kSplitRows) return 1;
+  const int64_t nvec = V / (dtype == PR_BF16 ? 8 : 4);
+  const int64_t want = (2048 + n_rows - 1) / n_rows, most = nvec / 1024;
+  const int64_t G = want < most ? want : most;
+  return static_cast<int>(G < 1 ? 1 : G > kMaxSplit ? kMaxSplit : G);
+}
+
+// Few rows whose gradient is wanted are spread over the device although they
+// fit a workgroup: one compute unit alone takes 20 us for 304 KB. Captured
+// calls, spread and not: 16 rows of 151,936 bfloat16 logits 12.2 and 22.5 us,
+// 64 rows 19.9 and 25.1, 96 rows 26.7 and 25.8; 16 rows of 32,000 float32
+// logits 9.5 and 10.1, 32 rows 11.9 and 10.3.
+constexpr int64_t kFewRows = 64, kFewSmallRows = 32;
+
+// Most workgroups that each work out their own row's factors: it saves a
+// launch, 1 to 2 us, and costs more than that past this many.
+constexpr int64_t kFewGroups = 512;
+
 size_t up16(size_t b) { return (b + 15) & ~size_t{15}; }
 
 template <typename Tin>
 hipError_t policy(const PolicyArgs& a, hipStream_t stream) {
-  RowGrad* rg = reinterpret_cast<RowGrad*>(reinterpret_cast<char*>(a.row_loss) +
-                                           up16(static_cast<size_t>(a.rows.n_rows) * sizeof(double)));
   const int64_t n = a.rows.n_rows, nvec = a.rows.V / Elem<Tin>::kVec;
   hipError_t e = hipSuccess;
+  if (a.G > 0) {
+    RowGrad* rg = reinterpret_cast<RowGrad*>(a.row_loss);
+    RowSum* part = reinterpret_cast<RowSum*>(rg + n);
+    hipLaunchKernelGGL(parts_kernel<Tin>, dim3(static_cast<unsigned>(n * a.G)), dim3(kStatsBlock), 0, stream, a.rows,
+                       part, a.G);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t parts = grad_parts<Tin>(a.rows.V);
+    if (a.rows.grad && n * parts <= kFewGroups) {
+      hipLaunchKernelGGL(policy_parts_kernel<Tin>, dim3(static_cast<unsigned>(parts), static_cast<unsigned>(n + 1)),
+                         dim3(kGradBlock), 0, stream, a, part);
+      return hipGetLastError();
+    }
+    hipLaunchKernelGGL(policy_finish_kernel<Tin>, dim3(1), dim3(kGradBlock), 0, stream, a, part,
+                       a.rows.grad ? rg : nullptr);
+    e = hipGetLastError();
+    return e == hipSuccess && a.rows.grad ? launch_grad<Tin>(a.rows, rg, stream) : e;
+  }
   if (n > 0 && a.rows.grad && nvec <= kRowVectors) {
     const bool small = nvec <= kSmallRowVectors;
     const int64_t most = small ? 2 * kCUs : kCUs;
@@ -741,6 +848,8 @@ hipError_t policy(const PolicyArgs& a, hipStream_t stream) {
       hipLaunchKernelGGL((policy_row_kernel<Tin, 15, 12, 8>), grid, dim3(1024), 0, stream, a);
     e = hipGetLastError();
   } else if (n > 0) {
+    RowGrad* rg = reinterpret_cast<RowGrad*>(reinterpret_cast<char*>(a.row_loss) +
+                                             up16(static_cast<size_t>(n) * sizeof(double)));
     hipLaunchKernelGGL(policy_stats_kernel<Tin>, dim3(static_cast<unsigned>(n)), dim3(kStatsBlock), 0, stream, a, rg);
     e = hipGetLastError();
     if (e == hipSuccess && a.rows.grad) e = launch_grad<Tin>(a.rows, rg, stream);
@@ -788,23 +897,25 @@ hipError_t preference(const PreferenceArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-size_t policy_workspace_bytes(int64_t n_rows) {
+int policy_split(int64_t n_rows, int32_t V, pr_dtype dtype, bool grad) {
+  if (n_rows <= 0 || n_rows >= kSplitRows) return 0;
+  const int64_t nvec = V / (dtype == PR_BF16 ? 8 : 4);
+  const int64_t few = nvec <= kSmallRowVectors ? kFewSmallRows : kFewRows;
+  return grad && nvec <= kRowVectors && n_rows > few ? 0 : row_parts(n_rows, V, dtype);
+}
+
+size_t policy_workspace_bytes(int64_t n_rows, int32_t V, pr_dtype dtype) {
   const size_t n = n_rows < 0 ? 0 : static_cast<size_t>(n_rows);
-  return up16(n * sizeof(double)) + n * sizeof(RowGrad);
+  const size_t terms = up16(n * sizeof(double));
+  const size_t parts = n_rows < kSplitRows ? n * static_cast<size_t>(row_parts(n_rows, V, dtype)) * sizeof(RowSum) : 0;
+  return n * sizeof(RowGrad) + (terms > parts ? terms : parts);
 }
 
 hipError_t launch_policy(const PolicyArgs& a, pr_dtype dtype, hipStream_t stream) {
   return dtype == PR_BF16 ? policy<uint16_t>(a, stream) : policy<float>(a, stream);
 }
 
-int preference_split(int64_t n_rows, int32_t V, pr_dtype dtype) {
-  // Below 1,024 rows a row is spread over workgroups, at least 1,024 vectors each.
-  const int64_t nvec = V / (dtype == PR_BF16 ? 8 : 4);
-  if (n_rows <= 0 || n_rows >= 1024) return 1;
-  const int64_t want = (2048 + n_rows - 1) / n_rows, most = nvec / 1024;
-  const int64_t G = want < most ? want : most;
-  return static_cast<int>(G < 1 ? 1 : G > kMaxSplit ? kMaxSplit : G);
-}
+int preference_split(int64_t n_rows, int32_t V, pr_dtype dtype) { return row_parts(n_rows, V, dtype); }
 
 size_t preference_workspace_bytes(int64_t n_rows, int32_t n_pairs, int32_t G) {
   const size_t n = n_rows < 0 ? 0 : static_cast<size_t>(n_rows), P = n_pairs < 0 ? 0 : static_cast<size_t>(n_pairs);

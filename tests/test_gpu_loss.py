@@ -239,6 +239,33 @@ def test_policy_special_rows(V, dtype):
         assert math.isnan(float(got["loss"])) == (max(count) >= 8)
 
 
+@pytest.mark.parametrize("n", [3, 50, 700])
+@pytest.mark.parametrize("V", [1000, 70000])
+def test_policy_clipped_rows_with_forbidden_tokens(n, V):
+    """Rows whose gradient is 0 because the ratio is clipped, with logits of -inf among them: 0 everywhere, in each way
+    that rows are dealt out; rows beside them as the oracle has them."""
+    if n * V > 4_000_000:
+        n = 40
+    rng = np.random.default_rng(n)
+    z = rng.normal(0, 2, (n, V)).astype(np.float32)
+    z[:, V // 3:V // 2] = -np.inf
+    ids = rng.integers(0, V // 3, n).astype(np.int32)
+    u = z.astype(np.float64)
+    l = u[np.arange(n), ids] - np.logaddexp.reduce(u, axis=1)
+    up = np.arange(n) % 2 == 0
+    old = np.where(up, l - 1.0, l).astype(np.float32)  # every other ratio is e, past the clip
+    A, w, T = np.ones(n, np.float32), np.ones(n, np.float32), np.ones(n, np.float32)
+    cu = lambda x: torch.tensor(x, device="cuda")  # noqa: E731
+    got = pr.policy_loss(cu(z), cu(ids), cu(T), cu(w), cu(A), cu(old))
+    torch.cuda.synchronize()
+    g = got["grad"].cpu().numpy()
+    assert np.isfinite(g).all() and (g[up] == 0).all()
+    assert ((got["flags"].cpu().numpy() == pr.FLAG_CLIPPED) == up).all()
+    if not up.all():
+        o = oloss.policy_loss(z[1:2], "f32", ids[1:2], T[1:2], w[1:2], A[1:2], old[1:2])
+        near_gradient(got["grad"][1:2], o, T[1:2], torch.float32, 2 * L_ABS)
+
+
 def test_policy_probability_zero():
     """A token of probability 0: ratio 0; with a KL term the loss is infinite, as the formula has it."""
     logits = torch.zeros(1, 16, device="cuda")
