@@ -513,21 +513,18 @@ def _row_stride(t) -> int:
 
 
 def _loss_outputs(sizes, workspace, need: int, device):
-    """Float32 outputs of these sizes and the scratch of a call, from one allocation (see _outputs): the caller's
-    workspace where it serves, else a part of it. Returns the outputs, the workspace's address and its bytes."""
+    """Float32 outputs of these sizes and the scratch of a call, from one allocation as tensors of their own (see
+    _outputs): the caller's workspace where it serves, else the part before the outputs. Returns the workspace's
+    address, its bytes and the outputs."""
     if workspace is not None:
         _check_workspace(workspace, device)
         have = workspace.numel() * workspace.element_size()
         if have >= need and workspace.data_ptr() % 16 == 0:
-            return _split_floats(sizes, device), workspace.data_ptr(), have
-    *out, scratch = _split_floats([*sizes, (need + 3) // 4], device)
-    return out, scratch.data_ptr(), need
-
-
-def _split_floats(sizes, device):
-    """Float32 tensors of these sizes, each 16-byte aligned, from one allocation (see _outputs)."""
-    parts = [p for k in sizes for p in (k, -k % 4)]
-    return torch.empty(sum(parts), dtype=torch.float32, device=device).unsafe_split_with_sizes(parts)[::2]
+            out = torch.empty(sum(sizes), dtype=torch.float32, device=device).unsafe_split_with_sizes(sizes)
+            return workspace.data_ptr(), have, out
+    sizes = [(need + 3) // 4, *sizes]
+    scratch, *out = torch.empty(sum(sizes), dtype=torch.float32, device=device).unsafe_split_with_sizes(sizes)
+    return scratch.data_ptr(), need, out
 
 
 def policy_loss(logits: torch.Tensor, ids: torch.Tensor, temperature, weight: torch.Tensor, advantage: torch.Tensor,
@@ -557,7 +554,7 @@ def policy_loss(logits: torch.Tensor, ids: torch.Tensor, temperature, weight: to
     _check_row_floats(device, n, temperature=temperature, weight=weight, advantage=advantage, old_logprob=old_logprob,
                       ref_logprob=ref_logprob)
     L = _abi.lib()
-    (logprob, ratio, kl, loss), ws, ws_bytes = _loss_outputs((n, n, n, 1), workspace,
+    ws, ws_bytes, (logprob, ratio, kl, loss) = _loss_outputs((n, n, n, 1), workspace,
                                                              L.pr_policy_loss_workspace(code, n, V), device)
     flags = torch.empty(n, dtype=torch.int32, device=device)
     params = _abi.PolicyParams(clip_low, clip_high, kl_coef, grad_scale)
@@ -599,7 +596,7 @@ def preference_loss(logits: torch.Tensor, ids: torch.Tensor, temperature, weight
         raise ValueError("offsets must have 2 n_pairs + 1 entries")
     n_pairs = offsets.shape[0] // 2
     L = _abi.lib()
-    (logprob, q, pair, h, loss), ws, ws_bytes = _loss_outputs(
+    ws, ws_bytes, (logprob, q, pair, h, loss) = _loss_outputs(
         (n, 2 * n_pairs, n_pairs, n_pairs, 1), workspace, L.pr_preference_loss_workspace(code, n, V, n_pairs), device)
     flags = torch.empty(n, dtype=torch.int32, device=device)
     params = _abi.PreferenceParams(beta, label_smoothing, margin, grad_scale)

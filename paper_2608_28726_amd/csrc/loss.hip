@@ -357,18 +357,21 @@ __device__ __forceinline__ void grad_stretch(const LossRows& a, int64_t r, int32
   stream_grad(out + h + static_cast<int64_t>(j) * VEC, g);
 }
 
-// The gradients of the rows from `first` on (blockIdx.y).
-// SUM: the first workgroup also takes the loss that waits for the kernel
-// before this one, the mean of `sum`'s values. (Only small grids do that: it
-// saves a launch, but costs every workgroup about 10 %.)
-template <typename Tin, bool SUM>
+// The gradients of the rows from `first` on (blockIdx.y). With n_sum > 0 the
+// grid has a row more, whose first wave takes the loss that waits for the
+// kernel before this one: the mean of `sum`'s values.
+template <typename Tin>
 __global__ __launch_bounds__(kGradBlock) void grad_kernel(LossRows a, const RowGrad* rg, int64_t first,
                                                           const double* sum, int32_t n_sum, float* loss) {
-  if (SUM && blockIdx.x == 0 && blockIdx.y == 0) {
-    const double s = block_sum(sum, n_sum);
-    if (threadIdx.x == 0) loss[0] = static_cast<float>(s / n_sum);
-  }
   const int64_t r = first + blockIdx.y;
+  if (r == a.n_rows) {
+    if (blockIdx.x > 0 || threadIdx.x >= kWave) return;
+    double s = 0.0;
+    for (int32_t i = threadIdx.x; i < n_sum; i += kWave) s += sum[i];
+    s = wave_sum_d(s);
+    if (threadIdx.x == 0) loss[0] = static_cast<float>(s / n_sum);
+    return;
+  }
   grad_stretch<Tin>(a, r, blockIdx.x, rg[r]);
 }
 
@@ -671,13 +674,14 @@ int64_t grad_parts(int32_t V) {
 }
 
 template <typename Tin>
-hipError_t launch_grad(const LossRows& a, const RowGrad* rg, hipStream_t stream) {
+hipError_t launch_grad(const LossRows& a, const RowGrad* rg, hipStream_t stream, const double* sum = nullptr,
+                       int32_t n_sum = 0, float* loss = nullptr) {
   constexpr int64_t kMostY = 32768;
-  const int64_t parts = grad_parts<Tin>(a.V);
-  for (int64_t at = 0; at < a.n_rows; at += kMostY) {
-    const int64_t rows = a.n_rows - at < kMostY ? a.n_rows - at : kMostY;
-    hipLaunchKernelGGL((grad_kernel<Tin, false>), dim3(static_cast<unsigned>(parts), static_cast<unsigned>(rows)),
-                       dim3(kGradBlock), 0, stream, a, rg, at, nullptr, 0, nullptr);
+  const int64_t parts = grad_parts<Tin>(a.V), total = a.n_rows + (n_sum > 0 ? 1 : 0);
+  for (int64_t at = 0; at < total; at += kMostY) {
+    const int64_t rows = total - at < kMostY ? total - at : kMostY;
+    hipLaunchKernelGGL(grad_kernel<Tin>, dim3(static_cast<unsigned>(parts), static_cast<unsigned>(rows)),
+                       dim3(kGradBlock), 0, stream, a, rg, at, sum, n_sum, loss);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -719,6 +723,9 @@ __global__ __launch_bounds__(kStatsBlock) void preference_stats_kernel(Preferenc
   else
     preference_row(a, r, p, T, c, y, zy, l, rg);
 }
+
+// Most pairs whose mean one wave takes while the gradient is written.
+constexpr int32_t kPairsBeside = 4096;
 
 // One workgroup per pair: the sums over both requests, the pair's loss, and
 // the gradient's factors of the pair's rows. Rows that were split finish here.
@@ -878,18 +885,12 @@ hipError_t preference(const PreferenceArgs& a, hipStream_t stream) {
                        stream, a, l, rg, part, pair_loss);
     e = hipGetLastError();
   }
-  // The mean over pairs: a single pair's own kernel writes it, that of a small
-  // batch goes beside its gradient.
-  const int64_t parts = grad_parts<Tin>(a.rows.V);
-  if (e == hipSuccess && n > 0 && a.rows.grad) {
-    if (a.n_pairs > 1 && a.rows.n_rows * parts <= 2048 && a.n_pairs <= 4 * kGradBlock) {
-      hipLaunchKernelGGL((grad_kernel<Tin, true>), dim3(static_cast<unsigned>(parts), static_cast<unsigned>(n)),
-                         dim3(kGradBlock), 0, stream, a.rows, rg, int64_t{0}, pair_loss, a.n_pairs, a.loss);
-      return hipGetLastError();
-    }
-    e = launch_grad<Tin>(a.rows, rg, stream);
-  }
-  if (e != hipSuccess || a.n_pairs == 1) return e;
+  // The mean over pairs: a single pair's own kernel writes it, that of a few
+  // thousand goes beside their gradient.
+  const bool beside = n > 0 && a.rows.grad && a.n_pairs > 1 && a.n_pairs <= kPairsBeside;
+  if (e == hipSuccess && n > 0 && a.rows.grad)
+    e = launch_grad<Tin>(a.rows, rg, stream, pair_loss, beside ? a.n_pairs : 0, a.loss);
+  if (e != hipSuccess || beside || a.n_pairs == 1) return e;
   hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(kSumBlock), 0, stream, pair_loss,
                      static_cast<int64_t>(a.n_pairs), static_cast<double>(a.n_pairs), a.loss);
   return hipGetLastError();
