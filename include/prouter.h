@@ -510,7 +510,8 @@ void pr_policy_params_default(pr_policy_params* params);
  *                (grad_stride >= vocab), aligned to the element size; times
  *                grad_scale, rounded to nearest. NULL: not computed. It may be
  *                the logits themselves (the same pointer and stride); any
- *                other overlap is rejected.
+ *                other overlap is rejected. No other output may overlap an
+ *                input (not checked).
  *   workspace    device scratch of at least pr_policy_loss_workspace bytes,
  *                16-byte aligned; no initialisation needed.
  * A row with a nonzero weight that is flagged NONFINITE, BAD_TP or BAD_ID has

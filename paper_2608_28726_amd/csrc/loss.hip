@@ -230,12 +230,14 @@ __device__ RowSum stretch_sum(const Tin* row, int32_t V, int g, int G, float c) 
   return merge_block<BLOCK>(L, c);
 }
 
-// The sums of the rows' stretches, G of them a row.
+// The sums of the rows' stretches, G of them a row, and each row's token's
+// logit, for kernels that read it while the gradient takes the logits' place.
 template <typename Tin>
-__global__ __launch_bounds__(kStatsBlock) void parts_kernel(LossRows a, RowSum* part, int32_t G) {
+__global__ __launch_bounds__(kStatsBlock) void parts_kernel(LossRows a, RowSum* part, float* zy, int32_t G) {
   const int64_t r = blockIdx.x / G;
   const int g = blockIdx.x % G;
   if (a.weight[r] == 0.0f) return;
+  if (threadIdx.x == 0 && g == 0) zy[r] = token_logit<Tin>(a, r, a.ids[r]);
   const RowSum p = stretch_sum<Tin, kStatsBlock>(row_ptr<Tin>(a, r), a.V, g, G, scale_of(a.temperature[r]));
   if (threadIdx.x == 0) part[r * G + g] = p;
 }
@@ -321,6 +323,13 @@ __device__ __forceinline__ void stream_grad(Tin* at, const vec4u& v) {
 
 __device__ __forceinline__ float grad_of(float z, const RowGrad& q) { return q.k * fast_exp2(fmaf(z, q.c, -q.A)); }
 
+// The element outside a row's vectors that thread t takes: the first 8
+// threads those before the vectors, the next 8 those after them (V: none).
+__device__ __forceinline__ int32_t scalar_element(int t, int32_t h, int32_t tail, int32_t V) {
+  if (t < 8) return t < h ? t : V;
+  return t - 8 < V - tail ? tail + t - 8 : V;
+}
+
 // The gradient of a stretch of a row, a vector per thread of workgroup `part`:
 // short workgroups in memory order, past the caches, are what reads and
 // writes fastest at once here (6.5 TB/s; four vectors a thread 4.9). Each
@@ -336,7 +345,7 @@ __device__ __forceinline__ void grad_stretch(const LossRows& a, int64_t r, int32
   const int32_t y = a.ids[r];
   const bool zero = q.k == 0.0f && q.gy == 0.0f;
   if (part == 0 && t < 16) {
-    const int32_t e = t < 8 ? (t < h ? t : a.V) : tail + t - 8;  // the thread's scalar element
+    const int32_t e = scalar_element(t, h, tail, a.V);
     if (e < a.V) GradVec<Tin>::store1(out, e, zero ? 0.0f : e == y ? q.gy : grad_of(Elem<Tin>::load1(row, e), q));
   }
   const int32_t j = part * kGradBlock + t;
@@ -375,25 +384,24 @@ __global__ __launch_bounds__(kGradBlock) void grad_kernel(LossRows a, const RowG
   grad_stretch<Tin>(a, r, blockIdx.x, rg[r]);
 }
 
-// A split row's policy loss from its parts.
-template <typename Tin>
-__device__ __forceinline__ PolicyRow policy_from_parts(const PolicyArgs& a, int64_t r, const RowSum* part) {
+// A split row's policy loss from its parts. The logits are not read: they
+// may be giving way to the gradient.
+__device__ __forceinline__ PolicyRow policy_from_parts(const PolicyArgs& a, int64_t r, const RowSum* part,
+                                                       const float* zy) {
   const float w = a.rows.weight[r];
   if (w == 0.0f) return policy_masked();
-  const float T = a.rows.temperature[r], c = scale_of(T);
+  const float T = a.rows.temperature[r], c = scale_of(T), z = zy[r];
   const int32_t y = a.rows.ids[r];
-  const float zy = token_logit<Tin>(a.rows, r, y);
   const RowSum s = merge_parts(part + r * a.G, a.G, c);
-  return policy_row(a, r, row_value(s, T, c, y, a.rows.V, zy), T, c, s.S, w);
+  return policy_row(a, r, row_value(s, T, c, y, a.rows.V, z), T, c, s.S, w);
 }
 
 // All split rows' outputs, gradient factors (rg NULL: not wanted) and the
 // loss, by one workgroup.
-template <typename Tin>
-__device__ __forceinline__ void policy_finish(const PolicyArgs& a, const RowSum* part, RowGrad* rg) {
+__device__ __forceinline__ void policy_finish(const PolicyArgs& a, const RowSum* part, const float* zy, RowGrad* rg) {
   double sum = 0.0;
   for (int64_t r = threadIdx.x; r < a.rows.n_rows; r += kGradBlock) {
-    const PolicyRow p = policy_from_parts<Tin>(a, r, part);
+    const PolicyRow p = policy_from_parts(a, r, part, zy);
     policy_write(a, r, p);
     if (rg) rg[r] = p.grad;
     sum += p.term;
@@ -402,20 +410,20 @@ __device__ __forceinline__ void policy_finish(const PolicyArgs& a, const RowSum*
   if (threadIdx.x == 0) a.loss[0] = static_cast<float>(sum);
 }
 
-template <typename Tin>
-__global__ __launch_bounds__(kGradBlock) void policy_finish_kernel(PolicyArgs a, const RowSum* part, RowGrad* rg) {
-  policy_finish<Tin>(a, part, rg);
+__global__ __launch_bounds__(kGradBlock) void policy_finish_kernel(PolicyArgs a, const RowSum* part, const float* zy,
+                                                                  RowGrad* rg) {
+  policy_finish(a, part, zy, rg);
 }
 
 // The gradients of a few split rows: each workgroup works out its own row's
 // factors instead of waiting for a kernel that does. The first workgroup of
 // the grid's last row finishes the rows.
 template <typename Tin>
-__global__ __launch_bounds__(kGradBlock) void policy_parts_kernel(PolicyArgs a, const RowSum* part) {
+__global__ __launch_bounds__(kGradBlock) void policy_parts_kernel(PolicyArgs a, const RowSum* part, const float* zy) {
   if (blockIdx.y + 1 < gridDim.y)
-    grad_stretch<Tin>(a.rows, blockIdx.y, blockIdx.x, policy_from_parts<Tin>(a, blockIdx.y, part).grad);
+    grad_stretch<Tin>(a.rows, blockIdx.y, blockIdx.x, policy_from_parts(a, blockIdx.y, part, zy).grad);
   else if (blockIdx.x == 0)
-    policy_finish<Tin>(a, part, nullptr);
+    policy_finish(a, part, zy, nullptr);
 }
 
 // Makes the compiler forget what it knows of a vector, so that it unpacks it
@@ -534,7 +542,7 @@ __global__ __launch_bounds__((DW + 1) * kWave) void policy_row_kernel(PolicyArgs
       const RowView<Tin> x(a.rows, r);
       const float w = a.rows.weight[r];
       if (w == 0.0f) continue;
-      const int32_t e = lane < 8 ? (lane < x.h ? lane : V) : x.tail() + lane - 8;  // the lane's scalar element
+      const int32_t e = scalar_element(lane, x.h, x.tail(), V);
       const float T = a.rows.temperature[r], c = scale_of(T);
       const int32_t y = a.rows.ids[r];
       const float zy = token_logit<Tin>(a.rows, r, y);
@@ -561,7 +569,7 @@ __global__ __launch_bounds__((DW + 1) * kWave) void policy_row_kernel(PolicyArgs
       const int64_t r = row_of(rows_off, k);
       if (a.rows.weight[r] != 0.0f) continue;
       const RowView<Tin> x(a.rows, r);
-      const int32_t e = lane < 8 ? (lane < x.h ? lane : V) : x.tail() + lane - 8;
+      const int32_t e = scalar_element(lane, x.h, x.tail(), V);
       if (lane == 0) {
         policy_write(a, r, policy_masked());
         a.row_loss[r] = 0.0;
@@ -830,17 +838,18 @@ hipError_t policy(const PolicyArgs& a, hipStream_t stream) {
   if (a.G > 0) {
     RowGrad* rg = reinterpret_cast<RowGrad*>(a.row_loss);
     RowSum* part = reinterpret_cast<RowSum*>(rg + n);
+    float* zy = reinterpret_cast<float*>(part + n * a.G);
     hipLaunchKernelGGL(parts_kernel<Tin>, dim3(static_cast<unsigned>(n * a.G)), dim3(kStatsBlock), 0, stream, a.rows,
-                       part, a.G);
+                       part, zy, a.G);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t parts = grad_parts<Tin>(a.rows.V);
     if (a.rows.grad && n * parts <= kFewGroups) {
       hipLaunchKernelGGL(policy_parts_kernel<Tin>, dim3(static_cast<unsigned>(parts), static_cast<unsigned>(n + 1)),
-                         dim3(kGradBlock), 0, stream, a, part);
+                         dim3(kGradBlock), 0, stream, a, part, zy);
       return hipGetLastError();
     }
-    hipLaunchKernelGGL(policy_finish_kernel<Tin>, dim3(1), dim3(kGradBlock), 0, stream, a, part,
+    hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(kGradBlock), 0, stream, a, part, zy,
                        a.rows.grad ? rg : nullptr);
     e = hipGetLastError();
     return e == hipSuccess && a.rows.grad ? launch_grad<Tin>(a.rows, rg, stream) : e;
@@ -908,8 +917,8 @@ int policy_split(int64_t n_rows, int32_t V, pr_dtype dtype, bool grad) {
 size_t policy_workspace_bytes(int64_t n_rows, int32_t V, pr_dtype dtype) {
   const size_t n = n_rows < 0 ? 0 : static_cast<size_t>(n_rows);
   const size_t terms = up16(n * sizeof(double));
-  const size_t parts = n_rows < kSplitRows ? n * static_cast<size_t>(row_parts(n_rows, V, dtype)) * sizeof(RowSum) : 0;
-  return n * sizeof(RowGrad) + (terms > parts ? terms : parts);
+  const size_t parts = static_cast<size_t>(row_parts(n_rows, V, dtype)) * sizeof(RowSum) + sizeof(float);
+  return n * sizeof(RowGrad) + (n_rows < kSplitRows && n * parts > terms ? n * parts : terms);
 }
 
 hipError_t launch_policy(const PolicyArgs& a, pr_dtype dtype, hipStream_t stream) {
