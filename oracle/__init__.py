@@ -21,12 +21,16 @@ ship rule p >= tau):
   path draws each token from.
 * :mod:`oracle.calibrate` -- the threshold tau for a ship fraction on a
   validation pool, and the P-square streaming quantile (bounded memory).
+* :mod:`oracle.loss` -- the policy and preference losses over logit rows and
+  their gradients.
+* :mod:`oracle.adamw` -- the AdamW step and its 8-bit states.
 
 Parity pinning: every function here is pinned by ``tests/test_oracle_pins.py``,
 ``tests/test_oracle_sequence.py``, ``tests/test_oracle_head.py``,
-``tests/test_oracle_calibrate.py`` and ``tests/test_oracle_sampling.py`` against
-closed forms, invariants, pure-Python brute force and (for the head) an
-independent implementation of the same architecture, except the default
+``tests/test_oracle_calibrate.py``, ``tests/test_oracle_sampling.py``,
+``tests/test_oracle_loss.py`` and ``tests/test_oracle_adamw.py`` against closed
+forms, invariants, pure-Python brute force, differences and (for the head, the
+losses' gradients and the optimizer) an independent implementation, except the default
 score head (a fixed linear summary chosen because the paper publishes no
 trained head weights) and the transformer head's weights, which are *parity
 unpinned* against the paper.
@@ -57,3 +61,4 @@ from .sequence import (  # noqa: F401
 from .head import HEAD_WEIGHTS, head_score, head_scores  # noqa: F401,E402
 from .calibrate import P2Quantile, calibrate_threshold, p2_quantile  # noqa: F401,E402
 from .sampling import token_probabilities  # noqa: F401,E402
+from .loss import policy_loss, preference_loss  # noqa: F401,E402
