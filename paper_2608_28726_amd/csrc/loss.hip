@@ -430,12 +430,6 @@ __global__ __launch_bounds__(kGradBlock) void policy_parts_kernel(PolicyArgs a, 
 // anew in each pass instead of keeping 8 floats of each through all of them.
 __device__ __forceinline__ void forget(vec4u& v) { asm volatile("" : "+v"(v)); }
 
-// 16 bytes of each lane from memory into LDS: lane i's go to slots[i]
-// (`slots` is the wave's).
-__device__ __forceinline__ void load_to_lds(const vec4u* from, vec4u* slots) {
-  __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void*)slots, 16, 0, 0);
-}
-
 // A row as the fused kernel sees it: its vectors start at the first 16-byte
 // boundary, h elements in; up to 2 x 7 elements before and after are scalars.
 template <typename Tin>
@@ -462,8 +456,9 @@ struct RowView {
   }
 };
 
-// Vectors of the rows that policy_row_kernel holds, by its two sizes.
-constexpr int64_t kSmallRowVectors = 19 * 7 * kWave, kRowVectors = 20 * 15 * kWave;
+// Vectors of the rows that policy_row_kernel holds, by its sizes: four, two and
+// one workgroups a compute unit.
+constexpr int64_t kTinyRowVectors = 6 * 7 * kWave, kSmallRowVectors = 19 * 7 * kWave, kRowVectors = 20 * 15 * kWave;
 
 // Most rows whose order policy_row_kernel works out for itself.
 constexpr int64_t kListedRows = 65536;
@@ -471,22 +466,20 @@ constexpr int kListed = kListedRows / kCUs + 1;
 
 // The policy loss of a row and its gradient in one read of the row.
 //
-// A workgroup keeps the row on the chip between its sum and its gradient: its
-// first DW waves hold NR vectors per thread in registers and NL in LDS (which
-// the loads fill without passing through registers). One more wave takes what
-// is scalar in a row (its inputs, the elements outside the vectors, the loss
-// in 64 bits): the registers for that are not taken from those that hold the
-// row.
+// A workgroup keeps the row in registers between its sum and its gradient, NR
+// vectors in each thread of its first DW waves, and adds each vector to its
+// sums as it arrives. One more wave takes what is scalar in a row (its inputs,
+// the elements outside the vectors, the loss in 64 bits): the registers for
+// that are not taken from those that hold the row.
 //
 // The grid is the workgroups that run at once. Memory serves loads and stores
 // best when they do not mix, and workgroups that start together and do the
 // same stay together: so the rows that count are dealt out by their rank
 // among those that do, and the zero gradients of the others are written last.
-template <typename Tin, int DW, int NR, int NL>
+template <typename Tin, int DW, int NR>
 __global__ __launch_bounds__((DW + 1) * kWave) void policy_row_kernel(PolicyArgs a) {
   constexpr int VEC = Elem<Tin>::kVec, NT = DW * kWave;
-  __shared__ vec4u held[NL * NT];
-  __shared__ float sh_m[DW + 1], sh_s[DW + 1];
+  __shared__ RowSum sh_sum[DW];
   __shared__ RowGrad sh_q;
   __shared__ int32_t rows_on[kListed], rows_off[kListed];
   __shared__ uint32_t sh_n[DW + 1];
@@ -547,15 +540,12 @@ __global__ __launch_bounds__((DW + 1) * kWave) void policy_row_kernel(PolicyArgs
       const int32_t y = a.rows.ids[r];
       const float zy = token_logit<Tin>(a.rows, r, y);
       const float z = e < V ? Elem<Tin>::load1(x.row, e) : -INFINITY;
-      float m = wave_max(z);
-      if (lane == 0) sh_m[DW] = m;
+      LaneSum own;
+      own.add1(z, c);
+      const float S = wave_sum(own.s);
       __syncthreads();
-      m = wave_max(lane <= DW ? sh_m[lane] : -INFINITY);
-      const float A = fmaxf(m * c, kNegSentinel);
-      const float own = wave_sum(fast_exp2(fmaf(z, c, -A)));
-      __syncthreads();
-      const float S = wave_sum(lane < DW ? sh_s[lane] : lane == DW ? own : 0.0f);
-      const PolicyRow p = policy_row(a, r, row_value(RowSum{m, S}, T, c, y, V, zy), T, c, S, w);
+      const RowSum sum = merge_lanes(lane < DW ? sh_sum[lane] : RowSum{lane == DW ? own.mw : -INFINITY, lane == DW ? S : 0.0f}, c);
+      const PolicyRow p = policy_row(a, r, row_value(sum, T, c, y, V, zy), T, c, sum.S, w);
       const RowGrad q = p.grad;
       if (lane == 0) sh_q = q;
       __syncthreads();
@@ -580,69 +570,56 @@ __global__ __launch_bounds__((DW + 1) * kWave) void policy_row_kernel(PolicyArgs
   }
 
   const int t = threadIdx.x;  // below NT
+  // A row's temperature and token are read a turn ahead: its loads return in
+  // order, so what is read after the row's vectors arrives after them.
+  int64_t r_next = turns > 0 ? row_of(rows_on, 0) : 0;
+  float T_next = turns > 0 ? a.rows.temperature[r_next] : 1.0f;
+  int32_t y_next = turns > 0 ? a.rows.ids[r_next] : 0;
   for (int64_t k = 0; k < turns; ++k) {
-    const int64_t r = row_of(rows_on, k);
-    if (!listed && a.rows.weight[r] == 0.0f) continue;
+    const int64_t r = r_next;
+    const float c = scale_of(T_next);
+    const int32_t y = y_next;
+    const bool more = k + 1 < turns;
+    r_next = more ? row_of(rows_on, k + 1) : r;
+    if (!listed && a.rows.weight[r] == 0.0f) {
+      T_next = a.rows.temperature[r_next];
+      y_next = a.rows.ids[r_next];
+      continue;
+    }
     const RowView<Tin> x(a.rows, r);
-    // The lanes of a wave fill consecutive 16-byte slots of LDS. Only these
-    // lanes read them again, so no barrier is needed, only their arrival (and
-    // that the previous row's have been read).
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-    for (int u = 0; u < NL; ++u)
-      if (t < x.nvec - u * NT) load_to_lds(x.in(u * NT, t), held + u * NT + wave * kWave);
+    // Every lane loads for every u, past the row's end a vector of the row
+    // again, so that the loads in flight are always as many and a wave can
+    // wait for one after the other. (A row without vectors reads the
+    // workspace's first 16 bytes in their place.)
+    auto place = [&](int u) {
+      const int32_t at = u * NT < x.nvec ? u * NT : 0;
+      const vec4u* p = x.in(at, static_cast<uint32_t>(max(min(t, x.nvec - 1 - at), 0)));
+      return x.nvec > 0 ? p : reinterpret_cast<const vec4u*>(a.row_loss);
+    };
     vec4u v[NR];
 #pragma unroll
-    for (int u = 0; u < NR; ++u)
-      v[u] = t < x.nvec - (NL + u) * NT ? *x.in((NL + u) * NT, t) : neg_inf_vec<Tin>();
-    const float c = scale_of(a.rows.temperature[r]);
-    const int32_t y = a.rows.ids[r];
-
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    auto in_lds = [&](int u) { return t < x.nvec - u * NT ? held[u * NT + t] : neg_inf_vec<Tin>(); };
-
-    float m = -INFINITY;
-    auto top = [&](const vec4u& p) {
-      float z[VEC];
-      Elem<Tin>::unpack(p, z);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) m = fmaxf(m, z[i]);
-      __builtin_amdgcn_sched_barrier(0);
+    for (int u = 0; u < NR; ++u) v[u] = *place(u);
+    // A lane's vector u, -inf past the row's end.
+    auto within = [&](vec4u p, int u) {
+      if ((u + 1) * NT > x.nvec && t >= x.nvec - u * NT) p = neg_inf_vec<Tin>();
+      return p;
     };
-#pragma unroll
-    for (int u = 0; u < NL; ++u) top(in_lds(u));
-#pragma unroll
-    for (int u = 0; u < NR; ++u) top(v[u]);
-    m = wave_max(m);
-    if (lane == 0) sh_m[wave] = m;
-    __syncthreads();
-    m = wave_max(lane <= DW ? sh_m[lane] : -INFINITY);
-    const float A = fmaxf(m * c, kNegSentinel);
-    float S = 0.0f;
+    LaneSum L;
     auto sum = [&](const vec4u& p) {
       float z[VEC];
       Elem<Tin>::unpack(p, z);
-      float s0 = fast_exp2(fmaf(z[0], c, -A)), s1 = fast_exp2(fmaf(z[1], c, -A));
-#pragma unroll
-      for (int i = 2; i < VEC; i += 2) {
-        s0 += fast_exp2(fmaf(z[i], c, -A));
-        s1 += fast_exp2(fmaf(z[i + 1], c, -A));
-      }
-      S += s0 + s1;
+      L.add(z, c);
       __builtin_amdgcn_sched_barrier(0);
     };
 #pragma unroll
-    for (int u = 0; u < NL; ++u) sum(in_lds(u));
-#pragma unroll
-    for (int u = 0; u < NR; ++u) {
-      forget(v[u]);
-      sum(v[u]);
-    }
-    S = wave_sum(S);
-    if (lane == 0) sh_s[wave] = S;
+    for (int u = 0; u < NR; ++u) sum(within(v[u], u));
+    const float S = wave_sum(L.s);
+    if (lane == 0) sh_sum[wave] = RowSum{L.mw, S};
     __syncthreads();
     __syncthreads();
     const RowGrad q = sh_q;
+    T_next = a.rows.temperature[r_next];
+    y_next = a.rows.ids[r_next];
     const int32_t jy = y >= x.h && y < x.tail() ? (y - x.h) / VEC : -1, ky = (y - x.h) % VEC;
     auto put = [&](const vec4u& p, int32_t at) {
       float z[VEC];
@@ -657,12 +634,9 @@ __global__ __launch_bounds__((DW + 1) * kWave) void policy_row_kernel(PolicyArgs
       __builtin_amdgcn_sched_barrier(0);
     };
 #pragma unroll
-    for (int u = 0; u < NL; ++u)
-      if (t < x.nvec - u * NT) put(held[u * NT + t], u * NT);
-#pragma unroll
     for (int u = 0; u < NR; ++u) {
       forget(v[u]);
-      if (t < x.nvec - (NL + u) * NT) put(v[u], (NL + u) * NT);
+      if (t < x.nvec - u * NT) put(v[u], u * NT);
     }
   }
   for (int64_t k = 0; k < turns_off; ++k) {
@@ -855,13 +829,14 @@ hipError_t policy(const PolicyArgs& a, hipStream_t stream) {
     return e == hipSuccess && a.rows.grad ? launch_grad<Tin>(a.rows, rg, stream) : e;
   }
   if (n > 0 && a.rows.grad && nvec <= kRowVectors) {
-    const bool small = nvec <= kSmallRowVectors;
-    const int64_t most = small ? 2 * kCUs : kCUs;
+    const int64_t most = nvec <= kTinyRowVectors ? 4 * kCUs : nvec <= kSmallRowVectors ? 2 * kCUs : kCUs;
     const dim3 grid(static_cast<unsigned>(n < most ? n : most));
-    if (small)
-      hipLaunchKernelGGL((policy_row_kernel<Tin, 7, 11, 8>), grid, dim3(512), 0, stream, a);
+    if (nvec <= kTinyRowVectors)
+      hipLaunchKernelGGL((policy_row_kernel<Tin, 7, 6>), grid, dim3(512), 0, stream, a);
+    else if (nvec <= kSmallRowVectors)
+      hipLaunchKernelGGL((policy_row_kernel<Tin, 7, 19>), grid, dim3(512), 0, stream, a);
     else
-      hipLaunchKernelGGL((policy_row_kernel<Tin, 15, 12, 8>), grid, dim3(1024), 0, stream, a);
+      hipLaunchKernelGGL((policy_row_kernel<Tin, 15, 20>), grid, dim3(1024), 0, stream, a);
     e = hipGetLastError();
   } else if (n > 0) {
     RowGrad* rg = reinterpret_cast<RowGrad*>(reinterpret_cast<char*>(a.row_loss) +

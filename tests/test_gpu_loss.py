@@ -156,6 +156,59 @@ def test_policy(n, V, dtype, pad, start, use_ref):
         assert bool((d.as_strided((n - 1, pad), (V + pad, 1), d.storage_offset() + V) == 0).all())
 
 
+@pytest.mark.parametrize("n,V,dtype,pad", [(70001, 9, torch.float32, 0), (66000, 40, torch.bfloat16, 3),
+                                           (2500, 3001, torch.bfloat16, 0), (1100, 8000, torch.float32, 1),
+                                           (600, 32000, torch.float32, 0), (1300, 50257, torch.bfloat16, 0),
+                                           (300, 70001, torch.float32, 0), (600, 151936, torch.bfloat16, 0),
+                                           (1030, 170000, torch.bfloat16, 0)])
+def test_policy_many_rows(n, V, dtype, pad):
+    """Batches that take every workgroup several rows, in each size of a row, listed or not, against plain float64
+    operations on the device."""
+    print(f"case policy many n={n} V={V} {dtype}", flush=True)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    logits = torch.empty(n, V + pad, device="cuda").normal_(generator=g).mul_(3.0).to(dtype)[:, :V]
+    ids = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    T = torch.rand(n, generator=g, device="cuda") + 0.5
+    w = torch.rand(n, generator=g, device="cuda") + 0.1
+    w[torch.rand(n, generator=g, device="cuda") < 0.3] = 0.0
+    if n > 20:
+        w[5:17] = 0.0
+    on = w != 0
+    logits[~on] = math.nan
+    A = torch.empty(n, device="cuda").normal_(generator=g)
+    l = torch.zeros(n, dtype=torch.float64, device="cuda")
+    step = max(1, 200_000_000 // V)
+    for a in range(0, n, step):
+        u = logits[a:a + step].double() / T[a:a + step, None].double()
+        l[a:a + step] = torch.log_softmax(u, 1).gather(1, ids[a:a + step, None].long())[:, 0]
+    delta = torch.empty(n, device="cuda").normal_(generator=g).mul_(0.3)
+    delta = torch.where((delta.exp() - 0.8).abs() < 2e-3, delta + 0.01, delta)
+    delta = torch.where((delta.exp() - 1.2).abs() < 2e-3, delta + 0.01, delta)
+    old = torch.where(on, (l - delta).float(), 0.0)
+    got = pr.policy_loss(logits, ids, T, w, A, old, grad_scale=0.5)
+    torch.cuda.synchronize()
+    ratio = torch.exp(l - old.double())
+    free, held = ratio * A, ratio.clamp(0.8, 1.2) * A
+    clipped = on & (free > held)
+    terms = torch.where(on, -w.double() * torch.minimum(free, held), 0.0)
+    assert torch.equal(got["flags"], torch.where(on, torch.where(clipped, pr.FLAG_CLIPPED, 0), pr.FLAG_MASKED).int())
+    near("logprob", got["logprob"].cpu(), torch.where(on, l, 0.0).cpu(), L_ABS)
+    near("loss", got["loss"].cpu(), [float(terms.sum())], 2 * L_ABS * float(terms.abs().sum()))
+    coef = torch.where(on, 0.5 * w.double() * torch.where(clipped, 0.0, -free) / T.double(), 0.0)
+    half_ulp = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24
+    for a in range(0, n, step):
+        rows = slice(a, a + step)
+        u = logits[rows].double() / T[rows, None].double()
+        want = -torch.softmax(u, 1)
+        want.scatter_add_(1, ids[rows, None].long(), torch.ones_like(want[:, :1]))
+        want = torch.where(on[rows, None], want * coef[rows, None], 0.0)
+        off = (got["grad"][rows].double() - want).abs()
+        allowed = coef[rows, None].abs() * (2.0 ** -21 + 2 * L_ABS) + (half_ulp * 1.01 + 2 * L_ABS) * want.abs() + 1e-38
+        bad = ~(off <= allowed)
+        assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:3].tolist())
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("V", [65, 4096, 50257])
 def test_policy_gradient_elsewhere(V, dtype):
@@ -343,6 +396,50 @@ def test_preference(lengths, V, dtype, pad, start, options):
     again = call(grad_scale=3.0, grad=d)
     for k in ("loss", "pair_logit", "seq_logratio", "logprob", "grad"):
         assert torch.equal(again[k], got[k]), k
+
+
+@pytest.mark.parametrize("n_pairs,most,V,dtype", [(5000, 2, 5, torch.float32), (300, 12, 3001, torch.bfloat16),
+                                                  (40, 60, 50257, torch.float32), (2, 900, 200, torch.float32)])
+def test_preference_many_pairs(n_pairs, most, V, dtype):
+    """Batches of many pairs or long requests (empty ones among them), against plain float64 operations on the device."""
+    rng = np.random.default_rng(n_pairs)
+    lengths = rng.integers(0, most + 1, 2 * n_pairs)
+    off = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+    n = int(off[-1])
+    print(f"case preference many pairs={n_pairs} rows={n} V={V} {dtype}", flush=True)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    logits = torch.empty(n, V, device="cuda").normal_(generator=g).mul_(3.0).to(dtype)
+    ids = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    T = torch.rand(n, generator=g, device="cuda") + 0.5
+    w = torch.rand(n, generator=g, device="cuda") + 0.1
+    w[torch.rand(n, generator=g, device="cuda") < 0.2] = 0.0
+    u = logits.double() / T[:, None].double()
+    p = torch.softmax(u, 1)
+    l = torch.log_softmax(u, 1).gather(1, ids[:, None].long())[:, 0]
+    ref = (l + torch.empty(n, device="cuda").normal_(generator=g) * 0.3).float()
+    req = torch.from_numpy(np.repeat(np.arange(2 * n_pairs), lengths)).cuda()
+    q = torch.zeros(2 * n_pairs, dtype=torch.float64, device="cuda").index_add_(0, req, w.double() * (l - ref.double()))
+    h = 0.3 * (q[0::2] - q[1::2])
+    got = pr.preference_loss(logits, ids, T, w, torch.from_numpy(off).cuda(), ref, beta=0.3, grad_scale=n_pairs)
+    torch.cuda.synchronize()
+    q_abs = L_ABS * most * 1.1
+    near("seq_logratio", got["seq_logratio"].cpu(), q.cpu(), q_abs)
+    near("pair_logit", got["pair_logit"].cpu(), h.cpu(), 0.6 * q_abs)
+    want = torch.nn.functional.softplus(-h)
+    near("pair_loss", got["pair_loss"].cpu(), want.cpu(), 0.6 * q_abs)
+    near("loss", got["loss"].cpu(), [float(want.mean())], 0.6 * q_abs)
+    dq = torch.stack([-torch.sigmoid(-h), torch.sigmoid(-h)], 1).reshape(-1) * 0.3
+    coef = (dq[req] * w.double() / T.double())[:, None]
+    want = -coef * p
+    want.scatter_add_(1, ids[:, None].long(), coef)
+    half_ulp = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24
+    rel = 0.6 * q_abs + 2.0 ** -22
+    bad = ~((got["grad"].double() - want).abs()
+            <= coef.abs() * (2.0 ** -21 + rel) + (half_ulp * 1.01 + rel) * want.abs() + 1e-38)
+    assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:3].tolist())
+    alone = pr.preference_loss(logits, ids, T, w, torch.from_numpy(off).cuda(), ref, beta=0.3, grad=False)
+    assert abs(float(alone["loss"]) - float(got["loss"])) <= 2.0 ** -23 * abs(float(got["loss"]))
 
 
 def test_preference_bad_and_masked_rows():
