@@ -456,9 +456,14 @@ struct RowView {
   }
 };
 
-// Vectors of the rows that policy_row_kernel holds, by its sizes: four, two and
-// one workgroups a compute unit.
-constexpr int64_t kTinyRowVectors = 6 * 7 * kWave, kSmallRowVectors = 19 * 7 * kWave, kRowVectors = 20 * 15 * kWave;
+// Vectors of the rows that policy_row_kernel holds, by its two sizes (two and
+// one workgroups a compute unit). Shorter rows than the least take two passes:
+// what a workgroup spends on a row beside its vectors then costs more than the
+// second read. 1.2 GB of bfloat16 rows, held and in two passes: 16,384 logits a
+// row 684 and 608 us, 32,000 578 and 576, 50,257 510 and 593, 151,936 483 and
+// 569.
+constexpr int64_t kLeastRowVectors = 4500, kSmallRowVectors = 19 * 7 * kWave, kRowVectors = 20 * 15 * kWave;
+bool held_row(int64_t nvec) { return nvec >= kLeastRowVectors && nvec <= kRowVectors; }
 
 // Most rows whose order policy_row_kernel works out for itself.
 constexpr int64_t kListedRows = 65536;
@@ -612,7 +617,8 @@ __global__ __launch_bounds__((DW + 1) * kWave) void policy_row_kernel(PolicyArgs
       __builtin_amdgcn_sched_barrier(0);
     };
 #pragma unroll
-    for (int u = 0; u < NR; ++u) sum(within(v[u], u));
+    for (int u = 0; u < NR; ++u)
+      if (u * NT < x.nvec) sum(within(v[u], u));
     const float S = wave_sum(L.s);
     if (lane == 0) sh_sum[wave] = RowSum{L.mw, S};
     __syncthreads();
@@ -828,12 +834,10 @@ hipError_t policy(const PolicyArgs& a, hipStream_t stream) {
     e = hipGetLastError();
     return e == hipSuccess && a.rows.grad ? launch_grad<Tin>(a.rows, rg, stream) : e;
   }
-  if (n > 0 && a.rows.grad && nvec <= kRowVectors) {
-    const int64_t most = nvec <= kTinyRowVectors ? 4 * kCUs : nvec <= kSmallRowVectors ? 2 * kCUs : kCUs;
+  if (n > 0 && a.rows.grad && held_row(nvec)) {
+    const int64_t most = nvec <= kSmallRowVectors ? 2 * kCUs : kCUs;
     const dim3 grid(static_cast<unsigned>(n < most ? n : most));
-    if (nvec <= kTinyRowVectors)
-      hipLaunchKernelGGL((policy_row_kernel<Tin, 7, 6>), grid, dim3(512), 0, stream, a);
-    else if (nvec <= kSmallRowVectors)
+    if (nvec <= kSmallRowVectors)
       hipLaunchKernelGGL((policy_row_kernel<Tin, 7, 19>), grid, dim3(512), 0, stream, a);
     else
       hipLaunchKernelGGL((policy_row_kernel<Tin, 15, 20>), grid, dim3(1024), 0, stream, a);
@@ -886,7 +890,7 @@ int policy_split(int64_t n_rows, int32_t V, pr_dtype dtype, bool grad) {
   if (n_rows <= 0 || n_rows >= kSplitRows) return 0;
   const int64_t nvec = V / (dtype == PR_BF16 ? 8 : 4);
   const int64_t few = nvec <= kSmallRowVectors ? kFewSmallRows : kFewRows;
-  return grad && nvec <= kRowVectors && n_rows > few ? 0 : row_parts(n_rows, V, dtype);
+  return grad && held_row(nvec) && n_rows > few ? 0 : row_parts(n_rows, V, dtype);
 }
 
 size_t policy_workspace_bytes(int64_t n_rows, int32_t V, pr_dtype dtype) {
