@@ -636,7 +636,8 @@ pr_status pr_adamw_create(const pr_adamw_tensor* tensors, int32_t n_tensors, pr_
  * One step. grads: host array of n_tensors device pointers, read during the
  * call, or NULL: those of the tensors' descriptors. A NULL entry leaves that
  * tensor as it is. Steps of a handle share no scratch; those on the same
- * tensors must be ordered.
+ * tensors must be ordered. A step captured into a graph repeats its rates,
+ * step number and random numbers on every replay.
  */
 pr_status pr_adamw_step(pr_adamw* handle, const void* const* grads, const pr_adamw_params* params, void* stream);
 

@@ -44,7 +44,7 @@ struct AdamPlan {
 };
 
 // Bytes of the last-level cache: a step over more gains by going past the
-// caches (222 million elements, 32-bit states: 1,196 -> 1,078 us, 8-bit ones
+// caches (216 million elements, 32-bit states: 1,196 -> 1,078 us, 8-bit ones
 // 650 -> 599), a smaller one finds there what the pass before it left.
 constexpr int64_t kAdamCached = int64_t{256} << 20;
 

@@ -292,6 +292,37 @@ def test_policy_special_rows(V, dtype):
         assert math.isnan(float(got["loss"])) == (max(count) >= 8)
 
 
+@pytest.mark.parametrize("V,dtype", [(30000, torch.float32), (60000, torch.bfloat16), (40000, torch.float32),
+                                     (80000, torch.bfloat16)])
+def test_policy_special_rows_held(V, dtype):
+    """The special rows among many rows, of the sizes that a workgroup holds: all count, then only the good ones."""
+    base = special_rows(V, dtype)
+    k, times = len(base), 128 // len(base) + 1
+    n = k * times
+    logits = torch.tensor(np.stack([r[0] for r in base])).to(dtype)
+    ids = np.array([r[1] for r in base], np.int32)
+    T = np.array([r[2] for r in base], np.float32)
+    A = np.linspace(-1, 1.5, k).astype(np.float32)
+    good = np.arange(k) < 8
+    fine = oloss.policy_loss(raw_of(logits), name_of(dtype), ids, T, np.where(good, 1.0, 0.0), A, np.full(k, -3.0, np.float32))
+    old = np.full(k, -3.0, np.float32)
+    old[:8] = fine["logprob"][:8].clip(min=-80.0) - 0.1
+    cu = lambda x: torch.tensor(np.tile(x, times), device="cuda")  # noqa: E731
+    for w in (np.full(k, 0.5, np.float32), np.where(good, 0.5, 0.0).astype(np.float32)):
+        o = oloss.policy_loss(raw_of(logits), name_of(dtype), ids, T, w, A, old)
+        got = pr.policy_loss(logits.cuda().repeat(times, 1), cu(ids), cu(T), cu(w), cu(A), cu(old))
+        torch.cuda.synchronize()
+        assert got["flags"].cpu().tolist() == o["flags"].tolist() * times
+        near("logprob", got["logprob"].cpu(), np.tile(o["logprob"], times), 4 * L_ABS)
+        g = got["grad"].view(times, k, V)
+        # the loss is a mean over the rows: `times` as many rows, if the weights are normed by their count
+        for t in range(times):
+            near_gradient(g[t, :8], {"dl": o["dl"][good], "grad": o["grad"][good]}, T[good], dtype, 2e-5)
+            bad = g[t, 8:].float().cpu().numpy()
+            assert np.isnan(bad).all() if w[8] else (bad == 0).all()
+        assert math.isnan(float(got["loss"])) == bool(w[8])
+
+
 @pytest.mark.parametrize("n", [3, 50, 700])
 @pytest.mark.parametrize("V", [1000, 70000])
 def test_policy_clipped_rows_with_forbidden_tokens(n, V):
