@@ -271,12 +271,16 @@ __device__ __forceinline__ RowSum merge_parts(const RowSum* part, int G, float c
   return s;
 }
 
+// Workgroups of a launch of kStatsBlock or kPairBlock threads: a grid holds
+// less than 2^32 threads, so longer lists of rows or pairs take several.
+constexpr int64_t kMostGroups = int64_t{1} << 23;
+
 // One workgroup per row: its sum of exps, then everything but its gradient.
 // The read bounds it: 912 counting of 2,048 rows of 262,144 float32 logits
 // take 166 us (0.96 GB, 5.8 TB/s).
 template <typename Tin>
-__global__ __launch_bounds__(kStatsBlock) void policy_stats_kernel(PolicyArgs a, RowGrad* rg) {
-  const int64_t r = blockIdx.x;
+__global__ __launch_bounds__(kStatsBlock) void policy_stats_kernel(PolicyArgs a, RowGrad* rg, int64_t first) {
+  const int64_t r = first + blockIdx.x;
   const float w = a.rows.weight[r];
   PolicyRow p = policy_masked();
   if (w != 0.0f) {
@@ -714,8 +718,8 @@ __device__ __forceinline__ double preference_row(const PreferenceArgs& a, int64_
 // 621 us (4.0 GB, 6.5 TB/s).
 template <typename Tin>
 __global__ __launch_bounds__(kStatsBlock) void preference_stats_kernel(PreferenceArgs a, double* l, RowGrad* rg,
-                                                                      RowSum* part) {
-  const int64_t r = blockIdx.x / a.G;
+                                                                      RowSum* part, int64_t first) {
+  const int64_t r = first + blockIdx.x / a.G;
   const int g = blockIdx.x % a.G;
   if (a.rows.weight[r] == 0.0f) {
     if (threadIdx.x == 0 && g == 0) {
@@ -749,9 +753,10 @@ __device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log
 
 template <typename Tin>
 __global__ __launch_bounds__(kPairBlock) void preference_pair_kernel(PreferenceArgs a, double* l, RowGrad* rg,
-                                                                    const RowSum* part, double* pair_loss) {
+                                                                    const RowSum* part, double* pair_loss,
+                                                                    int32_t first) {
   __shared__ double sh[2][kPairBlock / kWave];
-  const int p = blockIdx.x;
+  const int64_t p = first + static_cast<int32_t>(blockIdx.x);
   int64_t off[3];
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
@@ -835,6 +840,11 @@ constexpr int64_t kFewRows = 64, kFewSmallRows = 32;
 // launch, 1 to 2 us, and costs more than that past this many.
 constexpr int64_t kFewGroups = 512;
 
+// Workgroups of the launch that starts at `at` of `total`.
+unsigned groups_from(int64_t at, int64_t total) {
+  return static_cast<unsigned>(total - at < kMostGroups ? total - at : kMostGroups);
+}
+
 size_t up16(size_t b) { return (b + 15) & ~size_t{15}; }
 
 template <typename Tin>
@@ -871,8 +881,10 @@ hipError_t policy(const PolicyArgs& a, hipStream_t stream) {
   } else if (n > 0) {
     RowGrad* rg = reinterpret_cast<RowGrad*>(reinterpret_cast<char*>(a.row_loss) +
                                              up16(static_cast<size_t>(n) * sizeof(double)));
-    hipLaunchKernelGGL(policy_stats_kernel<Tin>, dim3(static_cast<unsigned>(n)), dim3(kStatsBlock), 0, stream, a, rg);
-    e = hipGetLastError();
+    for (int64_t at = 0; at < n && e == hipSuccess; at += kMostGroups) {
+      hipLaunchKernelGGL(policy_stats_kernel<Tin>, dim3(groups_from(at, n)), dim3(kStatsBlock), 0, stream, a, rg, at);
+      e = hipGetLastError();
+    }
     if (e == hipSuccess && a.rows.grad) e = launch_grad<Tin>(a.rows, rg, stream);
   }
   if (e != hipSuccess) return e;
@@ -889,14 +901,15 @@ hipError_t preference(const PreferenceArgs& a, hipStream_t stream) {
   double* pair_loss = l + n;
   RowSum* part = reinterpret_cast<RowSum*>(pair_loss + a.n_pairs);
   hipError_t e = hipSuccess;
-  if (n > 0) {
-    hipLaunchKernelGGL(preference_stats_kernel<Tin>, dim3(static_cast<unsigned>(n * static_cast<size_t>(a.G))),
-                       dim3(kStatsBlock), 0, stream, a, l, rg, part);
+  // Only batches of few rows are split: with G > 1 one launch takes them all.
+  for (int64_t at = 0; at < a.rows.n_rows && e == hipSuccess; at += kMostGroups) {
+    hipLaunchKernelGGL(preference_stats_kernel<Tin>, dim3(groups_from(at, a.rows.n_rows) * static_cast<unsigned>(a.G)),
+                       dim3(kStatsBlock), 0, stream, a, l, rg, part, at);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && a.n_pairs > 0) {
-    hipLaunchKernelGGL(preference_pair_kernel<Tin>, dim3(static_cast<unsigned>(a.n_pairs)), dim3(kPairBlock), 0,
-                       stream, a, l, rg, part, pair_loss);
+  for (int64_t at = 0; at < a.n_pairs && e == hipSuccess; at += kMostGroups) {
+    hipLaunchKernelGGL(preference_pair_kernel<Tin>, dim3(groups_from(at, a.n_pairs)), dim3(kPairBlock), 0, stream, a,
+                       l, rg, part, pair_loss, static_cast<int32_t>(at));
     e = hipGetLastError();
   }
   // The mean over pairs: a single pair's own kernel writes it, that of a few

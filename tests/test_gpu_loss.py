@@ -537,6 +537,43 @@ def test_differences(dtype):
         assert abs(num - float(basep["grad"][r, v])) < step * step + 1e-6 / step
 
 
+def test_more_rows_than_a_launch():
+    """More rows, and more pairs, than workgroups whose threads are counted in 32 bits: several launches take them. Two
+    tokens a row, whose log-probs are log sigmoids."""
+    n_pairs = (1 << 24) + 3
+    n = 2 * n_pairs
+    print(f"case more rows than a launch n={n}", flush=True)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    logits = torch.empty(n, 2, device="cuda").normal_(generator=g)
+    ids = torch.randint(0, 2, (n,), generator=g, device="cuda", dtype=torch.int32)
+    one = torch.ones(n, device="cuda")
+    gap = (logits[:, 0].double() - logits[:, 1].double()) * (1 - 2 * ids)
+    l = torch.nn.functional.logsigmoid(gap)
+    d_other = -torch.sigmoid(-gap)  # dl/dz of the other token
+
+    def check(got, coef):
+        assert float((got["logprob"].double() - l).abs().max()) <= L_ABS + 2.0 ** -24 * float(l.abs().max())
+        assert not bool(got["flags"].any())
+        other = got["grad"].double().gather(1, 1 - ids[:, None].long())[:, 0]
+        of_y = got["grad"].double().gather(1, ids[:, None].long())[:, 0]
+        want = coef * d_other
+        for x in (other - want, of_y + want):
+            assert bool((x.abs() <= coef.abs() * (2.0 ** -21 + 2 * L_ABS) + 2.0 ** -23 * want.abs() + 1e-38).all())
+
+    # ratio 1, advantage 1: the loss is -n / n
+    got = pr.policy_loss(logits, ids, 1.0, one / n, one, l.float(), grad_scale=n)
+    check(got, -(one / n).double() * n)
+    assert abs(float(got["loss"]) + 1.0) <= 1e-5
+    off = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    got = pr.preference_loss(logits, ids, 1.0, one, off, beta=1.0, grad_scale=n_pairs)
+    h = l[0::2] - l[1::2]
+    assert float((got["pair_logit"].double() - h).abs().max()) <= 2 * L_ABS + 2.0 ** -23 * float(h.abs().max())
+    want = float(torch.nn.functional.softplus(-h).mean())
+    assert abs(float(got["loss"]) - want) <= 2 * L_ABS + 2.0 ** -23
+    check(got, torch.stack([-torch.sigmoid(-h), torch.sigmoid(-h)], 1).reshape(-1))
+
+
 def test_many_rows_on_another_stream():
     """Calls on a stream of their own, with a workspace of the caller's filled with NaN, give the same results."""
     n, V = 700, 3001
