@@ -331,7 +331,9 @@ void launch_kind(const AdamPlan& plan, int64_t at, int64_t count, const AdamScal
                   : launch<Tp, Tg, false, false>(c, count, s, grads, stream);
 }
 
-constexpr int64_t kMostGroups = int64_t{1} << 30;  // workgroups of a launch
+// Workgroups of a launch: a grid holds less than 2^32 threads, so a plan of
+// more than 8.6e9 elements takes several.
+constexpr int64_t kMostGroups = (int64_t{1} << 31) / kThreads;
 
 }  // namespace
 

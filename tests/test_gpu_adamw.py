@@ -189,6 +189,37 @@ def test_eight_bit_training_follows_the_32_bit_one():
     assert losses[0] < 0.02 * first and losses[1] < 0.02 * first + 1.2 * losses[0], (first, losses)
 
 
+def test_more_elements_than_a_launch():
+    """17.2e9 elements, more than 2^32 threads take 4 each: several launches, and element offsets past 2^34. Random
+    numbers repeat after 2^32 elements, and so does all else here."""
+    n = (1 << 34) + 4096 + 77
+    if torch.cuda.mem_get_info()[0] < 115 << 30:
+        pytest.skip("needs 103 GB of device memory")
+    print(f"case adamw n={n}", flush=True)
+    p = torch.full((n,), 1.0, dtype=torch.bfloat16, device="cuda")
+    g = torch.full((n,), -0.25, dtype=torch.bfloat16, device="cuda")
+    opt = pr.AdamW([p], grads=[g], state_bits=8, seed=5)
+    # the first step moves every element by lr, twice the spacing of bfloat16 above 1
+    opt.step(lr=2.0 ** -6, eps=0.0, weight_decay=0.0)
+    torch.cuda.synchronize()
+    s = opt.states[0]
+    k = 70000
+    m, v = f32_moments(np.full(k, -0.25, np.float32), np.zeros(k, np.float32), np.zeros(k, np.float32),
+                       dict(beta1=0.9, beta2=0.999), 1.0)
+    bits = oadam.random_bits(k, 0, 5, 1)
+    for name, x, rnd in (("m", m, bits & np.uint64(0xFFFFF)), ("v", v, bits >> np.uint64(12))):
+        codes, exps = oadam.encode(x, rnd.astype(np.int64), name)
+        assert np.array_equal(s[name][:k].cpu().numpy(), codes)
+        assert np.array_equal(s[name + "_exp"][:k // 256].cpu().numpy(), exps[:k // 256])
+    assert float(p[:k].min()) >= 1.0 + 2.0 ** -7 and float(p[:k].max()) <= 1.0 + 3 * 2.0 ** -7
+    for t, period in ((p, 1 << 32), (s["m"], 1 << 32), (s["v"], 1 << 32), (s["m_exp"], 1 << 24), (s["v_exp"], 1 << 24)):
+        for a in range(period, t.numel(), period):
+            part = t[a:a + period]
+            assert torch.equal(part, t[:part.numel()]), (period, a)
+    del p, g, opt, s, t, part
+    torch.cuda.empty_cache()
+
+
 def test_step_on_another_stream_and_in_a_graph():
     sizes = [5, 300, 70001]
     runs = []
