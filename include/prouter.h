@@ -496,7 +496,8 @@ void pr_policy_params_default(pr_policy_params* params);
  *   kl   = exp(d) - 1 - d
  *   loss = sum over rows of weight (kl_coef kl - gain)
  *   dloss/dz_v = weight ((clipped ? 0 : -ratio A) - kl_coef (exp(d) - 1)) / T (delta_vy - softmax(u)_v)
- * where clipped says that the second product is strictly the smaller.
+ * where clipped says that the second product is strictly the smaller; with
+ * kl_coef = 0 there is no KL term, also where kl is infinite.
  *   logits .. temperature  as for pr_token_features (no top-p).
  *   weight       float [n_rows]: each row's weight in the sum, mask and
  *                normaliser in one. A row of weight 0 is not read (its logits

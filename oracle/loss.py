@@ -20,7 +20,8 @@ R24  A row of weight 0 takes no part: its logits, id and temperature may be
 R25  A row that counts and is NONFINITE, BAD_TP or BAD_ID (the rules of R1, R3
      and R7) has l = NaN: the loss and the row's gradient are NaN.
 R26  At ratio A == clip(ratio) A the gradient goes through the ratio: only a
-     strictly smaller clipped product stops it.
+     strictly smaller clipped product stops it. kl_coef = 0 leaves the KL term
+     out also where the KL is infinite (a token of probability 0).
 """
 
 from __future__ import annotations
@@ -92,8 +93,9 @@ def policy_loss(raw, dtype, ids, T, weight, advantage, old_logprob, ref_logprob=
             flags[r] |= FLAG_CLIPPED
         d = float(ref_logprob[r]) - l[r] if ref_logprob is not None else 0.0
         kl[r] = math.inf if d == math.inf else math.expm1(d) - d
-        terms.append(w * (kl_coef * kl[r] - (bounded * A if clipped else ratio[r] * A)))
-        dl[r] = w * ((0.0 if clipped else -ratio[r] * A) - kl_coef * math.expm1(d))
+        beta_kl, beta_rise = (kl_coef * kl[r], kl_coef * math.expm1(d)) if kl_coef else (0.0, 0.0)
+        terms.append(w * (beta_kl - (bounded * A if clipped else ratio[r] * A)))
+        dl[r] = w * ((0.0 if clipped else -ratio[r] * A) - beta_rise)
     if ref_logprob is None:
         kl[:] = 0.0
     return {"loss": math.fsum(terms) if not any(map(math.isnan, terms)) else math.nan, "logprob": l, "ratio": ratio,

@@ -18,9 +18,9 @@
 // S = sum 2^x_v, softmax(u)_v = 2^x_v / S. A row's sums over the vocabulary
 // are float32 per lane (at most a few hundred terms each, all positive). What
 // follows per row (l, the loss's term, the coefficient) and the sums over rows
-// are in 64 bits; the ratio and 1 - p_y are float32 exponentials of 64-bit
-// arguments, one rounding each (in 64 bits they took registers that hold the
-// row). A gradient element is rounded to its type once.
+// are in 64 bits; the ratio and 1 - p_y have the precision of float32
+// exponentials of 64-bit arguments (in 64 bits they took registers that hold
+// the row). A gradient element is rounded to its type once.
 #include "loss.h"
 #include "row_scan.h"
 
@@ -152,6 +152,13 @@ __device__ __forceinline__ float token_logit(const LossRows& a, int64_t r, int32
   return y >= 0 && y < a.V ? Elem<Tin>::load1(row_ptr<Tin>(a, r), y) : 0.0f;
 }
 
+// exp(x) with the range of 64 bits and the precision of 32, so that a ratio
+// beyond float32 times an advantage of 0 is 0.
+__device__ __forceinline__ double exp_wide(double x) {
+  const double t = x * 1.4426950408889634, k = fmin(fmax(rint(t), -2000.0), 2000.0);
+  return ldexp(static_cast<double>(exp2f(static_cast<float>(t - k))), static_cast<int>(k));
+}
+
 // What the policy loss makes of a row.
 struct PolicyRow {
   double term;  // of the loss
@@ -162,7 +169,7 @@ struct PolicyRow {
 
 __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, int64_t r, const RowValue& v, float T, float c,
                                                 float S, float w) {
-  const double A = a.advantage[r], ratio = expf(static_cast<float>(v.l - static_cast<double>(a.old_logprob[r])));
+  const double A = a.advantage[r], ratio = exp_wide(v.l - static_cast<double>(a.old_logprob[r]));
   const double free = ratio * A, held = fmin(fmax(ratio, a.clip_lo), a.clip_hi) * A;
   const bool clipped = free > held;
   double kl = 0.0, rise = 0.0;
@@ -171,10 +178,11 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, int64_t r, 
     rise = expm1(d);
     kl = d == INFINITY ? d : rise - d;  // a token of probability 0
   }
+  const bool with_kl = a.kl_coef > 0.0;  // without, an infinite KL stands beside the loss alone
   const double gain = v.flags ? v.l : (clipped ? held : free);
-  const double dl = static_cast<double>(w) * ((clipped ? 0.0 : -free) - (a.ref_logprob ? a.kl_coef * rise : 0.0));
+  const double dl = static_cast<double>(w) * ((clipped ? 0.0 : -free) - (with_kl ? a.kl_coef * rise : 0.0));
   PolicyRow p;
-  p.term = static_cast<double>(w) * ((a.ref_logprob ? a.kl_coef * kl : 0.0) - gain);
+  p.term = static_cast<double>(w) * ((with_kl ? a.kl_coef * kl : 0.0) - gain);
   p.logprob = static_cast<float>(v.l);
   p.ratio = static_cast<float>(ratio);
   p.kl = static_cast<float>(kl);

@@ -363,6 +363,44 @@ def test_policy_probability_zero():
     assert float(got["kl"]) == math.inf and float(got["loss"]) == math.inf
 
 
+def test_policy_kl_beside_a_loss_without_it():
+    """kl_coef = 0 with a reference: the KL is an output alone, infinite at a token of probability 0, and loss and
+    gradient do without it."""
+    logits = torch.randn(3, 300, device="cuda")
+    logits[1, 7] = -math.inf
+    one = torch.ones(3, device="cuda")
+    ids = torch.full((3,), 7, dtype=torch.int32, device="cuda")
+    plain = pr.policy_loss(logits, ids, one, one, one, -one)
+    got = pr.policy_loss(logits, ids, one, one, one, -one, -one)
+    assert float(got["kl"][1]) == math.inf and math.isfinite(float(got["loss"]))
+    for k in ("loss", "grad", "ratio", "flags"):
+        assert torch.equal(got[k], plain[k]), k
+    assert bool((got["grad"][1] == 0).all())
+
+
+@pytest.mark.parametrize("V", [64, 40000])
+def test_policy_ratio_beyond_float32(V):
+    """A ratio of e^100: clipped at a positive advantage, worth nothing at an advantage of 0, and finite again under a
+    weight that brings it back into range."""
+    n = 200
+    logits = torch.zeros(n, V, device="cuda")
+    l = -math.log(V)
+    A = torch.tensor([1.0, 0.0, -1.0, 0.0], device="cuda").repeat(n // 4)
+    w = torch.tensor([1.0, 1.0, 1e-30, 0.5], device="cuda").repeat(n // 4)
+    old = torch.full((n,), l - 100.0, device="cuda")
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")
+    got = pr.policy_loss(logits, ids, 1.0, w, A, old)
+    x = l - float(old[0])  # with old's rounding
+    push = float(w[2]) * math.exp(x)
+    assert bool((got["ratio"] == math.inf).all())
+    # the exponent's argument is off by L_ABS, the exponential by two roundings of float32
+    near("loss", got["loss"].cpu(), [n // 4 * (push - 1.2)], 0.0, L_ABS + 2.0 ** -21)
+    want = torch.zeros(n, V, dtype=torch.float64)
+    want[2::4] = -push / V
+    want[2::4, 0] = push * (1 - 1 / V)
+    near("grad", got["grad"].cpu(), want, push * 2.0 ** -21, L_ABS + 2.0 ** -21)
+
+
 def test_policy_all_masked_and_empty():
     logits = torch.full((5, 300), math.nan, device="cuda")
     z = torch.zeros(5, device="cuda")

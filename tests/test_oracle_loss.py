@@ -109,3 +109,15 @@ def test_undefined_rows():
     assert math.isnan(o["loss"]) and np.isnan(o["grad"][:2]).all() and np.isfinite(o["grad"][2]).all()
     o = oloss.policy_loss(z, "f32", [0, 9, 1], [1.0, 1.0, 1.0], [0.0, 0.0, 1.0], [1.0] * 3, [-1.0] * 3)
     assert math.isfinite(o["loss"]) and (o["grad"][:2] == 0).all()
+
+
+def test_no_kl_term_without_a_coefficient():
+    """kl_coef = 0: loss and gradient are those without a reference, also at a token of probability 0."""
+    z = np.zeros((2, 5), np.float32)
+    z[1, 2] = -np.inf
+    ids, T, w, A, old = [2, 2], np.ones(2, np.float32), np.ones(2), np.ones(2), np.full(2, -1.0)
+    plain = oloss.policy_loss(z, "f32", ids, T, w, A, old)
+    o = oloss.policy_loss(z, "f32", ids, T, w, A, old, np.full(2, -1.0))
+    assert o["kl"][1] == math.inf and o["kl"][0] > 0
+    assert o["loss"] == plain["loss"] and np.array_equal(o["grad"], plain["grad"])
+    assert math.isinf(oloss.policy_loss(z, "f32", ids, T, w, A, old, np.full(2, -1.0), kl_coef=0.1)["loss"])
