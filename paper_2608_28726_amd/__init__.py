@@ -626,12 +626,20 @@ class AdamW:
     rounding.
 
     The tensors given and made here are kept, not copied: a step changes them
-    in place, and they must stay where they are.
+    in place, and they must stay where they are. No two may overlap.
+
+    The device's plan of the tensors is made at construction, or, for want of
+    ``grads``, by the first :meth:`step` or :meth:`moments` and again by a
+    first step whose gradients are not of the parameters' type: such a call
+    allocates and waits for the device, so it cannot be captured into a graph.
+    After :meth:`close` there are no more steps.
     """
 
     def __init__(self, params, grads=None, copies=None, state_bits: int = 32, states=None, seed: int = 0,
                  steps: int = 0):
         self._h = C.c_void_p()
+        self._closed = False
+        self._plan_dtype = None  # of the gradients that the plan takes
         self.params = list(params)
         if not self.params:
             raise ValueError("params must hold at least one tensor")
@@ -666,7 +674,7 @@ class AdamW:
                 self._check(s[name], f"states' {name}", kind, size)
         self._seed = int(seed) & 0xFFFFFFFFFFFFFFFF
         if self._grad_dtype is not None:
-            self._create()
+            self._plan(self._grad_dtype)
 
     def _check(self, t, what, dtype, size):
         if t.dtype != dtype or t.device != self.device or not t.is_contiguous() or (size is not None and t.numel() != size):
@@ -698,8 +706,11 @@ class AdamW:
             sizes.update(m_exp=blocks, v_exp=blocks)
         return {k: torch.zeros(size, dtype=kind, device=self.device) for k, size in sizes.items()}
 
-    def _create(self):
-        self.close()
+    def _plan(self, grad_dtype):
+        """Makes the device's plan for gradients of this type, unless it is there."""
+        if self._h and self._plan_dtype == grad_dtype:
+            return
+        self._destroy()
         T = (_abi.AdamWTensor * len(self.params))()
         for i, (t, p, s) in enumerate(zip(T, self.params, self.states)):
             t.param, t.n = p.data_ptr(), p.numel()
@@ -709,21 +720,27 @@ class AdamW:
             if self.state_bits == 8:
                 t.m_exp, t.v_exp = s["m_exp"].data_ptr(), s["v_exp"].data_ptr()
         code = {torch.float32: _abi.PR_F32, torch.bfloat16: _abi.PR_BF16}
-        st = _abi.lib().pr_adamw_create(T, len(T), code[self._dtype], code[self._grad_dtype], self.state_bits,
+        st = _abi.lib().pr_adamw_create(T, len(T), code[self._dtype], code[grad_dtype], self.state_bits,
                                         self._seed, C.byref(self._h))
         _abi.check("pr_adamw_create", st)
+        self._plan_dtype = grad_dtype
+
+    def _check_open(self):
+        if self._closed:
+            raise ValueError("the optimizer is closed")
 
     def step(self, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
              grad_scale: float = 1.0, grads=None) -> None:
         """One step (``pr_adamw_step``) with the gradients given here or at construction; a None among those given
         here leaves its tensor as it is."""
+        self._check_open()
         pointers = None
         if grads is not None:
             grads = self._list(grads, "step's grads", None)
             dtype = next(t.dtype for t in grads if t is not None)
             if self._grad_dtype is None:
+                self._plan(dtype)
                 self._grad_dtype = dtype
-                self._create()
             elif dtype != self._grad_dtype:
                 raise ValueError(f"step's grads must be {self._grad_dtype} tensors")
             pointers = (C.c_void_p * len(grads))(*[None if t is None else t.data_ptr() for t in grads])
@@ -744,12 +761,11 @@ class AdamW:
         elements, which receive the values and are returned instead; tensor j
         starts at 256 times the blocks of the tensors before it, and entries
         between tensors are left as they are."""
+        self._check_open()
         if self.state_bits == 32:
             return tuple([s[k].view(p.shape) for s, p in zip(self.states, self.params)] for k in ("m", "v"))
-        if not self._h:
-            self._grad_dtype = self._dtype  # nothing is stepped yet: any type of gradient will do
-            self._create()
-            self._grad_dtype = None
+        # Before a first step any type of gradient will do.
+        self._plan(self._grad_dtype or self._dtype)
         total = _abi.PR_ADAMW_BLOCK * sum(self._blocks)
         given = out is not None
         if not given:
@@ -768,10 +784,14 @@ class AdamW:
             at += _abi.PR_ADAMW_BLOCK * blocks
         return lists
 
-    def close(self) -> None:
+    def _destroy(self):
         if self._h:
             _abi.lib().pr_adamw_destroy(self._h)
             self._h = C.c_void_p()
+
+    def close(self) -> None:
+        self._closed = True
+        self._destroy()
 
     def __del__(self):
         try:

@@ -276,3 +276,51 @@ def test_refusals():
     eight = pr.AdamW([p], state_bits=8)
     with pytest.raises(ValueError):
         eight.moments(out=(torch.zeros(512, dtype=torch.bfloat16, device="cuda"), torch.zeros(300, device="cuda")))
+
+
+def test_closed_and_replanned():
+    """A closed optimizer takes no step and no moments (a plan made anew for moments once took the gradients' buffers
+    for the parameters' type). Moments before the first step leave later steps as they are."""
+    n = 3001
+    for bits in (8, 32):
+        p, g = torch.ones(n, device="cuda"), torch.ones(n, dtype=torch.bfloat16, device="cuda")
+        opt = pr.AdamW([p], grads=[g], state_bits=bits)
+        opt.step(lr=0.125)
+        opt.close()
+        opt.close()
+        for call in (opt.moments, lambda: opt.step(lr=0.125), lambda: opt.step(lr=0.125, grads=[g.float()])):
+            with pytest.raises(ValueError):
+                call()
+        assert opt.steps == 1
+    for grad_dtype in (torch.float32, torch.bfloat16):
+        runs = []
+        for first in (False, True):
+            p, g = torch.ones(n, device="cuda"), torch.linspace(-1, 1, n, device="cuda").to(grad_dtype)
+            opt = pr.AdamW([p], state_bits=8, seed=4)
+            if first:
+                m, v = opt.moments()
+                assert bool((m[0] == 0).all()) and bool((v[0] == 0).all())
+            for _ in range(2):
+                opt.step(lr=0.125, grads=[g])
+                opt.moments()
+            torch.cuda.synchronize()
+            runs.append([p, *opt.states[0].values()])
+        for a, b in zip(*runs):
+            assert torch.equal(a, b)
+
+
+def test_first_step_captured_after_moments():
+    """A plan that moments() made serves a first step with gradients of the parameters' type, also in a graph."""
+    n = 3001
+    p, g = torch.ones(n, device="cuda"), torch.linspace(-1, 1, n, device="cuda")
+    other = p.clone()
+    opt, eager = pr.AdamW([p], state_bits=8), pr.AdamW([other], state_bits=8)
+    opt.moments()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step(lr=0.125, grads=[g])
+    graph.replay()
+    eager.step(lr=0.125, grads=[g])
+    torch.cuda.synchronize()
+    assert torch.equal(p, other)
