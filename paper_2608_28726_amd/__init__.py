@@ -734,6 +734,7 @@ class AdamW:
         """One step (``pr_adamw_step``) with the gradients given here or at construction; a None among those given
         here leaves its tensor as it is."""
         self._check_open()
+        stream = _check_current(self.device, "the optimizer's tensors")
         pointers = None
         if grads is not None:
             grads = self._list(grads, "step's grads", None)
@@ -746,7 +747,6 @@ class AdamW:
             pointers = (C.c_void_p * len(grads))(*[None if t is None else t.data_ptr() for t in grads])
         elif self.grads is None:
             raise ValueError("step needs grads: none were given at construction")
-        stream = _check_current(self.device, "the optimizer's tensors")
         p = _abi.AdamWParams(float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), float(grad_scale),
                              self.steps + 1)
         _abi.check("pr_adamw_step", _abi.lib().pr_adamw_step(self._h, pointers, C.byref(p), stream))
@@ -764,6 +764,7 @@ class AdamW:
         self._check_open()
         if self.state_bits == 32:
             return tuple([s[k].view(p.shape) for s, p in zip(self.states, self.params)] for k in ("m", "v"))
+        stream = _check_current(self.device, "the optimizer's tensors")
         # Before a first step any type of gradient will do.
         self._plan(self._grad_dtype or self._dtype)
         total = _abi.PR_ADAMW_BLOCK * sum(self._blocks)
@@ -772,7 +773,6 @@ class AdamW:
             out = tuple(torch.zeros(total, dtype=torch.bfloat16, device=self.device) for _ in range(2))
         for t in out:
             self._check(t, "out", torch.bfloat16, total)
-        stream = _check_current(self.device, "the optimizer's tensors")
         _abi.check("pr_adamw_moments", _abi.lib().pr_adamw_moments(self._h, _ptr(out[0]), _ptr(out[1]), stream))
         if given:
             return out

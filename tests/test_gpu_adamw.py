@@ -15,6 +15,7 @@ import torch
 
 import paper_2608_28726_amd as pr
 from oracle import adamw as oadam
+from paper_2608_28726_amd import _abi
 from tests.gpu_common import require_gpu
 
 pytestmark = pytest.mark.gpu
@@ -324,3 +325,20 @@ def test_first_step_captured_after_moments():
     eager.step(lr=0.125, grads=[g])
     torch.cuda.synchronize()
     assert torch.equal(p, other)
+
+
+def test_no_plan_on_another_device(monkeypatch):
+    """With another device current, calls are refused before they make a plan, which would lie on that device."""
+    p, g = torch.ones(300, device="cuda"), torch.ones(300, device="cuda")
+    opt = pr.AdamW([p], state_bits=8)
+    made = []
+    create = _abi.lib().pr_adamw_create
+    with monkeypatch.context() as patch:
+        patch.setattr(torch.cuda, "current_device", lambda: p.device.index + 1)
+        patch.setattr(_abi.lib(), "pr_adamw_create", lambda *a: made.append(a) or create(*a))
+        for call in (opt.moments, lambda: opt.step(lr=0.125, grads=[g])):
+            with pytest.raises(ValueError):
+                call()
+    assert not made and opt.steps == 0
+    opt.step(lr=0.125, weight_decay=0.0, grads=[g])
+    assert abs(float(p[0]) - 0.875) < 1e-6
