@@ -626,7 +626,8 @@ class AdamW:
     rounding.
 
     The tensors given and made here are kept, not copied: a step changes them
-    in place, and they must stay where they are. No two may overlap.
+    in place, and they must stay where they are (one given another storage
+    afterwards is stepped where it was). No two may overlap.
 
     The device's plan of the tensors is made at construction, or, for want of
     ``grads``, by the first :meth:`step` or :meth:`moments` and again by a
@@ -667,11 +668,17 @@ class AdamW:
         if len(self.states) != n:
             raise ValueError(f"states must have {n} entries")
         kind = torch.float32 if state_bits == 32 else torch.uint8
+        names = ("m", "v", "m_exp", "v_exp")[:2 if state_bits == 32 else 4]
         for s, k, b in zip(self.states, self._sizes, blocks):
-            for name, size in (("m", k), ("v", k)) + ((("m_exp", b), ("v_exp", b)) if state_bits == 8 else ()):
+            for name, size in zip(names, (k, k, b, b)):
                 if name not in s:
                     raise ValueError(f"a state of {state_bits} bits needs '{name}'")
                 self._check(s[name], f"states' {name}", kind, size)
+        # What was checked, as tensors of its own: the plan's addresses stay allocated and of the checked sizes when one
+        # of the caller's is given another storage.
+        alias = lambda tensors: None if tensors is None else [t.detach() for t in tensors]  # noqa: E731
+        self._planned = (alias(self.params), alias(self.grads), alias(self.copies),
+                         [{k: s[k].detach() for k in names} for s in self.states])
         self._seed = int(seed) & 0xFFFFFFFFFFFFFFFF
         if self._grad_dtype is not None:
             self._plan(self._grad_dtype)
@@ -686,8 +693,8 @@ class AdamW:
         if tensors is None:
             return None
         tensors = list(tensors)
-        if len(tensors) != len(self.params):
-            raise ValueError(f"{what} must have {len(self.params)} entries")
+        if len(tensors) != len(self._sizes):
+            raise ValueError(f"{what} must have {len(self._sizes)} entries")
         if dtype is None:
             dtype = next((t.dtype for t in tensors if t is not None), None)
             if dtype not in (torch.float32, torch.bfloat16):
@@ -711,11 +718,12 @@ class AdamW:
         if self._h and self._plan_dtype == grad_dtype:
             return
         self._destroy()
-        T = (_abi.AdamWTensor * len(self.params))()
-        for i, (t, p, s) in enumerate(zip(T, self.params, self.states)):
+        params, grads, copies, states = self._planned
+        T = (_abi.AdamWTensor * len(params))()
+        for i, (t, p, s) in enumerate(zip(T, params, states)):
             t.param, t.n = p.data_ptr(), p.numel()
-            t.grad = self.grads[i].data_ptr() if self.grads else None
-            t.copy = self.copies[i].data_ptr() if self.copies else None
+            t.grad = grads[i].data_ptr() if grads else None
+            t.copy = copies[i].data_ptr() if copies else None
             t.m, t.v = s["m"].data_ptr(), s["v"].data_ptr()
             if self.state_bits == 8:
                 t.m_exp, t.v_exp = s["m_exp"].data_ptr(), s["v_exp"].data_ptr()

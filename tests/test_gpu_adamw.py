@@ -342,3 +342,30 @@ def test_no_plan_on_another_device(monkeypatch):
     assert not made and opt.steps == 0
     opt.step(lr=0.125, weight_decay=0.0, grads=[g])
     assert abs(float(p[0]) - 0.875) < 1e-6
+
+
+
+
+def test_replaced_storages():
+    """What a step writes to stays allocated, and is what was checked, when a parameter, gradient or state is given
+    another storage afterwards."""
+    n = 1 << 20
+    big = [torch.ones(n, device="cuda") for _ in range(2)]
+    wide = torch.full((2 * n,), 3.0, device="cuda")
+    for bound in (True, False):
+        p, g = big[0].clone(), big[1].clone()
+        opt = pr.AdamW([p], grads=[g] if bound else None, copies=[p.bfloat16()])
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        kept, p.data = p.detach(), wide
+        opt.states[0]["v"] = None
+        opt.copies[0] = None
+        if bound:
+            g.data = torch.zeros(2, device="cuda")
+        assert torch.cuda.memory_allocated() >= before
+        # the step goes to what was given, and to nothing else
+        del opt.params[:]
+        opt.step(lr=0.125, weight_decay=0.0, grads=None if bound else [g])
+        torch.cuda.synchronize()
+        assert bool(((kept - 0.875).abs() < 1e-6).all()) and bool((wide == 3.0).all())
+        del kept, opt
