@@ -601,10 +601,11 @@ typedef struct pr_adamw pr_adamw;
  * when a step is given its gradients). For each element, with
  * g = grad_scale grad:
  *   m' = beta1 m + (1 - beta1) g,  v' = beta2 v + (1 - beta2) g g
- *   p' = p (1 - lr weight_decay) - lr c1 m' / (c2 sqrt(v') + eps),
+ *   p' = p - (lr weight_decay p + lr c1 m' / (c2 sqrt(v') + eps)),
  *   c1 = 1 / (1 - beta1^step),  c2 = 1 / sqrt(1 - beta2^step)
- * in float32. bfloat16 parameters are rounded stochastically, so that
- * steps below half their spacing still count on average.
+ * in float32. bfloat16 parameters are rounded stochastically from that, so
+ * that steps below half their spacing still count on average, down to half of
+ * float32's (2^-25 to 2^-24 of p).
  *
  * 8-bit states: the elements i / 256 of a tensor share an exponent byte E.
  * The code of m is a sign bit and k (7 bits: 4 of exponent, 3 of mantissa),

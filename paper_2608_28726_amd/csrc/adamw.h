@@ -28,7 +28,8 @@ struct AdamChunk {
 
 struct AdamScalars {
   float beta1, one_minus_beta1, beta2, one_minus_beta2;
-  float decay;       // 1 - lr weight_decay
+  float decay;       // lr weight_decay
+  float keep;        // 1 - lr weight_decay
   float rate;        // lr c1
   float c2, eps;
   float grad_scale;

@@ -741,7 +741,8 @@ pr_status pr_adamw_step(pr_adamw* handle, const void* const* grads, const pr_ada
   s.one_minus_beta1 = static_cast<float>(1.0 - p.beta1);
   s.beta2 = static_cast<float>(p.beta2);
   s.one_minus_beta2 = static_cast<float>(1.0 - p.beta2);
-  s.decay = static_cast<float>(1.0 - p.lr * p.weight_decay);
+  s.decay = static_cast<float>(p.lr * p.weight_decay);
+  s.keep = static_cast<float>(1.0 - p.lr * p.weight_decay);
   s.rate = static_cast<float>(p.lr / (1.0 - std::pow(p.beta1, static_cast<double>(p.step))));
   s.c2 = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(p.beta2, static_cast<double>(p.step))));
   s.eps = static_cast<float>(p.eps);

@@ -369,3 +369,54 @@ def test_replaced_storages():
         torch.cuda.synchronize()
         assert bool(((kept - 0.875).abs() < 1e-6).all()) and bool((wide == 3.0).all())
         del kept, opt
+
+
+def decay_case(n, dtype, seed):
+    """Parameters of size about 1 with states that move each by an update of its own, 1e-6 wide: many times the
+    spacing of float32, so that roundings to nearest average out."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    p = (torch.rand(n, generator=g, device="cuda") + 0.5).to(dtype)
+    m = torch.empty(n, device="cuda").normal_(generator=g)
+    v = torch.ones(n, device="cuda")
+    grad = torch.empty(n, device="cuda").normal_(generator=g)
+    return p, grad, m, v
+
+
+@pytest.mark.parametrize("weight_decay", [0.01, 0.1, 0.2])
+@pytest.mark.parametrize("eps", [1e-8, 0.0])
+def test_weight_decay_at_small_rates(weight_decay, eps):
+    """lr weight_decay far below float32's spacing at 1: on average every parameter decays by it. A rounding moves
+    p'/p by 2^-24 at most, 3.5e-8 in the mean square; the mean of 2^20 of them is within 5 x 3.5e-8 / 2^10 of 0."""
+    n, o = 1 << 20, dict(lr=1e-6, beta1=0.9, beta2=0.999, eps=eps, weight_decay=weight_decay)
+    p, grad, m, v = decay_case(n, torch.float32, 31)
+    before = [host(x) for x in (p, grad, m, v)]
+    pr.AdamW([p], grads=[grad], states=[dict(m=m, v=v)], steps=500).step(**o)
+    torch.cuda.synchronize()
+    want, _, _ = oadam.adamw(*before, 501, **o)
+    off = float(np.mean((host(p).astype(np.float64) - want) / before[0]))
+    assert abs(off) <= 5 * 3.5e-8 / 2 ** 10, (off, o["lr"] * weight_decay)
+
+
+def test_weight_decay_of_bfloat16_parameters_at_small_rates():
+    """The float32 step that a bfloat16 parameter is rounded from holds the decay: with the documented random bits the
+    stochastic rounding gives the same 16 bits. The update is off by about 4e-7 of 1e-6, so the float32 step differs
+    from the float64 one's nearest in 1 of 10^5 elements, and its rounding in 1 of 2^16 of those: none of 2^24."""
+    n, o = 1 << 24, dict(lr=1e-6, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01)
+    p, grad, m, v = decay_case(n, torch.bfloat16, 32)
+    before = [host(x) for x in (p, grad, m, v)]
+    pr.AdamW([p], grads=[grad], states=[dict(m=m, v=v)], steps=500, seed=6).step(**o)
+    torch.cuda.synchronize()
+    want, _, _ = oadam.adamw(*before, 501, **o)
+    bits = want.astype(np.float32).view(np.uint32) + (oadam.random_bits(n, 0, 6, 501) & np.uint64(0xFFFF)).astype(np.uint32)
+    off = int((p.view(torch.int16).cpu().numpy().view(np.uint16) != (bits >> np.uint32(16)).astype(np.uint16)).sum())
+    assert off <= 1, off
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("weight_decay", [0.0, 0.1])
+def test_infinite_parameters_stay(dtype, weight_decay):
+    p = torch.tensor([math.inf, -math.inf, 1.0, math.nan], device="cuda").to(dtype)
+    pr.AdamW([p], grads=[torch.full((4,), 0.5, device="cuda")]).step(lr=2.0 ** -6, weight_decay=weight_decay)
+    torch.cuda.synchronize()
+    assert p[:2].tolist() == [math.inf, -math.inf] and 0.97 < float(p[2]) < 1.0 and math.isnan(float(p[3]))
