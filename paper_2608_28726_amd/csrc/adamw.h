@@ -34,7 +34,7 @@ struct AdamScalars {
   float c2, eps;
   float grad_scale;
   uint32_t key;      // of the step's random numbers
-  int32_t tiny_eps;  // eps does not dwarf the roots of values that the fast square root takes for 0
+  int32_t tiny_eps;  // eps does not dwarf c2 times the roots of values that the fast square root takes for 0
 };
 
 struct AdamPlan {

@@ -747,7 +747,8 @@ pr_status pr_adamw_step(pr_adamw* handle, const void* const* grads, const pr_ada
   s.c2 = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(p.beta2, static_cast<double>(p.step))));
   s.eps = static_cast<float>(p.eps);
   s.grad_scale = static_cast<float>(p.grad_scale);
-  s.tiny_eps = p.eps < 1e-12;
+  // Roots of values below 2^-126 are below 1.1e-19: times c2 a part in 10^7 of such an eps.
+  s.tiny_eps = p.eps < 1e-12 * static_cast<double>(s.c2);
   s.key = step_key(handle->seed, p.step);
   const int32_t n = static_cast<int32_t>(handle->chunk_begin.size()) - 1;
   if (!grads)

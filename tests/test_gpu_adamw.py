@@ -420,3 +420,15 @@ def test_infinite_parameters_stay(dtype, weight_decay):
     pr.AdamW([p], grads=[torch.full((4,), 0.5, device="cuda")]).step(lr=2.0 ** -6, weight_decay=weight_decay)
     torch.cuda.synchronize()
     assert p[:2].tolist() == [math.inf, -math.inf] and 0.97 < float(p[2]) < 1.0 and math.isnan(float(p[3]))
+
+
+def test_small_eps_beside_a_large_correction():
+    """eps = 1e-12 with beta2 so near 1 that c2 sqrt(v) counts beside it for v below 2^-126."""
+    o = dict(lr=1.0, beta1=0.9, beta2=1 - 2.0 ** -40, eps=1e-12, weight_decay=0.0)
+    z = np.zeros(5, np.float32)
+    m = np.array([1e-12, -3e-12, 2e-12, 1e-13, 0.0], np.float32)
+    v = np.array([1e-38, 5e-39, 1.1e-38, 2e-39, 1e-38], np.float32)
+    p, grad = torch.zeros(5, device="cuda"), torch.zeros(5, device="cuda")
+    pr.AdamW([p], grads=[grad], states=[dict(m=torch.tensor(m, device="cuda"), v=torch.tensor(v, device="cuda"))]).step(**o)
+    torch.cuda.synchronize()
+    check_param(host(p), z, z, m, v, 1, o, 1.0)
