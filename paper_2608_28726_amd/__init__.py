@@ -765,12 +765,14 @@ class AdamW:
 
         32-bit states are returned themselves. 8-bit ones are decoded
         (``pr_adamw_moments``) to bfloat16, which holds them exactly.
-        ``out``: two bfloat16 buffers of 256 entries per block of 256
-        elements, which receive the values and are returned instead; tensor j
+        ``out`` (8-bit states): two bfloat16 buffers of 256 entries per block
+        of 256 elements, which receive the values and are returned instead; tensor j
         starts at 256 times the blocks of the tensors before it, and entries
         between tensors are left as they are."""
         self._check_open()
         if self.state_bits == 32:
+            if out is not None:
+                raise ValueError("out is for 8-bit states: 32-bit ones are returned themselves")
             return tuple([s[k].view(p.shape) for s, p in zip(self.states, self.params)] for k in ("m", "v"))
         stream = _check_current(self.device, "the optimizer's tensors")
         # Before a first step any type of gradient will do.

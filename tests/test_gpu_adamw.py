@@ -432,3 +432,13 @@ def test_small_eps_beside_a_large_correction():
     pr.AdamW([p], grads=[grad], states=[dict(m=torch.tensor(m, device="cuda"), v=torch.tensor(v, device="cuda"))]).step(**o)
     torch.cuda.synchronize()
     check_param(host(p), z, z, m, v, 1, o, 1.0)
+
+
+def test_moments_of_32_bit_states_take_no_buffers():
+    """32-bit states are returned themselves: buffers that would be left as they are get refused."""
+    p = torch.zeros(300, device="cuda")
+    opt = pr.AdamW([p])
+    out = tuple(torch.zeros(512, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    with pytest.raises(ValueError):
+        opt.moments(out=out)
+    assert opt.moments()[0][0].data_ptr() == opt.states[0]["m"].data_ptr()
