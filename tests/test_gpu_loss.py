@@ -688,3 +688,26 @@ def test_refusals():
     for opts in (dict(beta=0.0), dict(beta=math.nan), dict(label_smoothing=1.1), dict(margin=math.inf)):
         with pytest.raises(pr.ProuterError):
             pr.preference_loss(z, ids, 1.0, f, off, **opts)
+
+
+@pytest.mark.parametrize("n,V", [(1024, 1 << 22), (1, 1 << 26)])
+def test_policy_long_rows(n, V):
+    """Rows so long that a lane adds thousands of terms: the log-prob keeps the precision of the module docstring.
+    All tokens but one share a logit, so that roundings do not average out."""
+    logits = torch.empty(n, V, device="cuda")
+    one = torch.ones(n, device="cuda")
+    w = torch.zeros(n, device="cuda")
+    w[0] = w[n - 1] = 1.0
+    for z in (-0.3, -0.9, -1.1):
+        for r in {0, n - 1}:
+            logits[r] = z
+            logits[r, 5] = 0.0
+        ids = torch.full((n,), 5, dtype=torch.int32, device="cuda")
+        want = -math.log1p((V - 1) * math.exp(float(np.float32(z))))
+        for T, scale in ((1.0, 1.0), (0.5, 2.0)):
+            l = want if T == 1.0 else -math.log1p((V - 1) * math.exp(2 * float(np.float32(z))))
+            got = pr.policy_loss(logits, ids, T, w, one, one * l, grad=False)
+            off = pr.preference_loss(logits, ids, T, w, torch.tensor([0, 0, n], dtype=torch.int32, device="cuda"),
+                                     grad=False)
+            for x in (got, off):
+                near("logprob", x["logprob"][w != 0].cpu(), np.full(int(w.sum()), l), L_ABS, 2.0 ** -24)
