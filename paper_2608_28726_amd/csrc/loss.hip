@@ -501,10 +501,18 @@ struct RowView {
 // Vectors of the rows that policy_row_kernel holds, by its two sizes (two and
 // one workgroups a compute unit). Shorter rows than the least take two passes:
 // what a workgroup spends on a row beside its vectors then costs more than the
-// second read. 1.2 GB of bfloat16 rows, held and in two passes: 16,384 logits a
-// row 684 and 608 us, 32,000 578 and 576, 50,257 510 and 593, 151,936 483 and
-// 569.
-constexpr int64_t kLeastRowVectors = 4500, kSmallRowVectors = 19 * 7 * kWave, kRowVectors = 20 * 15 * kWave;
+// second read. 1.2 GB of rows that all count, held and in two passes (us, in
+// brackets the row's vectors): bfloat16 16,384 logits a row (2,048) 710 and
+// 615, 24,000 (3,000) 593 and 580, 32,000 (4,000) 535 and 575, 50,257 510 and
+// 596, 65,536 475 and 569, 70,000 (8,750, the larger size) 496 and 588, 100,000
+// 487 and 570, 151,936 484 and 574; float32 8,192 (2,048) 669 and 601, 12,000
+// (3,000) 566 and 571, 16,000 (4,000) 521 and 580, 32,000 484 and 565, 40,000
+// (10,000, the larger size) 464 and 585. Fewer rows of 32,000 bfloat16 logits:
+// 128 rows 11.7 and 13.6, 512 18.4 and 23.9, 1,000 31 and 39. Batches that the
+// last-level cache keeps between two passes are the exception, and only long
+// rows among them: of 151,936 bfloat16 logits 300 rows 62 and 54, 512 79.6 and
+// 79.8, 1,024 143 and 155.
+constexpr int64_t kLeastRowVectors = 3500, kSmallRowVectors = 19 * 7 * kWave, kRowVectors = 20 * 15 * kWave;
 bool held_row(int64_t nvec) { return nvec >= kLeastRowVectors && nvec <= kRowVectors; }
 
 // Most rows whose order policy_row_kernel works out for itself.
@@ -762,8 +770,11 @@ __global__ __launch_bounds__(kStatsBlock) void preference_stats_kernel(Preferenc
     preference_row(a, r, p, T, c, y, zy, l, rg);
 }
 
-// Most pairs whose mean one wave takes while the gradient is written.
-constexpr int32_t kPairsBeside = 4096;
+// Most pairs whose mean one wave takes while the gradient is written. Beside it
+// and in a launch of its own, two rows of 2,000 bfloat16 logits a pair: 32 pairs
+// 10.7 and 12.5 us, 256 11.9 and 13.8, 512 15.7 and 16.4, 1,000 23.3 and 22.2,
+// 4,096 67.9 and 57.5.
+constexpr int32_t kPairsBeside = 512;
 
 // One workgroup per pair: the sums over both requests, the pair's loss, and
 // the gradient's factors of the pair's rows. Rows that were split finish here.
@@ -837,24 +848,33 @@ __global__ __launch_bounds__(kPairBlock) void preference_pair_kernel(PreferenceA
   }
 }
 
-// Below this many rows a row may be spread over workgroups.
-constexpr int64_t kSplitRows = 1024;
+// Below this many rows a row may be spread over workgroups. Spread and whole,
+// preference loss: 64 rows of 50,257 bfloat16 logits 14.4 and 17.1 us, of
+// 151,936 float32 logits 30.5 and 41.0; 128 rows 17.5 and 19.6, 47.2 and 53.7;
+// 200 rows 23.1 and 22.3, 66.8 and 68.5; 256 rows 25.1 and 24.7, 83.1 and 80.5;
+// 400 rows 32.7 and 31.2, 126 and 124.
+constexpr int64_t kSplitRows = 256;
 
-// Workgroups along a row for its sums: about 2,048 in all, each with at least
-// 1,024 vectors.
+// Workgroups along a row for its sums: about 1,024 in all, each with at least
+// 512 vectors. Preference loss, about 512, 1,024 and 2,048 in all: 128 rows of
+// 151,936 bfloat16 logits 29.3, 30.8 and 33.1 us, 200 rows of as many float32
+// logits 68.6, 66.5 and 67.9, 60 rows of 50,257 bfloat16 logits 13.8, 13.7 and
+// 13.6. At least 256, 512 and 1,024 vectors: 17 rows of 50,257 11.7, 11.4 and
+// 12.1 us, 60 rows 14.7, 13.7 and 15.0, 2 rows of 32,000 10.5, 10.2 and 10.5.
 int row_parts(int64_t n_rows, int32_t V, pr_dtype dtype) {
   if (n_rows <= 0 || n_rows >= kSplitRows) return 1;
   const int64_t nvec = V / (dtype == PR_BF16 ? 8 : 4);
-  const int64_t want = (2048 + n_rows - 1) / n_rows, most = nvec / 1024;
+  const int64_t want = (1024 + n_rows - 1) / n_rows, most = nvec / 512;
   const int64_t G = want < most ? want : most;
   return static_cast<int>(G < 1 ? 1 : G > kMaxSplit ? kMaxSplit : G);
 }
 
 // Few rows whose gradient is wanted are spread over the device although they
 // fit a workgroup: one compute unit alone takes 20 us for 304 KB. Captured
-// calls, spread and not: 16 rows of 151,936 bfloat16 logits 12.2 and 22.5 us,
-// 64 rows 19.9 and 25.1, 96 rows 26.7 and 25.8; 16 rows of 32,000 float32
-// logits 9.5 and 10.1, 32 rows 11.9 and 10.3.
+// calls, spread and held: 16 rows of 151,936 bfloat16 logits 11.7 and 21.6 us,
+// 64 rows 19.5 and 24.2, 96 rows 24.5 and 24.9, 128 rows 29.3 and 25.7, of 40,000
+// float32 logits 32 rows 11.0 and 12.3, 64 rows 14.2 and 13.5; 16 rows of 32,000
+// float32 logits 8.5 and 11.0, 32 rows 11.2 and 11.4, 64 rows 12.6 and 12.0.
 constexpr int64_t kFewRows = 64, kFewSmallRows = 32;
 
 // Most workgroups that each work out their own row's factors: it saves a
