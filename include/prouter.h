@@ -617,7 +617,8 @@ typedef struct pr_adamw pr_adamw;
  * v the smallest positive code. A value is rounded up when its 20 low bits
  * plus 20 random ones carry: right on average, so that a moving average
  * moves although each step changes it by less than its spacing. E = 255: the
- * block holds NaN or an infinity and stands for NaN throughout.
+ * block holds NaN, an infinity or a magnitude above 15/8 2^127, and stands for
+ * NaN throughout.
  *   Random bits: element i of tensor j takes mix(i + mix(j + 1 + K)) mod 2^32
  *   with K the upper 32 bits of SplitMix64's output for (seed, step) and
  *     mix(x): x *= 0x9E3779B9; x ^= x >> 15; x *= 0x6A09E667; x ^= x >> 13
