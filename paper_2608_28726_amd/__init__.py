@@ -674,11 +674,7 @@ class AdamW:
                 if name not in s:
                     raise ValueError(f"a state of {state_bits} bits needs '{name}'")
                 self._check(s[name], f"states' {name}", kind, size)
-        # What was checked, as tensors of its own: the plan's addresses stay allocated and of the checked sizes when one
-        # of the caller's is given another storage.
-        alias = lambda tensors: None if tensors is None else [t.detach() for t in tensors]  # noqa: E731
-        self._planned = (alias(self.params), alias(self.grads), alias(self.copies),
-                         [{k: s[k].detach() for k in names} for s in self.states])
+        self._tensors, self._storages = self._describe(names)
         self._seed = int(seed) & 0xFFFFFFFFFFFFFFFF
         if self._grad_dtype is not None:
             self._plan(self._grad_dtype)
@@ -713,35 +709,36 @@ class AdamW:
             sizes.update(m_exp=blocks, v_exp=blocks)
         return {k: torch.zeros(size, dtype=kind, device=self.device) for k, size in sizes.items()}
 
+    def _describe(self, names):
+        """The tensors that were checked, for the plan, and their storages: kept, so that the plan's addresses stay
+        allocated when one of the caller's tensors is given another storage."""
+        T = (_abi.AdamWTensor * len(self.params))()
+        for i, (t, p, s) in enumerate(zip(T, self.params, self.states)):
+            t.param, t.n = p.data_ptr(), self._sizes[i]
+            t.grad = self.grads[i].data_ptr() if self.grads else None
+            t.copy = self.copies[i].data_ptr() if self.copies else None
+            for name in names:
+                setattr(t, name, s[name].data_ptr())
+        lists = (self.params, self.grads or (), self.copies or (), *([s[k] for s in self.states] for k in names))
+        return T, [t.untyped_storage() for tensors in lists for t in tensors]
+
     def _plan(self, grad_dtype):
         """Makes the device's plan for gradients of this type, unless it is there."""
         if self._h and self._plan_dtype == grad_dtype:
             return
         self._destroy()
-        params, grads, copies, states = self._planned
-        T = (_abi.AdamWTensor * len(params))()
-        for i, (t, p, s) in enumerate(zip(T, params, states)):
-            t.param, t.n = p.data_ptr(), p.numel()
-            t.grad = grads[i].data_ptr() if grads else None
-            t.copy = copies[i].data_ptr() if copies else None
-            t.m, t.v = s["m"].data_ptr(), s["v"].data_ptr()
-            if self.state_bits == 8:
-                t.m_exp, t.v_exp = s["m_exp"].data_ptr(), s["v_exp"].data_ptr()
         code = {torch.float32: _abi.PR_F32, torch.bfloat16: _abi.PR_BF16}
-        st = _abi.lib().pr_adamw_create(T, len(T), code[self._dtype], code[grad_dtype], self.state_bits,
-                                        self._seed, C.byref(self._h))
+        st = _abi.lib().pr_adamw_create(self._tensors, len(self._tensors), code[self._dtype], code[grad_dtype],
+                                        self.state_bits, self._seed, C.byref(self._h))
         _abi.check("pr_adamw_create", st)
         self._plan_dtype = grad_dtype
-
-    def _check_open(self):
-        if self._closed:
-            raise ValueError("the optimizer is closed")
 
     def step(self, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
              grad_scale: float = 1.0, grads=None) -> None:
         """One step (``pr_adamw_step``) with the gradients given here or at construction; a None among those given
         here leaves its tensor as it is."""
-        self._check_open()
+        if self._closed:
+            raise ValueError("the optimizer is closed")
         stream = _check_current(self.device, "the optimizer's tensors")
         pointers = None
         if grads is not None:
@@ -769,7 +766,8 @@ class AdamW:
         of 256 elements, which receive the values and are returned instead; tensor j
         starts at 256 times the blocks of the tensors before it, and entries
         between tensors are left as they are."""
-        self._check_open()
+        if self._closed:
+            raise ValueError("the optimizer is closed")
         if self.state_bits == 32:
             if out is not None:
                 raise ValueError("out is for 8-bit states: 32-bit ones are returned themselves")
