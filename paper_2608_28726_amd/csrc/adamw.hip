@@ -4,8 +4,9 @@
 // p' = p - (lr wd p + lr c1 m' / (c2 sqrt(v') + eps)), elementwise in float32.
 // The step moves 10 to 30 bytes an element for 30 to 80 operations: memory
 // bounds it. 216 million float32 parameters with bfloat16 gradients and copies:
-// 32-bit states 1,083 us (6.1 GB, 5.6 TB/s), 8-bit states 610 us (3.5 GB, 5.7
-// TB/s), their values 257 us (1.3 GB, 5.0 TB/s); a copy reaches 6.5 TB/s. Short
+// 32-bit states 1,092 us (6.1 GB, 5.6 TB/s), 8-bit states 629 us (3.5 GB, 5.5
+// TB/s), their values 266 us (1.3 GB, 4.9 TB/s) under a trace, 1,076 and 854 us
+// (both) without; a copy reaches 6.5 TB/s. Short
 // workgroups in memory order suit it: of 512 threads and 2,048 elements the
 // 8-bit step took 599 us, of 256 and 1,024 617, of 256 and 2,048 674.
 #include "adamw.h"
