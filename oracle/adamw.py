@@ -12,7 +12,8 @@ R27  8-bit states. 256 elements of a tensor share an exponent byte E. With
      with its 20 low bits rounded up, at least 16 (m) or 32 (v); a value is
      its bits' upper part after 20 random bits have been added, minus the
      base; results below 1 are 0 for m and 1 for a positive v.
-     E = 255 marks a block that holds a NaN or an infinity.
+     E = 255 marks a block that holds a NaN, an infinity or a magnitude above
+     15/8 2^127.
 """
 
 from __future__ import annotations
