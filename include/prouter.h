@@ -457,8 +457,115 @@ pr_status pr_stream_finish(pr_stream* state, const int32_t* slots, int32_t n, fl
 /* Clears n slots (device int32 [n]) without producing a verdict. */
 pr_status pr_stream_reset_slots(pr_stream* state, const int32_t* slots, int32_t n, void* stream);
 
+/*
+ * Beam search over streamed requests: slot slots[i * n_beams + b] takes the
+ * state that slot slots[i * n_beams + parent[i * n_beams + b]] had before the
+ * call (pr_beam_reorder for a state's slots). slots, parent: device int32
+ * [n_req][n_beams]; no slot twice. An entry whose parent lies outside
+ * [0, n_beams), or whose slot or parent's slot is not one of the state's, leaves
+ * its slot as it is. 1 <= n_beams <= PR_MAX_BEAMS. Ordered like steps on the same slots.
+ */
+pr_status pr_stream_reorder(pr_stream* state, const int32_t* slots, const int32_t* parent, int32_t n_req,
+                            int32_t n_beams, void* stream);
+
 /* Frees the state (synchronises the device first). NULL is ignored. */
 void pr_stream_destroy(pr_stream* state);
+
+/* ------------------------------------------------------------------------
+ * Beam search over logit rows, and the largest logits of each row (what is
+ * kept of a teacher's rows to train a student on them).
+ * ------------------------------------------------------------------------ */
+
+/* Largest k of pr_top_logits, pr_beam_select and pr_distill_loss, and most beams of a request. */
+#define PR_MAX_TOP_LOGITS 256
+#define PR_MAX_BEAMS 64
+
+/*
+ * The first k tokens of each row in the order of pr_token_features_t (larger
+ * raw logit first, equal ones by lower index), with their log-probs.
+ *   logits .. row_stride, temperature  as for pr_token_features.
+ *   k         1 .. PR_MAX_TOP_LOGITS.
+ *   ids       int32 [n_rows][k], device: the tokens. A token of probability 0
+ *             (logit -inf) is never among them: where there are fewer than k
+ *             others, the rest are -1 with a log-prob of -inf.
+ *   logprob   float [n_rows][k], device: z / T - lse (-inf below float32's range).
+ *   lse       float [n_rows], device, or NULL: log sum exp(z / T).
+ *   flags     uint32 [n_rows], device, or NULL. A row flagged NONFINITE or
+ *             BAD_TP has NaN log-probs and lse and ids of -1.
+ *   workspace device scratch of at least pr_top_logits_workspace bytes, 16-byte
+ *             aligned (may be NULL when that is 0), not shared with a call that
+ *             may overlap; no initialisation needed.
+ * The tokens are exact. n_rows == 0 launches nothing.
+ */
+size_t pr_top_logits_workspace(pr_dtype dtype, int64_t n_rows, int32_t vocab, int32_t k);
+pr_status pr_top_logits(const void* logits, pr_dtype dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,
+                        const float* temperature, int32_t k, int32_t* ids, float* logprob, float* lse,
+                        uint32_t* flags, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Outputs of pr_beam_select. scores, parent and token are required. */
+typedef struct pr_beam_out_t {
+  float* scores;   /* [n_req][k] the continuations' scores, best first */
+  int32_t* parent; /* [n_req][k] the beam that each continues, -1: none left */
+  int32_t* token;  /* [n_req][k] the token that it continues with, -1: none left */
+  float* logprob;  /* [n_req][k] that token's log-prob, or NULL */
+  uint32_t* flags; /* [n_req][n_beams] of the beams, or NULL */
+} pr_beam_out_t;
+
+/*
+ * A step of beam search: the k best continuations of each request's beams.
+ * Row i * n_beams + b holds the logits after beam b of request i. Beam b and
+ * token v make a candidate of score scores[i][b] + log softmax(z / T)[v];
+ * the larger score comes first, equal ones by lower beam, then in the order of
+ * the beam's tokens (larger raw logit, lower index). Scores are compared in 64
+ * bits, before they are rounded to float32.
+ *   logits, dtype, vocab, row_stride, temperature
+ *              as for pr_token_features, n_req * n_beams rows.
+ *   scores     float [n_req][n_beams], device: of the beams so far. A beam of
+ *              -inf has no candidates (beams that do not exist yet or any
+ *              more).
+ *   done       uint8 [n_req][n_beams], device, or NULL: nonzero for a beam that
+ *              has ended. Its one candidate is itself: done_token, a log-prob
+ *              of 0, its score as it is.
+ *   k          1 .. PR_MAX_TOP_LOGITS, any relation to n_beams.
+ *   out        host pointer to a struct of device arrays. No output may overlap
+ *              an input. Where a request has fewer than k candidates the last
+ *              are -1, -1 and -inf.
+ *   workspace  device scratch of at least pr_beam_select_workspace bytes,
+ *              16-byte aligned, not shared with a call that may overlap; no
+ *              initialisation needed.
+ * Rows of beams of -inf and of ended ones are not read (flag MASKED). A beam
+ * whose score is NaN or +inf, or whose row is flagged NONFINITE or BAD_TP, has
+ * no candidates. 1 <= n_beams <= PR_MAX_BEAMS, n_req * n_beams <= 2^23
+ * (PR_ERR_UNSUPPORTED above). n_req == 0 launches nothing.
+ */
+size_t pr_beam_select_workspace(pr_dtype dtype, int32_t n_req, int32_t n_beams, int32_t vocab, int32_t k);
+pr_status pr_beam_select(const void* logits, pr_dtype dtype, int32_t n_req, int32_t n_beams, int32_t vocab,
+                         int64_t row_stride, const float* temperature, const float* scores, const uint8_t* done,
+                         int32_t done_token, int32_t k, const pr_beam_out_t* out, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* A state of every beam: row i * n_beams + b starts row_stride bytes after the
+ * one before it and has row_bytes bytes. */
+typedef struct pr_beam_state {
+  void* rows; /* device, any alignment */
+  int64_t row_bytes;
+  int64_t row_stride;
+} pr_beam_state;
+
+/*
+ * Puts the beams' states into the order of the beams that were chosen, in
+ * place: row i * n_beams + b of each state becomes what row
+ * i * n_beams + parent[i][b] was before the call.
+ *   states    host array of n_states (read during the call), device memory.
+ *             No two may overlap (PR_ERR_INVALID_ARG; rows of two states may
+ *             lie side by side in one stride). 0 <= row_bytes <= row_stride.
+ *   parent    int32 [n_req][n_beams], device, with any repetition. An entry
+ *             outside [0, n_beams) leaves its row as it is.
+ * Nothing is allocated; only rows that change are written. One launch per 96
+ * states. 1 <= n_beams <= PR_MAX_BEAMS, n_req * n_beams < 2^31.
+ */
+pr_status pr_beam_reorder(const pr_beam_state* states, int32_t n_states, const int32_t* parent, int32_t n_req,
+                          int32_t n_beams, void* stream);
 
 /* ------------------------------------------------------------------------
  * Training the small model on what the routing saw: losses over the same
@@ -570,6 +677,63 @@ pr_status pr_preference_loss(const void* logits, pr_dtype dtype, int64_t n_rows,
                              const int32_t* offsets, int32_t n_pairs, const float* ref_logprob,
                              const pr_preference_params* params, float* loss, const pr_preference_out_t* out,
                              void* grad, int64_t grad_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* What pr_distill_loss makes of the probability that a row's entries leave over. */
+typedef enum pr_tail PR_ENUM_BASE {
+  PR_TAIL_DROP = 0,   /* nothing: the sum over the entries alone */
+  PR_TAIL_RENORM = 1, /* the entries' probabilities are divided by their sum */
+  PR_TAIL_REST = 2    /* all other tokens together are one more */
+} pr_tail;
+
+/* Options of pr_distill_loss. */
+typedef struct pr_distill_params {
+  pr_tail tail;
+  double grad_scale; /* finite factor of the gradient alone */
+} pr_distill_params;
+
+/* Per-token outputs of pr_distill_loss, each [n_rows]; any may be NULL. */
+typedef struct pr_distill_tokens_t {
+  float* token_loss; /* l */
+  float* mass;       /* P, the student's probability of the entries' tokens */
+  uint32_t* flags;
+} pr_distill_tokens_t;
+
+/* Fills *params (host pointer): PR_TAIL_REST, grad_scale = 1. */
+void pr_distill_params_default(pr_distill_params* params);
+
+/*
+ * Distillation from a teacher's largest log-probs, and its gradient in the
+ * student's logits. A row's entries are tokens v_i with the teacher's log-prob
+ * log q_i (as from pr_top_logits). With u = z / T, p = softmax(u),
+ * Q = sum q_i, P = sum p_{v_i}:
+ *   l = sum q_i (log q_i - log p_{v_i})         (q_i / Q for q_i with RENORM)
+ *     + r_q (log r_q - log r_p)                 with REST: r_q = max(0, 1 - Q), r_p = 1 - P
+ *   loss = sum over rows of weight l
+ *   dloss/dz_v = weight / T ((Q + r_q) p_v - q_i)            v = v_i
+ *              = weight / T (Q - P r_q / r_p) p_v            any other v
+ * (Q = 1 with RENORM, r_q = 0 without REST). Where no other token is left
+ * (r_p = 0: all others are -inf) the rest is no term. The factor T^2 that is
+ * usual with temperatures above 1 belongs in the weights.
+ *   logits .. row_stride, temperature, weight, loss, grad, workspace
+ *                as for pr_policy_loss.
+ *   top_ids, top_logprob
+ *                int32 and float, row r's entries at element r * top_stride,
+ *                k of them (top_stride >= k, 0 <= k <= PR_MAX_TOP_LOGITS; NULL
+ *                when k is 0), in any order. An entry of log-prob -inf is none,
+ *                whatever its id; a row may have none (l = 0). A log-prob of
+ *                NaN or +inf flags the row NONFINITE; an id outside [0, vocab),
+ *                or the same id twice, BAD_ID.
+ *   params       host pointer, or NULL for the defaults.
+ *   out          host pointer to a struct of device arrays, or NULL.
+ * A token of the teacher's with probability q_i > 0 that the student gives 0
+ * makes l +inf; its gradient is as above. Flagged rows as for pr_policy_loss.
+ */
+size_t pr_distill_loss_workspace(pr_dtype dtype, int64_t n_rows, int32_t vocab, int32_t k);
+pr_status pr_distill_loss(const void* logits, pr_dtype dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,
+                          const int32_t* top_ids, const float* top_logprob, int32_t k, int64_t top_stride,
+                          const float* temperature, const float* weight, const pr_distill_params* params, float* loss,
+                          const pr_distill_tokens_t* out, void* grad, int64_t grad_stride, void* workspace,
+                          size_t workspace_bytes, void* stream);
 
 /* One tensor of an AdamW step. Pointers are device pointers, aligned to their
  * element size. */

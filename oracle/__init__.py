@@ -24,12 +24,15 @@ ship rule p >= tau):
 * :mod:`oracle.loss` -- the policy and preference losses over logit rows and
   their gradients.
 * :mod:`oracle.adamw` -- the AdamW step and its 8-bit states.
+* :mod:`oracle.distill` -- a row's largest logits and the loss against a
+  teacher's.
+* :mod:`oracle.beam` -- a step of beam search and the reordering of states.
 
 Parity pinning: every function here is pinned by ``tests/test_oracle_pins.py``,
 ``tests/test_oracle_sequence.py``, ``tests/test_oracle_head.py``,
 ``tests/test_oracle_calibrate.py``, ``tests/test_oracle_sampling.py``,
-``tests/test_oracle_loss.py`` and ``tests/test_oracle_adamw.py`` against closed
-forms, invariants, pure-Python brute force, differences and (for the head, the
+``tests/test_oracle_loss.py``, ``tests/test_oracle_adamw.py`` and
+``tests/test_oracle_beam.py`` against closed forms, invariants, pure-Python brute force, differences and (for the head, the
 losses' gradients and the optimizer) an independent implementation, except the default
 score head (a fixed linear summary chosen because the paper publishes no
 trained head weights) and the transformer head's weights, which are *parity

@@ -14,8 +14,12 @@ top-K entropy (Sec. 3.1, Eq. 3): :func:`feature_sequence`.
 
 Streaming decode: :class:`StreamState`.
 
-Training the small model on what the routing saw: :func:`policy_loss` and
-:func:`preference_loss` over the same logit rows, with their gradients, and
+Beam search: :func:`beam_select`, :func:`beam_reorder` and
+:meth:`StreamState.reorder`; a row's largest logits: :func:`top_logits`.
+
+Training the small model on what the routing saw: :func:`policy_loss`,
+:func:`preference_loss` and, on a teacher's largest logits,
+:func:`distill_loss` over the same logit rows, with their gradients, and
 :class:`AdamW`.
 """
 
@@ -30,7 +34,8 @@ from ._abi import (FLAG_BAD_ID, FLAG_BAD_TP, FLAG_CLIPPED, FLAG_MASKED, FLAG_NON
                    FLAG_OUTSIDE_NUCLEUS, ProuterError)
 
 __all__ = ["token_features", "token_features_noalloc", "feature_sequence", "sample_features", "verifier_head", "request_aggregate", "route", "calibrate_threshold",
-           "validate_offsets", "StreamState", "policy_loss", "preference_loss", "AdamW",
+           "validate_offsets", "StreamState", "top_logits", "beam_select", "beam_reorder", "policy_loss", "preference_loss",
+           "distill_loss", "AdamW",
            "token_features_workspace", "ProuterError", "FEATURE_FLOATS", "FEATURE_INTS", "PAPER_TOP_K"]
 
 PAPER_TOP_K = 20  # K of the paper's top-K entropy (Sec. 3.1)
@@ -38,6 +43,7 @@ PAPER_TOP_K = 20  # K of the paper's top-K entropy (Sec. 3.1)
 FEATURE_FLOATS = ("max_logit", "lse", "entropy", "logprob", "maxprob", "margin")
 FEATURE_INTS = ("rank", "argmax", "cutoff")
 _LINKS = {"identity": 0, "sigmoid": 1}
+_TAILS = {"drop": _abi.PR_TAIL_DROP, "renorm": _abi.PR_TAIL_RENORM, "rest": _abi.PR_TAIL_REST}
 
 
 # What a call costs on the host is most of a small batch's time: pointers go to
@@ -449,6 +455,17 @@ class StreamState:
         _abi.check("pr_stream_reset_slots",
                    _abi.lib().pr_stream_reset_slots(self._h, _ptr(slots), slots.shape[0], _stream_handle()))
 
+    def reorder(self, slots: torch.Tensor, parent: torch.Tensor) -> None:
+        """Beam search (``pr_stream_reorder``): slot ``slots[i, b]`` takes the state that slot
+        ``slots[i, parent[i, b]]`` had; int32 [n_req, n_beams] tensors, no slot twice. A parent outside
+        [0, n_beams) leaves its slot as it is."""
+        stream = _check_current(slots.device, "slots")
+        n_req, B = _check_parents(parent, slots.device)
+        if slots.dtype != torch.int32 or slots.shape != parent.shape or not slots.is_contiguous():
+            raise ValueError(f"slots must be a contiguous int32 {list(parent.shape)} tensor")
+        _abi.check("pr_stream_reorder", _abi.lib().pr_stream_reorder(self._h, slots.data_ptr(), parent.data_ptr(), n_req,
+                                                                       B, stream))
+
     def close(self) -> None:
         if self._h:
             _abi.lib().pr_stream_destroy(self._h)
@@ -459,6 +476,150 @@ class StreamState:
             self.close()
         except Exception:
             pass
+
+
+# ---------------------------------------------------------------------------
+# Beam search and the largest logits of rows.
+
+def _check_logits(logits):
+    """Checks of logit rows on the current device. Returns the stream, the device and the type's code."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be a 2-D CUDA tensor with unit stride along the vocabulary")
+    code = _dtype_code(logits)
+    stream = _check_current(logits.device, "logits")
+    if not _rows_apart(logits, logits.shape[1]):
+        raise ValueError("logits must be a 2-D CUDA tensor with unit stride along the vocabulary and rows apart")
+    return stream, logits.device, code
+
+
+def _check_parents(parent, device):
+    if parent.dtype != torch.int32 or parent.dim() != 2 or not parent.is_contiguous() or parent.device != device:
+        raise ValueError(f"parent must be a contiguous int32 [n_req, n_beams] tensor on {device}")
+    return parent.shape
+
+
+def top_logits(logits: torch.Tensor, k: int, temperature=1.0, workspace: torch.Tensor | None = None) -> dict:
+    """The k largest logits of each row (``pr_top_logits``), 1 <= k <= 256.
+
+    ``logits`` [n_rows, V] float32/bfloat16, ``temperature`` float32 [n_rows]
+    or a Python float. Returns a dict with ``ids`` (int32 [n_rows, k], the
+    tokens: larger logit first, equal ones by lower index), ``logprob``
+    ([n_rows, k], their log-probs), ``lse`` and ``flags`` ([n_rows]). Tokens
+    of probability 0 are left out: where a row has fewer than k others, the
+    last ids are -1 with a log-prob of -inf (no entries for
+    :func:`distill_loss`). ``workspace``: optional device scratch of this
+    call, not shared with one that may overlap.
+    """
+    stream, device, code = _check_logits(logits)
+    n, V = logits.shape
+    k = int(k)
+    if not 1 <= k <= _abi.PR_MAX_TOP_LOGITS:
+        raise ValueError(f"k must be between 1 and {_abi.PR_MAX_TOP_LOGITS}")
+    temperature = _as_row_tensor(temperature, n, device)
+    _check_row_floats(device, n, temperature=temperature)
+    L = _abi.lib()
+    ws, ws_bytes, (logprob, lse) = _loss_outputs((n * k, n), workspace, L.pr_top_logits_workspace(code, n, V, k), device)
+    ids, flags = torch.empty(n * (k + 1), dtype=torch.int32, device=device).unsafe_split_with_sizes((n * k, n))
+    st = L.pr_top_logits(logits.data_ptr(), code, n, V, _row_stride(logits), temperature.data_ptr(), k, ids.data_ptr(),
+                         logprob.data_ptr(), lse.data_ptr(), flags.data_ptr(), ws, ws_bytes, stream)
+    _abi.check("pr_top_logits", st)
+    return {"ids": ids.view(n, k), "logprob": logprob.view(n, k), "lse": lse, "flags": flags}
+
+
+def beam_select(logits: torch.Tensor, scores: torch.Tensor, temperature=1.0, k: int | None = None,
+                done: torch.Tensor | None = None, done_token: int = -1, workspace: torch.Tensor | None = None) -> dict:
+    """A step of beam search (``pr_beam_select``): the k best continuations of each request's beams.
+
+    ``scores`` float32 [n_req, n_beams] (1 to 64 beams): of the beams so far,
+    -inf for beams that do not exist. ``logits`` [n_req * n_beams, V]
+    float32/bfloat16: row ``i * n_beams + b`` follows beam b of request i.
+    ``temperature``: float32 per row or a Python float. A continuation's score
+    is its beam's plus its token's log-prob; the best come first, equal ones by
+    lower beam, larger logit, lower token. ``k``: 1 to 256, by default n_beams.
+    ``done``: bool or uint8 [n_req, n_beams], beams that have ended; each
+    competes as it is, with ``done_token``.
+
+    Returns a dict with ``scores``, ``parent`` (the beam that is continued),
+    ``token`` and ``logprob`` (of the token), each [n_req, k], and the beams'
+    ``flags`` [n_req * n_beams]. Where a request has fewer than k
+    continuations, the last are -inf, -1, -1 and -inf. ``workspace`` as for
+    :func:`top_logits`.
+    """
+    stream, device, code = _check_logits(logits)
+    n, V = logits.shape
+    if scores.dtype != torch.float32 or scores.dim() != 2 or not scores.is_contiguous() or scores.device != device:
+        raise ValueError(f"scores must be a contiguous float32 [n_req, n_beams] tensor on {device}")
+    n_req, B = scores.shape
+    if not 1 <= B <= _abi.PR_MAX_BEAMS or n_req * B != n:
+        raise ValueError(f"scores must be [n_req, n_beams] with 1 to {_abi.PR_MAX_BEAMS} beams and a row of logits each")
+    k = B if k is None else int(k)
+    if not 1 <= k <= _abi.PR_MAX_TOP_LOGITS:
+        raise ValueError(f"k must be between 1 and {_abi.PR_MAX_TOP_LOGITS}")
+    if done is not None and (done.dtype not in (torch.bool, torch.uint8) or done.shape != scores.shape
+                             or not done.is_contiguous() or done.device != device):
+        raise ValueError(f"done must be a contiguous bool or uint8 {list(scores.shape)} tensor on {device}")
+    done_token = int(done_token)
+    if not -1 << 31 <= done_token < 1 << 31:
+        raise ValueError("done_token must be a 32-bit number")
+    temperature = _as_row_tensor(temperature, n, device)
+    _check_row_floats(device, n, temperature=temperature)
+    L = _abi.lib()
+    m = n_req * k
+    ws, ws_bytes, (best, logprob) = _loss_outputs((m, m), workspace, L.pr_beam_select_workspace(code, n_req, B, V, k),
+                                                  device)
+    parent, token, flags = torch.empty(2 * m + n, dtype=torch.int32, device=device).unsafe_split_with_sizes((m, m, n))
+    out = _abi.BeamOut(best.data_ptr(), parent.data_ptr(), token.data_ptr(), logprob.data_ptr(), flags.data_ptr())
+    st = L.pr_beam_select(logits.data_ptr(), code, n_req, B, V, _row_stride(logits), temperature.data_ptr(),
+                          scores.data_ptr(), _ptr(done), done_token, k, C.byref(out), ws, ws_bytes, stream)
+    _abi.check("pr_beam_select", st)
+    return {"scores": best.view(n_req, k), "parent": parent.view(n_req, k), "token": token.view(n_req, k),
+            "logprob": logprob.view(n_req, k), "flags": flags}
+
+
+def beam_reorder(states, parent: torch.Tensor) -> None:
+    """Puts beams' states into the order of the beams that were chosen, in place (``pr_beam_reorder``).
+
+    ``states``: tensors of any types, each [n_req * n_beams, ...] or
+    [n_req, n_beams, ...]: beam b of request i becomes what beam
+    ``parent[i, b]`` was. ``parent`` int32 [n_req, n_beams] (as
+    :func:`beam_select` returns it with k = n_beams); an entry outside
+    [0, n_beams) leaves its beam as it is. A beam's part of a tensor must be
+    contiguous; beams may lie apart. No two tensors may overlap.
+    """
+    states = [states] if isinstance(states, torch.Tensor) else list(states)
+    device = parent.device
+    stream = _check_current(device, "parent")
+    n_req, B = _check_parents(parent, device)
+    if not 1 <= B <= _abi.PR_MAX_BEAMS:
+        raise ValueError(f"parent must have 1 to {_abi.PR_MAX_BEAMS} beams")
+    n = n_req * B
+    S = (_abi.BeamState * len(states))()
+    for t, x in zip(S, states):
+        if x.device != device:
+            raise ValueError(f"states must be tensors on {device}")
+        if x.dim() >= 1 and x.shape[0] == n:
+            inner, stride, rows = x.shape[1:], x.stride(), 1
+        elif x.dim() >= 2 and x.shape[:2] == parent.shape:
+            inner, stride, rows = x.shape[2:], x.stride()[1:], 2
+            if B > 1 and n_req > 1 and x.stride(0) != B * x.stride(1):
+                inner = None
+        else:
+            raise ValueError(f"states must be [{n}, ...] or [{n_req}, {B}, ...] tensors")
+        size = 1
+        if inner is not None:
+            for d, extent in zip(reversed(x.stride()[rows:]), reversed(inner)):
+                if extent != 1 and d != size:
+                    inner = None
+                    break
+                size *= extent
+        if n == 0 or (inner is not None and size == 0):
+            continue  # nothing to move
+        # One row, or one request of one beam, may come with any stride.
+        step = size if n == 1 else (x.stride(0) if rows == 1 or B == 1 else stride[0])
+        if inner is None or step < size:
+            raise ValueError("a beam's part of a state must be contiguous, and the beams' apart")
+        t.rows, t.row_bytes, t.row_stride = x.data_ptr(), size * x.element_size(), step * x.element_size()
+    _abi.check("pr_beam_reorder", _abi.lib().pr_beam_reorder(S, len(S), parent.data_ptr(), n_req, B, stream))
 
 
 # ---------------------------------------------------------------------------
@@ -495,7 +656,8 @@ def _check_loss(logits, ids, temperature, grad):
     stream = _check_current(device, "logits")
     if not _rows_apart(logits, V):
         raise ValueError("logits must be a 2-D CUDA tensor with unit stride along the vocabulary and rows apart")
-    _check_index_tensor(ids, "ids", device, n)
+    if ids is not None:
+        _check_index_tensor(ids, "ids", device, n)
     if grad is True:
         grad = torch.empty((n, V), dtype=logits.dtype, device=device)
     elif grad is False or grad is None:
@@ -607,6 +769,57 @@ def preference_loss(logits: torch.Tensor, ids: torch.Tensor, temperature, weight
                               0 if grad is None else _row_stride(grad), ws, ws_bytes, stream)
     _abi.check("pr_preference_loss", st)
     out = {"loss": loss, "pair_loss": pair, "pair_logit": h, "seq_logratio": q, "logprob": logprob, "flags": flags}
+    if grad is not None:
+        out["grad"] = grad
+    return out
+
+
+def distill_loss(logits: torch.Tensor, top_ids: torch.Tensor, top_logprob: torch.Tensor, temperature,
+                 weight: torch.Tensor, tail: str = "rest", grad=True, grad_scale: float = 1.0,
+                 workspace: torch.Tensor | None = None) -> dict:
+    """Distillation from a teacher's largest log-probs, and its gradient (``pr_distill_loss``).
+
+    ``logits``, ``temperature``, ``weight``, ``grad``, ``workspace`` as for
+    :func:`policy_loss`. ``top_ids`` int32 and ``top_logprob`` float32
+    [n_rows, k], k up to 256: the teacher's tokens of each row and their
+    log-probs, as :func:`top_logits` returns them (entries of -inf are none).
+    The loss is the sum over rows of weight times the divergence of the
+    student's distribution p at ``temperature`` from the teacher's q:
+    sum of q (log q - log p) over the entries, where ``tail`` says what becomes
+    of the probability that they leave over: "rest" adds all other tokens as one
+    more, "drop" leaves it out, "renorm" divides the entries' q by their sum.
+
+    Returns a dict with ``loss`` (float32 [1]), ``token_loss``, ``mass`` (the
+    student's probability of the entries' tokens), ``flags`` ([n_rows]) and,
+    when wanted, ``grad``.
+    """
+    if tail not in _TAILS:
+        raise ValueError(f"tail must be one of {sorted(_TAILS)}")
+    if logits.dim() == 2 and (top_ids.dim() != 2 or top_ids.shape[0] != logits.shape[0]
+                              or top_ids.shape[1] > _abi.PR_MAX_TOP_LOGITS):
+        raise ValueError(f"top_ids must be an int32 [{logits.shape[0]}, k] tensor, k up to {_abi.PR_MAX_TOP_LOGITS}")
+    stream, device, code, temperature, grad = _check_loss(logits, None, temperature, grad)
+    n, V = logits.shape
+    k = top_ids.shape[1]
+    for name, t, dtype in (("top_ids", top_ids, torch.int32), ("top_logprob", top_logprob, torch.float32)):
+        if t.dtype != dtype or t.shape != (n, k) or t.device != device or (k > 0 and not _rows_apart(t, k)):
+            raise ValueError(f"{name} must be a {dtype} [{n}, {k}] tensor on {device} with unit stride along the entries "
+                             "and rows apart")
+    if n > 1 and top_ids.stride(0) != top_logprob.stride(0):
+        top_ids, top_logprob = top_ids.contiguous(), top_logprob.contiguous()
+    _check_row_floats(device, n, temperature=temperature, weight=weight)
+    L = _abi.lib()
+    ws, ws_bytes, (token_loss, mass, loss) = _loss_outputs((n, n, 1), workspace,
+                                                           L.pr_distill_loss_workspace(code, n, V, k), device)
+    flags = torch.empty(n, dtype=torch.int32, device=device)
+    params = _abi.DistillParams(_TAILS[tail], grad_scale)
+    tokens = _abi.DistillTokens(token_loss.data_ptr(), mass.data_ptr(), flags.data_ptr())
+    st = L.pr_distill_loss(logits.data_ptr(), code, n, V, _row_stride(logits), top_ids.data_ptr(),
+                           top_logprob.data_ptr(), k, max(k, _row_stride(top_ids)), temperature.data_ptr(),
+                           weight.data_ptr(), C.byref(params), loss.data_ptr(), C.byref(tokens), _ptr(grad),
+                           0 if grad is None else _row_stride(grad), ws, ws_bytes, stream)
+    _abi.check("pr_distill_loss", st)
+    out = {"loss": loss, "token_loss": token_loss, "mass": mass, "flags": flags}
     if grad is not None:
         out["grad"] = grad
     return out

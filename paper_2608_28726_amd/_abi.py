@@ -34,7 +34,9 @@ EXPORTED = (
     "pr_token_features_workspace_full", "pr_stream_step_workspace", "pr_stream_step_ws", "pr_token_features_ws",
     "pr_policy_params_default", "pr_policy_loss_workspace", "pr_policy_loss", "pr_preference_params_default",
     "pr_preference_loss_workspace", "pr_preference_loss", "pr_adamw_create", "pr_adamw_step", "pr_adamw_moments",
-    "pr_adamw_destroy",
+    "pr_adamw_destroy", "pr_top_logits_workspace", "pr_top_logits", "pr_beam_select_workspace", "pr_beam_select",
+    "pr_beam_reorder", "pr_stream_reorder", "pr_distill_params_default", "pr_distill_loss_workspace",
+    "pr_distill_loss",
 )
 
 PR_HEAD_WEIGHTS = 67329
@@ -42,6 +44,10 @@ PR_HEAD_WEIGHTS = 67329
 PR_MAX_TOP_K = 32
 
 PR_ADAMW_BLOCK = 256
+
+PR_MAX_TOP_LOGITS, PR_MAX_BEAMS = 256, 64
+
+PR_TAIL_DROP, PR_TAIL_RENORM, PR_TAIL_REST = range(3)
 
 
 class TokenFeatures(C.Structure):
@@ -74,6 +80,26 @@ class PreferenceParams(C.Structure):
 
 class PreferenceOut(C.Structure):
     _fields_ = [(name, C.c_void_p) for name in PREFERENCE_FIELDS]
+
+
+DISTILL_FIELDS = ("token_loss", "mass", "flags")
+BEAM_FIELDS = ("scores", "parent", "token", "logprob", "flags")
+
+
+class DistillParams(C.Structure):
+    _fields_ = [("tail", C.c_int), ("grad_scale", C.c_double)]
+
+
+class DistillTokens(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in DISTILL_FIELDS]
+
+
+class BeamOut(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in BEAM_FIELDS]
+
+
+class BeamState(C.Structure):
+    _fields_ = [("rows", C.c_void_p), ("row_bytes", C.c_int64), ("row_stride", C.c_int64)]
 
 
 class AdamWTensor(C.Structure):
@@ -181,6 +207,25 @@ def lib() -> C.CDLL:
     L.pr_preference_loss.argtypes = [vp, C.c_int, i64, i32, i64, vp, vp, vp, vp, i32, vp, C.POINTER(PreferenceParams),
                                      vp, C.POINTER(PreferenceOut), vp, i64, vp, sz, vp]
     L.pr_preference_loss.restype = C.c_int
+    L.pr_top_logits_workspace.argtypes = [C.c_int, i64, i32, i32]
+    L.pr_top_logits_workspace.restype = sz
+    L.pr_top_logits.argtypes = [vp, C.c_int, i64, i32, i64, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+    L.pr_top_logits.restype = C.c_int
+    L.pr_beam_select_workspace.argtypes = [C.c_int, i32, i32, i32, i32]
+    L.pr_beam_select_workspace.restype = sz
+    L.pr_beam_select.argtypes = [vp, C.c_int, i32, i32, i32, i64, vp, vp, vp, i32, i32, C.POINTER(BeamOut), vp, sz, vp]
+    L.pr_beam_select.restype = C.c_int
+    L.pr_beam_reorder.argtypes = [C.POINTER(BeamState), i32, vp, i32, i32, vp]
+    L.pr_beam_reorder.restype = C.c_int
+    L.pr_stream_reorder.argtypes = [vp, vp, vp, i32, i32, vp]
+    L.pr_stream_reorder.restype = C.c_int
+    L.pr_distill_params_default.argtypes = [C.POINTER(DistillParams)]
+    L.pr_distill_params_default.restype = None
+    L.pr_distill_loss_workspace.argtypes = [C.c_int, i64, i32, i32]
+    L.pr_distill_loss_workspace.restype = sz
+    L.pr_distill_loss.argtypes = [vp, C.c_int, i64, i32, i64, vp, vp, i32, i64, vp, vp, C.POINTER(DistillParams), vp,
+                                  C.POINTER(DistillTokens), vp, i64, vp, sz, vp]
+    L.pr_distill_loss.restype = C.c_int
     L.pr_adamw_create.argtypes = [C.POINTER(AdamWTensor), i32, C.c_int, C.c_int, i32, C.c_uint64, C.POINTER(vp)]
     L.pr_adamw_create.restype = C.c_int
     L.pr_adamw_step.argtypes = [vp, C.POINTER(vp), C.POINTER(AdamWParams), vp]

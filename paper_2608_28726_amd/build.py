@@ -32,7 +32,7 @@ TOOLS_LIB = os.path.join(PKG, "libprtools.so")
 TOOLS_SOURCES = ["tools/prtools.hip"]
 
 SOURCES = ["row_features.hip", "topp.hip", "aggregate.hip", "head.hip", "head_tiles.hip", "calibrate.hip",
-           "loss.hip", "adamw.hip", "api.hip"]
+           "loss.hip", "distill.hip", "select.hip", "reorder.hip", "adamw.hip", "api.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

@@ -1,6 +1,7 @@
 // C ABI of the verifier library: argument checks, launch-shape selection and
 // the streaming state object. Every compute step runs in the kernels of
 // row_features.hip, topp.hip and aggregate.hip.
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 #include <new>
@@ -9,8 +10,10 @@
 #include "adamw.h"
 #include "aggregate.h"
 #include "calibrate.h"
+#include "distill.h"
 #include "head.h"
 #include "loss.h"
+#include "select.h"
 #include "topp.h"
 
 using namespace pr;
@@ -157,6 +160,25 @@ uint32_t step_key(uint64_t seed, int64_t step) {
   x = (x ^ (x >> 30)) * 0xBF58476D1CE4E5B9ull;
   x = (x ^ (x >> 27)) * 0x94D049BB133111EBull;
   return static_cast<uint32_t>((x ^ (x >> 31)) >> 32);
+}
+
+pr_status check_beams(int32_t n_req, int32_t n_beams) {
+  if (n_req < 0 || n_beams < 1) return PR_ERR_INVALID_ARG;
+  if (n_beams > PR_MAX_BEAMS || n_req > INT32_MAX / n_beams) return PR_ERR_UNSUPPORTED;
+  return PR_OK;
+}
+
+// Whether two states share a byte: their rows' bytes from the first to the last
+// do, and they do not lie side by side in rows of one stride.
+bool states_overlap(const pr_beam_state& a, const pr_beam_state& b, int64_t n) {
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.rows), b0 = reinterpret_cast<uintptr_t>(b.rows);
+  const uintptr_t a1 = a0 + static_cast<uintptr_t>((n - 1) * a.row_stride + a.row_bytes);
+  const uintptr_t b1 = b0 + static_cast<uintptr_t>((n - 1) * b.row_stride + b.row_bytes);
+  if (a1 <= b0 || b1 <= a0) return false;
+  if (a.row_stride != b.row_stride) return true;
+  const int64_t s = a.row_stride, d = static_cast<int64_t>((b0 > a0 ? b0 - a0 : a0 - b0) % static_cast<uintptr_t>(s));
+  const int64_t lo = b0 > a0 ? a.row_bytes : b.row_bytes, hi = b0 > a0 ? b.row_bytes : a.row_bytes;
+  return d < lo || d + hi > s;
 }
 
 bool params_ok(const pr_agg_params& p) {
@@ -550,6 +572,28 @@ pr_status pr_stream_reset_slots(pr_stream* state, const int32_t* slots, int32_t 
   return hip_status(launch_stream_clear(state->dev, slots, n, as_stream(stream)));
 }
 
+pr_status pr_stream_reorder(pr_stream* state, const int32_t* slots, const int32_t* parent, int32_t n_req,
+                            int32_t n_beams, void* stream) {
+  if (!state) return PR_ERR_INVALID_ARG;
+  const pr_status st = check_beams(n_req, n_beams);
+  if (st != PR_OK) return st;
+  if (n_req == 0) return PR_OK;
+  if (!slots || !parent) return PR_ERR_INVALID_ARG;
+  const StreamDev& d = state->dev;
+  StateList list{};
+  auto add = [&](void* p, int64_t bytes) {
+    if (p && bytes > 0) list.s[list.n++] = pr_beam_state{p, bytes, bytes};
+  };
+  add(d.hist, static_cast<int64_t>(d.max_len) * 16);
+  add(d.sum, 32);
+  add(d.minv, 16);
+  add(d.count, 4);
+  add(d.nanbits, 4);
+  add(d.p2q, 160);
+  add(d.p2n, 64);
+  return hip_status(launch_reorder(list, slots, d.max_slots, parent, n_req, n_beams, as_stream(stream)));
+}
+
 void pr_stream_destroy(pr_stream* state) {
   if (!state) return;
   int prev = 0;
@@ -559,6 +603,113 @@ void pr_stream_destroy(pr_stream* state) {
   (void)hipFree(state->block);
   (void)hipSetDevice(prev);
   delete state;
+}
+
+size_t pr_top_logits_workspace(pr_dtype dtype, int64_t n_rows, int32_t vocab, int32_t k) {
+  return vocab < 2 || k < 1 ? 0 : top_workspace_bytes(n_rows, vocab, dtype, k);
+}
+
+pr_status pr_top_logits(const void* logits, pr_dtype dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,
+                        const float* temperature, int32_t k, int32_t* ids, float* logprob, float* lse,
+                        uint32_t* flags, void* workspace, size_t workspace_bytes, void* stream) {
+  const pr_status st = check_rows(logits, dtype, n_rows, vocab, row_stride, ids, temperature);
+  if (st != PR_OK) return st;
+  if (k < 1 || k > PR_MAX_TOP_LOGITS || (n_rows > 0 && !logprob)) return PR_ERR_INVALID_ARG;
+  const size_t need = pr_top_logits_workspace(dtype, n_rows, vocab, k);
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return PR_ERR_INVALID_ARG;
+  if (n_rows == 0) return PR_OK;
+  TopArgs a{};
+  a.logits = logits;
+  a.n_rows = n_rows;
+  a.V = vocab;
+  a.row_stride = row_stride;
+  a.temperature = temperature;
+  a.k = k;
+  a.ids = ids;
+  a.logprob = logprob;
+  a.lse = lse;
+  a.flags = flags;
+  a.ws = workspace;
+  return hip_status(launch_top(a, dtype, as_stream(stream)));
+}
+
+size_t pr_beam_select_workspace(pr_dtype dtype, int32_t n_req, int32_t n_beams, int32_t vocab, int32_t k) {
+  if (n_req < 1 || n_beams < 1 || vocab < 2 || k < 1) return 0;
+  return beam_workspace_bytes(static_cast<int64_t>(n_req) * n_beams, vocab, dtype, k);
+}
+
+pr_status pr_beam_select(const void* logits, pr_dtype dtype, int32_t n_req, int32_t n_beams, int32_t vocab,
+                         int64_t row_stride, const float* temperature, const float* scores, const uint8_t* done,
+                         int32_t done_token, int32_t k, const pr_beam_out_t* out, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  pr_status st = check_beams(n_req, n_beams);
+  if (st != PR_OK) return st;
+  const int64_t n = static_cast<int64_t>(n_req) * n_beams;
+  st = check_rows(logits, dtype, n, vocab, row_stride, reinterpret_cast<const int32_t*>(scores), temperature);
+  if (st != PR_OK) return st;
+  if (k < 1 || k > PR_MAX_TOP_LOGITS || !out) return PR_ERR_INVALID_ARG;
+  if (n > (1 << 23)) return PR_ERR_UNSUPPORTED;
+  if (n_req == 0) return PR_OK;
+  if (!out->scores || !out->parent || !out->token) return PR_ERR_INVALID_ARG;
+  const size_t need = pr_beam_select_workspace(dtype, n_req, n_beams, vocab, k);
+  if (!workspace || workspace_bytes < need || !aligned(workspace, 16)) return PR_ERR_INVALID_ARG;
+  BeamArgs a{};
+  a.logits = logits;
+  a.n_req = n_req;
+  a.B = n_beams;
+  a.V = vocab;
+  a.row_stride = row_stride;
+  a.temperature = temperature;
+  a.scores = scores;
+  a.done = done;
+  a.done_token = done_token;
+  a.k = k;
+  a.out = *out;
+  a.ws = workspace;
+  return hip_status(launch_beam(a, dtype, as_stream(stream)));
+}
+
+pr_status pr_beam_reorder(const pr_beam_state* states, int32_t n_states, const int32_t* parent, int32_t n_req,
+                          int32_t n_beams, void* stream) {
+  const pr_status st = check_beams(n_req, n_beams);
+  if (st != PR_OK) return st;
+  if (n_states < 0 || (n_states > 0 && !states)) return PR_ERR_INVALID_ARG;
+  const int64_t n = static_cast<int64_t>(n_req) * n_beams;
+  // No device holds more; byte offsets stay below 2^63.
+  constexpr int64_t kMostBytes = int64_t{1} << 42;
+  for (int32_t j = 0; j < n_states; ++j) {
+    const pr_beam_state& s = states[j];
+    if (s.row_bytes < 0 || s.row_stride < s.row_bytes || (n > 0 && s.row_stride > kMostBytes / n))
+      return PR_ERR_INVALID_ARG;
+    if (n > 0 && s.row_bytes > 0 && !s.rows) return PR_ERR_INVALID_ARG;
+  }
+  if (n_req == 0 || n_states == 0) return PR_OK;
+  if (!parent) return PR_ERR_INVALID_ARG;
+  try {
+    // By their first byte: a state can share bytes only with those that start before its end.
+    std::vector<pr_beam_state> by(states, states + n_states);
+    std::sort(by.begin(), by.end(), [](const pr_beam_state& a, const pr_beam_state& b) {
+      return reinterpret_cast<uintptr_t>(a.rows) < reinterpret_cast<uintptr_t>(b.rows);
+    });
+    for (size_t i = 0; i < by.size(); ++i) {
+      if (by[i].row_bytes == 0) continue;
+      const uintptr_t end =
+          reinterpret_cast<uintptr_t>(by[i].rows) + static_cast<uintptr_t>((n - 1) * by[i].row_stride + by[i].row_bytes);
+      for (size_t j = i + 1; j < by.size() && reinterpret_cast<uintptr_t>(by[j].rows) < end; ++j)
+        if (by[j].row_bytes > 0 && states_overlap(by[i], by[j], n)) return PR_ERR_INVALID_ARG;
+    }
+  } catch (...) {
+    return PR_ERR_NO_MEMORY;
+  }
+  for (int32_t at = 0; at < n_states; at += kStates) {
+    StateList list{};
+    for (int32_t j = at; j < n_states && j < at + kStates; ++j)
+      if (states[j].row_bytes > 0) list.s[list.n++] = states[j];
+    if (list.n == 0) continue;
+    const hipError_t e = launch_reorder(list, nullptr, 0, parent, n_req, n_beams, as_stream(stream));
+    if (e != hipSuccess) return hip_status(e);
+  }
+  return PR_OK;
 }
 
 void pr_policy_params_default(pr_policy_params* params) {
@@ -643,6 +794,47 @@ pr_status pr_preference_loss(const void* logits, pr_dtype dtype, int64_t n_rows,
   a.G = preference_split(n_rows, vocab, dtype);
   a.ws = workspace;
   return hip_status(launch_preference(a, dtype, as_stream(stream)));
+}
+
+void pr_distill_params_default(pr_distill_params* params) {
+  if (params) *params = pr_distill_params{PR_TAIL_REST, 1.0};
+}
+
+size_t pr_distill_loss_workspace(pr_dtype dtype, int64_t n_rows, int32_t vocab, int32_t k) {
+  (void)k;
+  return vocab < 2 ? 0 : distill_workspace_bytes(n_rows, vocab, dtype);
+}
+
+pr_status pr_distill_loss(const void* logits, pr_dtype dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,
+                          const int32_t* top_ids, const float* top_logprob, int32_t k, int64_t top_stride,
+                          const float* temperature, const float* weight, const pr_distill_params* params, float* loss,
+                          const pr_distill_tokens_t* out, void* grad, int64_t grad_stride, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  // The rows' ids may be missing where there are no entries.
+  const int32_t* ids = k > 0 ? top_ids : reinterpret_cast<const int32_t*>(weight);
+  const pr_status st =
+      check_loss(logits, dtype, n_rows, vocab, row_stride, ids, temperature, weight, loss, grad, grad_stride);
+  if (st != PR_OK) return st;
+  if (k < 0 || k > PR_MAX_TOP_LOGITS || top_stride < k || (k > 0 && n_rows > 0 && !top_logprob))
+    return PR_ERR_INVALID_ARG;
+  pr_distill_params p;
+  pr_distill_params_default(&p);
+  if (params) p = *params;
+  if (p.tail < PR_TAIL_DROP || p.tail > PR_TAIL_REST || !std::isfinite(p.grad_scale)) return PR_ERR_INVALID_ARG;
+  const size_t need = pr_distill_loss_workspace(dtype, n_rows, vocab, k);
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return PR_ERR_INVALID_ARG;
+  DistillArgs a{};
+  a.rows = loss_rows(logits, n_rows, vocab, row_stride, nullptr, temperature, weight, grad, grad_stride);
+  a.top_ids = top_ids;
+  a.top_logprob = top_logprob;
+  a.k = k;
+  a.top_stride = top_stride;
+  a.tail = p.tail;
+  a.grad_scale = p.grad_scale;
+  a.loss = loss;
+  if (out) a.out = *out;
+  a.ws = workspace;
+  return hip_status(launch_distill(a, dtype, as_stream(stream)));
 }
 
 pr_status pr_adamw_create(const pr_adamw_tensor* tensors, int32_t n_tensors, pr_dtype param_dtype,

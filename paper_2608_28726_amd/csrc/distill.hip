@@ -1,0 +1,375 @@
+// The loss of a student's logit rows against a teacher's largest log-probs, and
+// its gradient in the logits.
+//
+// A row's entries are the teacher's tokens v_i with q_i = exp(their log-prob).
+// With u = z / T, p = softmax(u), Q = sum q_i, P = sum p_{v_i}, r_p = 1 - P and
+// r_q = max(0, 1 - Q) (0 unless the rest is a term, and where r_p = 0):
+//   l = sum q_i (log q_i - log p_{v_i}) + r_q (log r_q - log r_p)
+//   dl/du_v = (Q + r_q) p_v - q_i             v = v_i
+//           = (Q r_p - r_q P) (p_v / r_p)     any other v
+// (q_i and Q divided by Q where the entries are normalised.)
+//
+// The sum over the tokens that are no entry's is taken on its own, relative to
+// its own largest logit: 1 - P would keep nothing of it where the student is
+// sure of the teacher's tokens, and the two factors above are finite at any r_p.
+// The vectors that hold entries' tokens are marked in a bit map, which the pass
+// over the row leaves out; a thread for each takes those.
+//
+// Exponents are in base 2 and sums as in the other losses: float32 sums of
+// positive terms, compensated per lane; what follows per row and over rows is
+// in 64 bits. A gradient element is rounded to its type once.
+#include "distill.h"
+#include "row_sum.h"
+
+namespace pr {
+namespace {
+
+constexpr int kMaxTop = PR_MAX_TOP_LOGITS;
+constexpr int kStatsBlock = 256;  // a thread for each of a row's entries
+constexpr int kGradBlock = 512;
+constexpr int kWindow = 1 << 15;  // vectors of a bit map
+static_assert(kStatsBlock >= kMaxTop && kGradBlock >= kMaxTop, "a thread for each entry");
+
+// What the gradient pass needs of a row: dz_v = k 2^fma(z_v, c, -A) outside the
+// entries, in_k 2^fma(z_v, c, -in_A) - q_k q_i in them. All factors 0: the
+// gradient is zero and the row is not read.
+struct alignas(16) RowDistill {
+  float A, k, in_A, in_k, c, q_k;
+  uint32_t pad[2];
+};
+
+// Sums over the entries.
+struct EntrySums {
+  double Q, cross;  // sum q, sum q (log q - u)
+};
+
+// A row's loss from its sums. part: of the tokens of the entries and of the others.
+struct RowLoss {
+  double loss, mass;
+  uint32_t flags;
+  RowDistill grad;
+};
+
+// log of a sum of exps, in 64 bits. S is relative to A = round(m c), whose
+// exact residual goes off its logarithm.
+__device__ __forceinline__ double log_sum(const RowSum& p, float T, float c) {
+  if (!(p.S > 0.0f)) return -__longlong_as_double(0x7ff0000000000000ll);
+  const float A = p.m * c;
+  const double delta = static_cast<double>(fmaf(p.m, c, -A));
+  return static_cast<double>(p.m) / static_cast<double>(T) + log(static_cast<double>(p.S)) -
+         delta * 0.69314718055994530942;
+}
+
+__device__ __forceinline__ RowLoss row_loss(const DistillArgs& a, const RowSum& in, const RowSum& out, const EntrySums& e,
+                                            uint32_t bad, float T, float c, float w) {
+  RowLoss x;
+  x.flags = bad;
+  if (!temperature_ok(T)) x.flags |= PR_FLAG_BAD_TP;
+  const float m = fmaxf(in.m, out.m);
+  if (!(fabsf(in.S) < INFINITY) || !(fabsf(out.S) < INFINITY) || m == INFINITY || m == -INFINITY)
+    x.flags |= PR_FLAG_NONFINITE;
+  if (!x.flags && fabsf(m) > ldexpf(T, 100)) x.flags |= PR_FLAG_BAD_TP;
+  if (x.flags) {
+    const float nan = __uint_as_float(0x7fc00000u);
+    x.loss = x.mass = __longlong_as_double(0x7ff8000000000000ll);
+    x.grad = RowDistill{0.0f, nan, 0.0f, nan, 0.0f, nan, {0, 0}};
+    return x;
+  }
+  const double li = log_sum(in, T, c), lo = log_sum(out, T, c);
+  const double hi = fmax(li, lo), lse = hi + log1p(exp(fmin(li, lo) - hi));
+  const double P = exp(li - lse), rp = exp(lo - lse);
+  const bool norm = a.tail == PR_TAIL_RENORM;
+  double Q = e.Q, rq = 0.0, scale = 1.0;
+  x.loss = e.cross + Q * lse;
+  if (norm) {
+    scale = Q > 0.0 ? 1.0 / Q : 0.0;
+    x.loss = Q > 0.0 ? x.loss / Q - log(Q) : 0.0;
+    Q = Q > 0.0 ? 1.0 : 0.0;
+  } else if (a.tail == PR_TAIL_REST && out.S > 0.0f) {
+    rq = fmax(0.0, 1.0 - Q);
+    if (rq > 0.0) x.loss += rq * (log(rq) - (lo - lse));
+  }
+  x.mass = P;
+  const double coef = a.grad_scale * static_cast<double>(w) / static_cast<double>(T);
+  RowDistill& g = x.grad;
+  g.c = c;
+  g.A = out.S > 0.0f ? out.m * c : 0.0f;
+  g.k = out.S > 0.0f ? static_cast<float>(coef * (Q * rp - rq * P) / static_cast<double>(out.S)) : 0.0f;
+  g.in_A = in.S > 0.0f ? in.m * c : 0.0f;
+  g.in_k = in.S > 0.0f ? static_cast<float>(coef * (Q + rq) * P / static_cast<double>(in.S)) : 0.0f;
+  g.q_k = static_cast<float>(coef * scale);
+  g.pad[0] = g.pad[1] = 0;
+  return x;
+}
+
+__device__ __forceinline__ RowLoss masked_row() {
+  return RowLoss{0.0, 0.0, PR_FLAG_MASKED, RowDistill{0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, {0, 0}}};
+}
+
+__device__ __forceinline__ void write_row(const DistillArgs& a, int64_t r, const RowLoss& x) {
+  if (a.out.token_loss) a.out.token_loss[r] = static_cast<float>(x.loss);
+  if (a.out.mass) a.out.mass[r] = static_cast<float>(x.mass);
+  if (a.out.flags) a.out.flags[r] = x.flags;
+}
+
+template <typename Tin>
+__device__ __forceinline__ const Tin* row_ptr(const LossRows& a, int64_t r) {
+  return static_cast<const Tin*>(a.logits) + r * a.row_stride;
+}
+
+// Entry i of a row: its token (-1: none, or out of range), its log-prob and
+// what is wrong with it.
+struct Entry {
+  int32_t id;
+  float logq;
+  uint32_t bad;
+};
+
+__device__ __forceinline__ Entry load_entry(const DistillArgs& a, int64_t r, int i) {
+  Entry e{-1, -INFINITY, 0};
+  if (i >= a.k) return e;
+  const float lq = a.top_logprob[r * a.top_stride + i];
+  if (lq == -INFINITY) return e;
+  const int32_t id = a.top_ids[r * a.top_stride + i];
+  if (!(lq < INFINITY)) e.bad |= PR_FLAG_NONFINITE;
+  if (id < 0 || id >= a.rows.V) e.bad |= PR_FLAG_BAD_ID;
+  if (!e.bad) {
+    e.id = id;
+    e.logq = lq;
+  }
+  return e;
+}
+
+// The stretch of up to VEC elements that a token belongs to: an aligned vector,
+// or the elements before or after them all.
+struct Group {
+  int32_t base, len, vec;  // vec: -1 before the vectors, -2 after them
+};
+
+template <typename Tin>
+__device__ __forceinline__ Group group_of(int32_t id, int32_t h, int32_t tail, int32_t V) {
+  constexpr int VEC = Elem<Tin>::kVec;
+  if (id < h) return Group{0, h, -1};
+  if (id >= tail) return Group{tail, V - tail, -2};
+  const int32_t j = (id - h) / VEC;
+  return Group{h + j * VEC, VEC, j};
+}
+
+// Sums of two doubles over the workgroup; every thread gets them.
+template <int BLOCK>
+__device__ __forceinline__ EntrySums sum_entries(EntrySums e) {
+  constexpr int NW = BLOCK / kWave;
+  __shared__ EntrySums sh[NW];
+  e.Q = wave_sum_d(e.Q);
+  e.cross = wave_sum_d(e.cross);
+  if (threadIdx.x % kWave == 0) sh[threadIdx.x / kWave] = e;
+  __syncthreads();
+  EntrySums t{0.0, 0.0};
+  for (int w = 0; w < NW; ++w) {
+    t.Q += sh[w].Q;
+    t.cross += sh[w].cross;
+  }
+  return t;
+}
+
+// One workgroup per row: its sums and everything but its gradient.
+template <typename Tin>
+__global__ __launch_bounds__(kStatsBlock) void distill_stats_kernel(DistillArgs a, double* term, RowDistill* rd,
+                                                                   int64_t first) {
+  constexpr int VEC = Elem<Tin>::kVec;
+  __shared__ alignas(16) int32_t sh_id[kMaxTop];
+  __shared__ uint32_t marks[kWindow / 32];
+  __shared__ uint32_t sh_bad, sh_ends;
+  const int64_t r = first + blockIdx.x;
+  const int t = threadIdx.x;
+  const float w = a.rows.weight[r];
+  if (w == 0.0f) {
+    if (t == 0) {
+      const RowLoss x = masked_row();
+      write_row(a, r, x);
+      term[r] = 0.0;
+      rd[r] = x.grad;
+    }
+    return;
+  }
+  const int32_t V = a.rows.V;
+  const Tin* row = row_ptr<Tin>(a.rows, r);
+  const float T = a.rows.temperature[r], c = scale_of(T);
+  const int32_t h = static_cast<int32_t>(head_elems<Tin>(row, V)), nvec = (V - h) / VEC, tail = h + nvec * VEC;
+  const vec4u* vp = reinterpret_cast<const vec4u*>(row + h);
+  const Entry e = load_entry(a, r, t);
+  const float z = e.id >= 0 ? Elem<Tin>::load1(row, e.id) : -INFINITY;
+  const Group g = group_of<Tin>(e.id, h, tail, V);
+  sh_id[t] = e.id;
+  if (t == 0) sh_bad = sh_ends = 0;
+  __syncthreads();
+  if (e.bad) atomicOr(&sh_bad, e.bad);
+  LaneSum<true> in, out;
+  in.add1(z, c);
+  // The first entry of a group takes the group's other elements.
+  {
+    float other[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) other[i] = -INFINITY;
+    if (e.id >= 0) {
+      uint32_t mine = 0;
+      bool owner = true, twice = false;
+      for (int i = 0; i < a.k; ++i) {
+        const int32_t o = sh_id[i], d = o - g.base;
+        if (o < 0 || d < 0 || d >= g.len) continue;
+        mine |= 1u << d;
+        if (i < t) owner = false;
+        if (i != t && o == e.id) twice = true;
+      }
+      if (twice) atomicOr(&sh_bad, PR_FLAG_BAD_ID);
+      if (owner) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+          if (i < g.len && !(mine >> i & 1u)) other[i] = Elem<Tin>::load1(row, g.base + i);
+        if (g.vec < 0) atomicOr(&sh_ends, g.vec == -1 ? 1u : 2u);
+      }
+    }
+    out.add(other, c);
+  }
+  __syncthreads();
+  const uint32_t ends = sh_ends;
+  out.add1(t < h && !(ends & 1u) ? Elem<Tin>::load1(row, t) : -INFINITY, c);
+  out.add1(t < V - tail && !(ends & 2u) ? Elem<Tin>::load1(row, tail + t) : -INFINITY, c);
+  for (int32_t w0 = 0; w0 < nvec; w0 += kWindow) {
+    const int32_t w1 = nvec - w0 < kWindow ? nvec : w0 + kWindow;
+    for (int i = t; i < kWindow / 32; i += kStatsBlock) marks[i] = 0;
+    __syncthreads();
+    if (e.id >= 0 && g.vec >= w0 && g.vec < w1) atomicOr(&marks[(g.vec - w0) / 32], 1u << (g.vec - w0) % 32);
+    __syncthreads();
+    vec4u v[4];
+    scan::stretch_prefetch<Tin, kStatsBlock, 4>(row, h, w0, w1, v);
+    scan::stream_stretch<Tin, kStatsBlock, 2, 4>(vp, w0, w1, v, [&](const vec4u* vv, int64_t j) {
+      float x[2 * VEC];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int32_t at = static_cast<int32_t>(j) + u * kStatsBlock - w0;
+        const bool marked = at < kWindow && (marks[at / 32] >> (at % 32) & 1u);
+        Elem<Tin>::unpack(marked ? neg_inf_vec<Tin>() : vv[u], x + u * VEC);
+      }
+      out.add(x, c);
+    });
+    __syncthreads();
+  }
+  const RowSum sum_in = merge_block<kStatsBlock>(in, c);
+  __syncthreads();
+  const RowSum sum_out = merge_block<kStatsBlock>(out, c);
+  // A probability of 0 adds nothing, whatever the student makes of its token.
+  const double q = e.id >= 0 ? exp(static_cast<double>(e.logq)) : 0.0;
+  EntrySums s{q, 0.0};
+  if (q > 0.0)
+    s.cross = q * (static_cast<double>(e.logq) - static_cast<double>(z) / static_cast<double>(T));
+  s = sum_entries<kStatsBlock>(s);
+  if (t != 0) return;
+  const RowLoss x = row_loss(a, sum_in, sum_out, s, sh_bad, T, c, w);
+  write_row(a, r, x);
+  term[r] = static_cast<double>(w) * x.loss;
+  rd[r] = x.grad;
+}
+
+// The gradients of the rows from `first` on (blockIdx.y), a vector per thread:
+// short workgroups in memory order, past the caches. Each finds the entries
+// among its own vectors.
+template <typename Tin>
+__global__ __launch_bounds__(kGradBlock) void distill_grad_kernel(DistillArgs a, const RowDistill* rd, int64_t first) {
+  constexpr int VEC = Elem<Tin>::kVec;
+  __shared__ int32_t sh_id[kMaxTop];
+  __shared__ float sh_q[kMaxTop];
+  __shared__ int sh_n;
+  const int64_t r = first + blockIdx.y;
+  const RowDistill q = rd[r];
+  const int part = blockIdx.x, t = threadIdx.x;
+  const int32_t V = a.rows.V;
+  const Tin* row = row_ptr<Tin>(a.rows, r);
+  Tin* out = static_cast<Tin*>(a.rows.grad) + r * a.rows.grad_stride;
+  const int32_t h = static_cast<int32_t>(head_elems<Tin>(row, V)), nvec = (V - h) / VEC, tail = h + nvec * VEC;
+  const int32_t j = part * kGradBlock + t;
+  const bool ends = part == 0 && t < 16;
+  const int32_t s = ends ? scalar_element(t, h, tail, V) : V;
+  if (q.k == 0.0f && q.in_k == 0.0f && q.q_k == 0.0f) {
+    if (s < V) GradVec<Tin>::store1(out, s, 0.0f);
+    if (j < nvec) stream_grad(out + h + static_cast<int64_t>(j) * VEC, vec4u{0, 0, 0, 0});
+    return;
+  }
+  vec4u v = neg_inf_vec<Tin>();
+  if (j < nvec) v = __builtin_nontemporal_load(reinterpret_cast<const vec4u*>(row + h) + j);
+  const float zs = s < V ? Elem<Tin>::load1(row, s) : 0.0f;
+  const Entry e = load_entry(a, r, t);
+  if (t == 0) sh_n = 0;
+  __syncthreads();
+  if (e.id >= 0) {
+    const Group g = group_of<Tin>(e.id, h, tail, V);
+    if (g.vec < 0 ? part == 0 : g.vec / kGradBlock == part) {
+      const int at = atomicAdd(&sh_n, 1);
+      sh_id[at] = e.id;
+      sh_q[at] = q.q_k * expf(e.logq);
+    }
+  }
+  __syncthreads();
+  const int n = sh_n;
+  if (s < V) {
+    float g = q.k * fast_exp2(fmaf(zs, q.c, -q.A));
+    for (int i = 0; i < n; ++i)
+      if (sh_id[i] == s) g = q.in_k * fast_exp2(fmaf(zs, q.c, -q.in_A)) - sh_q[i];
+    GradVec<Tin>::store1(out, s, g);
+  }
+  if (j >= nvec) return;
+  float z[VEC], g[VEC];
+  Elem<Tin>::unpack(v, z);
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) g[i] = q.k * fast_exp2(fmaf(z[i], q.c, -q.A));
+  const int32_t base = h + j * VEC;
+  for (int i = 0; i < n; ++i) {
+    const int32_t d = sh_id[i] - base;
+    if (d < 0 || d >= VEC) continue;
+#pragma unroll
+    for (int u = 0; u < VEC; ++u)
+      if (u == d) g[u] = q.in_k * fast_exp2(fmaf(z[u], q.c, -q.in_A)) - sh_q[i];
+  }
+  stream_grad(out + h + static_cast<int64_t>(j) * VEC, GradVec<Tin>::pack(g));
+}
+
+constexpr int64_t kMostGroups = int64_t{1} << 23;  // a grid holds less than 2^32 threads
+
+template <typename Tin>
+hipError_t distill(const DistillArgs& a, hipStream_t stream) {
+  const int64_t n = a.rows.n_rows;
+  RowDistill* rd = static_cast<RowDistill*>(a.ws);
+  double* term = reinterpret_cast<double*>(rd + n);
+  for (int64_t at = 0; at < n; at += kMostGroups) {
+    const int64_t rows = n - at < kMostGroups ? n - at : kMostGroups;
+    hipLaunchKernelGGL(distill_stats_kernel<Tin>, dim3(static_cast<unsigned>(rows)), dim3(kStatsBlock), 0, stream, a,
+                       term, rd, at);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.rows.grad) {
+    constexpr int64_t kMostY = 32768;
+    const int64_t nvec = a.rows.V / Elem<Tin>::kVec, parts = nvec > 0 ? (nvec + kGradBlock - 1) / kGradBlock : 1;
+    for (int64_t at = 0; at < n; at += kMostY) {
+      const int64_t rows = n - at < kMostY ? n - at : kMostY;
+      hipLaunchKernelGGL(distill_grad_kernel<Tin>, dim3(static_cast<unsigned>(parts), static_cast<unsigned>(rows)),
+                         dim3(kGradBlock), 0, stream, a, rd, at);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+  }
+  return launch_loss_sum(term, n, 1.0, a.loss, stream);
+}
+
+}  // namespace
+
+size_t distill_workspace_bytes(int64_t n_rows, int32_t, pr_dtype) {
+  const size_t n = n_rows < 0 ? 0 : static_cast<size_t>(n_rows);
+  return n * (sizeof(RowDistill) + sizeof(double));
+}
+
+hipError_t launch_distill(const DistillArgs& a, pr_dtype dtype, hipStream_t stream) {
+  return dtype == PR_BF16 ? distill<uint16_t>(a, stream) : distill<float>(a, stream);
+}
+
+}  // namespace pr

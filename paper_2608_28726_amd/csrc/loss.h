@@ -55,4 +55,7 @@ int preference_split(int64_t n_rows, int32_t V, pr_dtype dtype);
 size_t preference_workspace_bytes(int64_t n_rows, int32_t n_pairs, int32_t G);
 hipError_t launch_preference(const PreferenceArgs& a, pr_dtype dtype, hipStream_t stream);
 
+// loss[0] = (sum of v[0..n)) / over, in a fixed order.
+hipError_t launch_loss_sum(const double* v, int64_t n, double over, float* loss, hipStream_t stream);
+
 }  // namespace pr

@@ -1,0 +1,97 @@
+// Beam search's reordering of states: rows of bytes that take another row's
+// place within their request, in place.
+//
+// A thread owns 16 bytes of the rows of one request: it reads them of every row
+// that another row takes, then writes them, so that nothing is overwritten
+// before it is read and no scratch is needed. Rows that stay are neither read
+// (unless another takes them) nor written.
+#include "select.h"
+
+namespace pr {
+namespace {
+
+constexpr int kBlock = 256;
+
+// States start and end at any byte; global loads and stores need no alignment.
+typedef uint32_t Bytes16 __attribute__((ext_vector_type(4), aligned(1)));
+
+template <int MOST>
+__global__ __launch_bounds__(kBlock) void reorder_kernel(StateList states, const int32_t* rows, int32_t n_rows,
+                                                         const int32_t* parent, int32_t B) {
+  __shared__ int32_t sh_to[MOST], sh_from[MOST];
+  const int64_t first = static_cast<int64_t>(blockIdx.y) * B;
+  const pr_beam_state s = states.s[blockIdx.z];
+  if (threadIdx.x < MOST) {
+    const int b = threadIdx.x;
+    int32_t to = -1, from = -1;
+    if (b < B) {
+      const int32_t p = parent[first + b];
+      if (p >= 0 && p < B && p != b) {
+        to = rows ? rows[first + b] : static_cast<int32_t>(first + b);
+        from = rows ? rows[first + p] : static_cast<int32_t>(first + p);
+        if (to < 0 || to >= n_rows || from < 0 || from >= n_rows) to = -1;
+      }
+    }
+    sh_to[b] = to;
+    sh_from[b] = from;
+  }
+  __syncthreads();
+  char* const base = static_cast<char*>(s.rows);
+  const int64_t whole = s.row_bytes / 16;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kBlock;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x; i < whole; i += step) {
+    Bytes16 v[MOST];
+#pragma unroll
+    for (int b = 0; b < MOST; ++b)
+      if (sh_to[b] >= 0) v[b] = *reinterpret_cast<const Bytes16*>(base + sh_from[b] * s.row_stride + i * 16);
+#pragma unroll
+    for (int b = 0; b < MOST; ++b)
+      if (sh_to[b] >= 0) *reinterpret_cast<Bytes16*>(base + sh_to[b] * s.row_stride + i * 16) = v[b];
+  }
+  // The up to 15 bytes after them, one a thread.
+  const int64_t last = whole * 16 + threadIdx.x;
+  if (blockIdx.x == 0 && last < s.row_bytes) {
+    char v[MOST];
+#pragma unroll
+    for (int b = 0; b < MOST; ++b)
+      if (sh_to[b] >= 0) v[b] = base[sh_from[b] * s.row_stride + last];
+#pragma unroll
+    for (int b = 0; b < MOST; ++b)
+      if (sh_to[b] >= 0) base[sh_to[b] * s.row_stride + last] = v[b];
+  }
+}
+
+}  // namespace
+
+hipError_t launch_reorder(const StateList& states, const int32_t* rows, int32_t n_rows, const int32_t* parent,
+                          int32_t n_req, int32_t B, hipStream_t stream) {
+  int64_t most = 0;
+  for (int j = 0; j < states.n; ++j) most = states.s[j].row_bytes > most ? states.s[j].row_bytes : most;
+  const int64_t parts = (most / 16 + kBlock - 1) / kBlock;
+  constexpr int32_t kMostY = 32768;
+  for (int32_t at = 0; at < n_req; at += kMostY) {
+    const int32_t reqs = n_req - at < kMostY ? n_req - at : kMostY;
+    const dim3 grid(static_cast<unsigned>(parts < 1 ? 1 : parts > 64 ? 64 : parts), static_cast<unsigned>(reqs),
+                    static_cast<unsigned>(states.n));
+    StateList list = states;
+    const int64_t skip = static_cast<int64_t>(at) * B;
+    if (!rows)
+      for (int j = 0; j < list.n; ++j)
+        list.s[j].rows = static_cast<char*>(list.s[j].rows) + skip * list.s[j].row_stride;
+    auto run = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, stream, list, rows ? rows + skip : nullptr,
+                         rows ? n_rows : reqs * B, parent + skip, B);
+    };
+    if (B <= 8)
+      run(reorder_kernel<8>);
+    else if (B <= 32)
+      run(reorder_kernel<32>);
+    else
+      run(reorder_kernel<64>);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace pr
