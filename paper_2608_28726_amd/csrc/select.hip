@@ -100,43 +100,211 @@ __device__ Cut find_cut(Keys&& keys, uint32_t k, CutLds& s) {
   return c;
 }
 
-// The tokens of a row, for find_cut: every element's key.
-template <typename Tin, int BLOCK, typename Fn>
-__device__ __forceinline__ void row_keys(const Tin* row, int32_t V, Fn&& fn) {
-  constexpr int VEC = Elem<Tin>::kVec;
-  const int32_t h = static_cast<int32_t>(head_elems<Tin>(row, V)), nvec = (V - h) / VEC, tail = h + nvec * VEC;
-  const int t = threadIdx.x;
-  if (t < h) fn(place_key(Elem<Tin>::load1(row, t), t));
-  if (t < V - tail) fn(place_key(Elem<Tin>::load1(row, tail + t), tail + t));
-  for (int32_t j = t; j < nvec; j += BLOCK) {
-    float z[VEC];
-    Elem<Tin>::unpack(reinterpret_cast<const vec4u*>(row + h)[j], z);
-#pragma unroll
-    for (int u = 0; u < VEC; ++u) fn(place_key(z[u], h + j * VEC + u));
-  }
-}
+// A stretch of a row: its vectors [vb, ve), counted from element 0 wherever the
+// row lies (unaligned 16-byte loads), so that equal rows have equal sums; the
+// row's last stretch also has the elements after the vectors.
+template <typename Tin>
+struct Stretch {
+  static constexpr int VEC = Elem<Tin>::kVec;
+  typedef typename GradVec<Tin>::Store Vec;  // 16 bytes of an element's alignment
+  const Tin* row;
+  int32_t vb, ve, tail, n_tail;
 
-// The first k tokens of a row in no order, by one workgroup; returns how many there are.
-struct RowLds {
-  CutLds cut;
-  uint32_t n;
-  uint64_t key[kMaxTop];
+  __device__ __forceinline__ Stretch(const Tin* r, int32_t V, int g, int G) : row(r) {
+    const int64_t nvec = V / VEC;
+    vb = static_cast<int32_t>(nvec * g / G);
+    ve = static_cast<int32_t>(nvec * (g + 1) / G);
+    tail = static_cast<int32_t>(nvec * VEC);
+    n_tail = g == G - 1 ? V - tail : 0;
+  }
+  __device__ __forceinline__ const Vec* vectors() const { return reinterpret_cast<const Vec*>(row); }
+  __device__ __forceinline__ float tail_logit(int t) const { return t < n_tail ? Elem<Tin>::load1(row, tail + t) : -INFINITY; }
+  // fn(key) for each of the thread's elements.
+  template <int BLOCK, typename Fn>
+  __device__ __forceinline__ void keys(Fn&& fn) const {
+    fn(place_key(tail_logit(threadIdx.x), tail + threadIdx.x));
+    for (int32_t j = vb + static_cast<int32_t>(threadIdx.x); j < ve; j += BLOCK) {
+      float z[VEC];
+      Elem<Tin>::unpack(static_cast<vec4u>(vectors()[j]), z);
+#pragma unroll
+      for (int u = 0; u < VEC; ++u) fn(place_key(z[u], static_cast<int64_t>(j) * VEC + u));
+    }
+  }
 };
 
+constexpr int kCap = 2048;  // keys listed of a stretch
+
+template <int BLOCK>
+struct ListLds {
+  uint64_t key[kCap];
+  alignas(16) uint32_t hist[256];
+  CutLds cut;
+  float low[BLOCK / kWave], top[BLOCK / kWave];
+  float floor;  // at least k logits of the stretch are not below it
+  uint32_t n;
+};
+
+// The largest value, to 16 bits of its key, that at least j of the wave's
+// lanes' v are not below (-inf: there is none). j <= 64.
+__device__ __forceinline__ float wave_floor(float v, int j) {
+  const uint32_t key = float_key(v);
+  uint32_t at = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t up = at | 1u << bit;
+    if (__popcll(__ballot(key >= up)) >= j) at = up;
+  }
+  return at <= 0x007f0000u ? -INFINITY : key_float(at);
+}
+
+// Which of the 256 bins holds the k-th largest of what they count (0 where
+// there are fewer). One wave calls it.
+__device__ __forceinline__ int cut_bin(const uint32_t* hist, uint32_t k) {
+  const int l = static_cast<int>(__lane_id());  // bins 255 - 4l .. 252 - 4l
+  const vec4u n = *reinterpret_cast<const vec4u*>(hist + 252 - 4 * l);
+  const uint32_t incl = wave_incl_scan_u(n.x + n.y + n.z + n.w), before = incl - (n.x + n.y + n.z + n.w);
+  const uint64_t full = __ballot(incl >= k);
+  if (full == 0) return 0;
+  int bin = 252 - 4 * l;
+  if (before + n.w >= k)
+    bin += 3;
+  else if (before + n.w + n.z >= k)
+    bin += 2;
+  else if (before + n.w + n.z + n.y >= k)
+    bin += 1;
+  return __builtin_amdgcn_readlane(bin, static_cast<int>(__builtin_ctzll(full)));
+}
+
+// The k largest logits of a stretch and others beside them, as keys in s.key;
+// returns how many. One pass: the first vectors of all lanes give a floor that
+// k logits reach; from there on what reaches the floor is listed and counted in
+// 256 bins between it and the largest logit of the first vectors, and every
+// `k` listed logits the wave that lists the last of them raises the floor to the
+// bin that the k-th largest is in. The waves do not wait for each other: a floor
+// read late lists more. Rows in which far too many logits reach the floor (many
+// equal ones, or rising ones) are selected from by digits (find_cut).
 template <typename Tin, int BLOCK>
-__device__ int list_row(const Tin* row, int32_t V, int k, RowLds& s) {
-  // Of a bfloat16's key the low 16 bits follow from its sign.
-  constexpr uint32_t SKIP = sizeof(Tin) == 2 ? 0x0cu : 0u;
-  if (threadIdx.x == 0) s.n = 0;
-  const Cut cut = find_cut<BLOCK, SKIP>([&](auto fn) { row_keys<Tin, BLOCK>(row, V, fn); }, static_cast<uint32_t>(k),
-                                        s.cut);
-  row_keys<Tin, BLOCK>(row, V, [&](uint64_t key) {
-    if (!cut.takes(key)) return;
-    const uint32_t at = atomicAdd(&s.n, 1u);
-    if (at < static_cast<uint32_t>(kMaxTop)) s.key[at] = key;
-  });
+__device__ int list_stretch(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK>& s, RowSum* sum) {
+  constexpr int VEC = Elem<Tin>::kVec, NW = BLOCK / kWave, LD = 4;
+  const int t = threadIdx.x, wave = t / kWave;
+  const bool lead = t % kWave == 0;
+  vec4u v[LD];
+  scan::vector_prefetch<Tin, BLOCK, LD>(x.vectors(), x.vb, x.ve, v);
+  const float zt = x.tail_logit(t);
+  for (int i = t; i < 256; i += BLOCK) s.hist[i] = 0;
+  if (t == 0) s.n = 0;
+  float first = zt;
+#pragma unroll
+  for (int u = 0; u < LD; ++u) {
+    float z[VEC];
+    Elem<Tin>::unpack(v[u], z);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) first = fmaxf(first, z[i]);
+  }
+  const float low = wave_floor(first, (k + NW - 1) / NW), high = wave_max(first);
+  if (lead) {
+    s.low[wave] = low;
+    s.top[wave] = high;
+  }
   __syncthreads();
-  return static_cast<int>(min(s.n, static_cast<uint32_t>(k)));
+  float floor0 = s.low[0], top0 = s.top[0];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) {
+    floor0 = fminf(floor0, s.low[w]);
+    top0 = fmaxf(top0, s.top[w]);
+  }
+  floor0 = fmaxf(floor0, kNegSentinel);  // any finite logit
+  const float width = (top0 - floor0) * (1.0f / 255.0f), scale = width > 0.0f && width < INFINITY ? 1.0f / width : 0.0f;
+  auto bin_of = [&](float z) { return min(255, static_cast<int>(fmaxf((z - floor0) * scale, 0.0f))); };
+  if (t == 0) s.floor = floor0;
+  __syncthreads();
+
+  const uint32_t every = static_cast<uint32_t>(k < 64 ? 64 : k);
+  LaneSum<true> L;
+  auto list = [&](float z, int64_t i, bool& raise) {
+    const uint32_t at = atomicAdd(&s.n, 1u);
+    if (at < static_cast<uint32_t>(kCap)) {
+      s.key[at] = place_key(z, i);
+      atomicAdd(&s.hist[bin_of(z)], 1u);
+      raise |= at % every == every - 1;
+    } else {
+      raise = true;
+    }
+  };
+  auto raise_floor = [&](bool raise) {
+    if (!__any(raise)) return;
+    const int b = cut_bin(s.hist, static_cast<uint32_t>(k));
+    const bool full = s.n > static_cast<uint32_t>(kCap);  // list no more
+    // A sixteenth of a bin below its edge: the bins' own roundings are less.
+    const float f = full ? INFINITY : floor0 + (static_cast<float>(b) - 0.0625f) * width;
+    if ((b > 0 || full) && lead) __hip_atomic_store(&s.floor, f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  };
+  scan::stream_stretch<Tin, BLOCK, 2, LD>(x.vectors(), x.vb, x.ve, v, [&](const vec4u* vv, int64_t j) {
+    const float floor = __hip_atomic_load(&s.floor, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    float z[2 * VEC];
+    Elem<Tin>::unpack(vv[0], z);
+    Elem<Tin>::unpack(vv[1], z + VEC);
+    const float top = L.add(z, c);
+    if (!__any(top >= floor)) return;
+    bool raise = false;
+    if (top >= floor) {
+#pragma unroll
+      for (int i = 0; i < 2 * VEC; ++i)
+        if (z[i] >= floor) list(z[i], (j + (i / VEC) * BLOCK) * VEC + i % VEC, raise);
+    }
+    raise_floor(raise);
+  });
+  L.add1(zt, c);
+  bool unused = false;
+  if (zt >= floor0) list(zt, x.tail + t, unused);
+  *sum = merge_block<BLOCK>(L, c);  // its barrier ends the listing
+  const uint32_t n = s.n;
+  if (n > static_cast<uint32_t>(kCap)) {
+    // Of a bfloat16's key the low 16 bits follow from its sign.
+    constexpr uint32_t SKIP = sizeof(Tin) == 2 ? 0x0cu : 0u;
+    const Cut cut = find_cut<BLOCK, SKIP>([&](auto fn) { x.template keys<BLOCK>(fn); }, static_cast<uint32_t>(k), s.cut);
+    __syncthreads();
+    if (t == 0) s.n = 0;
+    __syncthreads();
+    x.template keys<BLOCK>([&](uint64_t key) {
+      if (!cut.takes(key)) return;
+      const uint32_t at = atomicAdd(&s.n, 1u);
+      if (at < static_cast<uint32_t>(kCap)) s.key[at] = key;
+    });
+    __syncthreads();
+    return static_cast<int>(min(s.n, static_cast<uint32_t>(k)));
+  }
+  if (n <= static_cast<uint32_t>(k) + 16) return static_cast<int>(n);
+  // Those from the k-th's bin on.
+  const int b = cut_bin(s.hist, static_cast<uint32_t>(k));
+  constexpr int PER = kCap / BLOCK;
+  uint64_t mine[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const uint32_t e = static_cast<uint32_t>(t + i * BLOCK);
+    mine[i] = e < n ? s.key[e] : 0;
+  }
+  __syncthreads();
+  if (t == 0) s.n = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (mine[i] != 0 && bin_of(key_logit(mine[i])) >= b) s.key[atomicAdd(&s.n, 1u)] = mine[i];
+  __syncthreads();
+  return static_cast<int>(s.n);
+}
+
+// The places of the n listed keys among themselves: fn(place, key) for each,
+// from 0, the largest's.
+template <int BLOCK, typename Fn>
+__device__ __forceinline__ void in_order(const uint64_t* key, int n, Fn&& fn) {
+  for (int e = threadIdx.x; e < n; e += BLOCK) {
+    const uint64_t mine = key[e];
+    int place = 0;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) place += key[i] > mine ? 1 : 0;
+    fn(place, mine);
+  }
 }
 
 // What log-probs of a row come from: log p of a logit is (z - m) / T - lnS.
@@ -162,40 +330,37 @@ __device__ __forceinline__ RowNorm row_norm(const RowSum& p, float T) {
   return x;
 }
 
-// Writes a row's first tokens in order from the n listed ones.
+// Writes a row's first k tokens in order from the n listed ones.
+template <int BLOCK>
 __device__ __forceinline__ void write_top(const TopArgs& a, int64_t r, const RowNorm& x, const uint64_t* key, int n) {
   const int t = threadIdx.x;
   const bool bad = x.flags != 0;
+  const float nan = __uint_as_float(0x7fc00000u);
   if (t == 0) {
-    if (a.lse) a.lse[r] = bad ? __uint_as_float(0x7fc00000u)
-                              : static_cast<float>(static_cast<double>(x.m) / static_cast<double>(x.T) + x.lnS);
+    if (a.lse) a.lse[r] = bad ? nan : static_cast<float>(static_cast<double>(x.m) / static_cast<double>(x.T) + x.lnS);
     if (a.flags) a.flags[r] = x.flags;
   }
-  if (t >= a.k) return;
-  int at = t;
-  int32_t id = -1;
-  float lp = bad ? __uint_as_float(0x7fc00000u) : -INFINITY;
-  if (!bad && t < n) {
-    const uint64_t mine = key[t];
-    at = 0;
-    for (int i = 0; i < n; ++i) at += key[i] > mine ? 1 : 0;
-    id = key_index(mine);
-    lp = static_cast<float>(x.logprob(key_logit(mine)));
+  if (bad) n = 0;
+  in_order<BLOCK>(key, n, [&](int place, uint64_t mine) {
+    if (place >= a.k) return;
+    a.ids[r * a.k + place] = key_index(mine);
+    a.logprob[r * a.k + place] = static_cast<float>(x.logprob(key_logit(mine)));
+  });
+  if (t >= n && t < a.k) {
+    a.ids[r * a.k + t] = -1;
+    a.logprob[r * a.k + t] = bad ? nan : -INFINITY;
   }
-  a.ids[r * a.k + at] = id;
-  a.logprob[r * a.k + at] = lp;
 }
 
-template <typename Tin>
-__global__ __launch_bounds__(kRowBlock) void top_kernel(TopArgs a, int64_t first) {
-  __shared__ RowLds s;
+template <typename Tin, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void top_kernel(TopArgs a, int64_t first) {
+  __shared__ ListLds<BLOCK> s;
   const int64_t r = first + blockIdx.x;
-  const Tin* row = static_cast<const Tin*>(a.logits) + r * a.row_stride;
   const float T = a.temperature[r];
-  const RowSum sum = stretch_sum<Tin, kRowBlock>(row, a.V, 0, 1, scale_of(T));
-  const RowNorm x = row_norm(sum, T);
-  const int n = x.flags ? 0 : list_row<Tin, kRowBlock>(row, a.V, a.k, s);
-  write_top(a, r, x, s.key, n);
+  const Stretch<Tin> x(static_cast<const Tin*>(a.logits) + r * a.row_stride, a.V, 0, 1);
+  RowSum sum;
+  const int n = list_stretch<Tin, BLOCK>(x, a.k, scale_of(T), s, &sum);
+  write_top<BLOCK>(a, r, row_norm(sum, T), s.key, n);
 }
 
 // ---------------------------------------------------------------------------
@@ -213,17 +378,21 @@ __device__ __forceinline__ bool beam_live(const BeamArgs& a, int64_t r, uint32_t
 // The first k tokens of each live beam's row, and its sum of exps.
 template <typename Tin>
 __global__ __launch_bounds__(kRowBlock) void beam_rows_kernel(BeamArgs a, RowSum* sums, uint64_t* list) {
-  __shared__ RowLds s;
+  __shared__ ListLds<kRowBlock> s;
   const int64_t r = blockIdx.x;
   uint32_t flags;
   if (!beam_live(a, r, &flags)) return;
-  const Tin* row = static_cast<const Tin*>(a.logits) + r * a.row_stride;
   const float T = a.temperature[r];
-  const RowSum sum = stretch_sum<Tin, kRowBlock>(row, a.V, 0, 1, scale_of(T));
-  const int n = row_norm(sum, T).flags ? 0 : list_row<Tin, kRowBlock>(row, a.V, a.k, s);
+  const Stretch<Tin> x(static_cast<const Tin*>(a.logits) + r * a.row_stride, a.V, 0, 1);
+  RowSum sum;
+  int n = list_stretch<Tin, kRowBlock>(x, a.k, scale_of(T), s, &sum);
+  if (row_norm(sum, T).flags) n = 0;
   const int t = threadIdx.x;
   if (t == 0) sums[r] = sum;
-  if (t < a.k) list[r * a.k + t] = t < n ? s.key[t] : 0;
+  in_order<kRowBlock>(s.key, n, [&](int place, uint64_t key) {
+    if (place < a.k) list[r * a.k + place] = key;
+  });
+  if (t >= n && t < a.k) list[r * a.k + t] = 0;
 }
 
 // A candidate of a request in the order of the selection: score, lower beam,
@@ -331,7 +500,7 @@ template <typename Tin>
 hipError_t top(const TopArgs& a, hipStream_t stream) {
   for (int64_t at = 0; at < a.n_rows; at += kMostGroups) {
     const int64_t rows = a.n_rows - at < kMostGroups ? a.n_rows - at : kMostGroups;
-    hipLaunchKernelGGL(top_kernel<Tin>, dim3(static_cast<unsigned>(rows)), dim3(kRowBlock), 0, stream, a, at);
+    hipLaunchKernelGGL((top_kernel<Tin, kRowBlock>), dim3(static_cast<unsigned>(rows)), dim3(kRowBlock), 0, stream, a, at);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
