@@ -27,12 +27,16 @@ template <bool LONG>
 struct LaneSum {
   float mw = -INFINITY, a = kNegSentinel, s = 0.0f, over = 0.0f;
 
-  // Returns the largest of z.
   template <int N>
-  __device__ __forceinline__ float add(const float (&z)[N], float c) {
+  __device__ __forceinline__ void add(const float (&z)[N], float c) {
     float top = z[0];
 #pragma unroll
     for (int k = 1; k < N; ++k) top = fmaxf(top, z[k]);
+    add_top(z, top, c);
+  }
+  // top: the largest of z.
+  template <int N>
+  __device__ __forceinline__ void add_top(const float (&z)[N], float top, float c) {
     if (__any(top > mw)) {
       mw = fmaxf(mw, wave_max(top));
       // A mask of the type's lowest value may overflow here: it adds nothing
@@ -56,7 +60,6 @@ struct LaneSum {
     } else {
       s += s0 + s1;
     }
-    return top;
   }
   __device__ __forceinline__ void add1(float z, float c) {
     const float v[1] = {z};

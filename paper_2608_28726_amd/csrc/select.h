@@ -17,6 +17,7 @@ struct TopArgs {
   float* logprob;  // [n_rows][k]
   float* lse;      // [n_rows]
   uint32_t* flags;
+  int G;  // workgroups per row (set by the launch)
   void* ws;
 };
 
@@ -31,6 +32,7 @@ struct BeamArgs {
   int32_t done_token;
   int32_t k;
   pr_beam_out_t out;
+  int G;  // workgroups per row (set by the launch)
   void* ws;
 };
 

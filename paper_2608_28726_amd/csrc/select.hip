@@ -34,6 +34,13 @@ __device__ __forceinline__ uint64_t score_key(double s) {
   return b >> 63 ? ~b : b | 0x8000000000000000ull;
 }
 
+// The same to float32: keys in one order have theirs in the same or equal. 0 stays 0.
+__device__ __forceinline__ uint32_t near_key(uint64_t k) {
+  if (k == 0) return 0;
+  const uint64_t b = k >> 63 ? k & 0x7fffffffffffffffull : ~k;
+  return float_key(static_cast<float>(__longlong_as_double(static_cast<long long>(b))));
+}
+
 struct CutLds {
   uint32_t hist[256];
   uint32_t digit, need, bin, total;
@@ -132,27 +139,47 @@ struct Stretch {
   }
 };
 
-constexpr int kCap = 2048;  // keys listed of a stretch
+// What a stretch lists: vectors, later keys in their place. KMAX: the largest k
+// that the lists are made for (a row of ordinary logits lists about
+// k (1 + log(the row / the first vectors)) vectors).
+template <int KMAX>
+constexpr int list_cap() {
+  return KMAX <= 64 ? 768 : 2048;
+}
 
-template <int BLOCK>
+template <int BLOCK, int KMAX>
 struct ListLds {
-  uint64_t key[kCap];
+  static constexpr int CAP = list_cap<KMAX>();  // vectors
+  static constexpr int KEYS = 2 * CAP;          // keys in the vectors' place
+  union {
+    struct {
+      vec4u vec[CAP];
+      int32_t at[CAP];
+    };
+    alignas(16) uint64_t key[KEYS + 4];
+  };
   alignas(16) uint32_t hist[256];
   CutLds cut;
-  float low[BLOCK / kWave], top[BLOCK / kWave];
+  float low[BLOCK / kWave], top[BLOCK / kWave], bottom[BLOCK / kWave];
   float floor;  // at least k logits of the stretch are not below it
   uint32_t n;
 };
 
-// The largest value, to 16 bits of its key, that at least j of the wave's
-// lanes' v are not below (-inf: there is none). j <= 64.
-__device__ __forceinline__ float wave_floor(float v, int j) {
-  const uint32_t key = float_key(v);
+// The largest value, to 16 bits of its key, that at least j of the N values of
+// each of the wave's lanes are not below (-inf: there is none). j <= 64 N.
+template <int N>
+__device__ __forceinline__ float wave_floor(const float (&v)[N], int j) {
+  uint32_t key[N];
+#pragma unroll
+  for (int u = 0; u < N; ++u) key[u] = float_key(v[u]);
   uint32_t at = 0;
 #pragma unroll
   for (int bit = 31; bit >= 16; --bit) {
     const uint32_t up = at | 1u << bit;
-    if (__popcll(__ballot(key >= up)) >= j) at = up;
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < N; ++u) n += __popcll(__ballot(key[u] >= up));
+    if (n >= j) at = up;
   }
   return at <= 0x007f0000u ? -INFINITY : key_float(at);
 }
@@ -175,17 +202,40 @@ __device__ __forceinline__ int cut_bin(const uint32_t* hist, uint32_t k) {
   return __builtin_amdgcn_readlane(bin, static_cast<int>(__builtin_ctzll(full)));
 }
 
-// The k largest logits of a stretch and others beside them, as keys in s.key;
+// The places of the n listed keys among themselves: fn(place, key) for each,
+// from 0, the largest's. The list is 16-byte aligned and closed by four zeros
+// (close_list, after which the threads have met).
+__device__ __forceinline__ int close_list(uint64_t* key, int n) {
+  if (threadIdx.x < 4) key[n + threadIdx.x] = 0;
+  __syncthreads();
+  return n;
+}
+typedef uint64_t Keys2 __attribute__((ext_vector_type(2)));
+template <int BLOCK, typename Fn>
+__device__ __forceinline__ void in_order(const uint64_t* key, int n, Fn&& fn) {
+  const Keys2* pair = reinterpret_cast<const Keys2*>(key);
+  for (int e = threadIdx.x; e < n; e += BLOCK) {
+    const uint64_t mine = key[e];
+    int place = 0;
+    for (int i = 0; i < n; i += 4) {
+      const Keys2 p = pair[i / 2], q = pair[i / 2 + 1];
+      place += (p.x > mine ? 1 : 0) + (p.y > mine ? 1 : 0) + (q.x > mine ? 1 : 0) + (q.y > mine ? 1 : 0);
+    }
+    fn(place, mine);
+  }
+}
+
+// The k largest logits of a stretch and a few beside them, as keys in s.key;
 // returns how many. One pass: the first vectors of all lanes give a floor that
-// k logits reach; from there on what reaches the floor is listed and counted in
-// 256 bins between it and the largest logit of the first vectors, and every
-// `k` listed logits the wave that lists the last of them raises the floor to the
-// bin that the k-th largest is in. The waves do not wait for each other: a floor
-// read late lists more. Rows in which far too many logits reach the floor (many
-// equal ones, or rising ones) are selected from by digits (find_cut).
-template <typename Tin, int BLOCK>
-__device__ int list_stretch(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK>& s, RowSum* sum) {
-  constexpr int VEC = Elem<Tin>::kVec, NW = BLOCK / kWave, LD = 4;
+// k logits reach; from there on every vector with a logit that reaches the floor
+// is listed, and its largest logit counted in 256 bins between the floor and the
+// largest of the first vectors; the wave that lists a k-th one raises the floor
+// to the bin that the k-th largest counted is in. The waves do not wait for each
+// other: a floor read late lists more. Rows in which far too many vectors reach
+// the floor (many equal logits, or rising ones) are selected from by digits.
+template <typename Tin, int BLOCK, int KMAX>
+__device__ int list_stretch(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK, KMAX>& s, RowSum* sum) {
+  constexpr int VEC = Elem<Tin>::kVec, NW = BLOCK / kWave, LD = 4, CAP = ListLds<BLOCK, KMAX>::CAP;
   const int t = threadIdx.x, wave = t / kWave;
   const bool lead = t % kWave == 0;
   vec4u v[LD];
@@ -193,118 +243,152 @@ __device__ int list_stretch(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK
   const float zt = x.tail_logit(t);
   for (int i = t; i < 256; i += BLOCK) s.hist[i] = 0;
   if (t == 0) s.n = 0;
-  float first = zt;
+  auto largest = [](const float (&z)[VEC]) {
+    float m = z[0];
+#pragma unroll
+    for (int i = 1; i < VEC; ++i) m = fmaxf(m, z[i]);
+    return m;
+  };
+  float first[LD];  // each vector's largest
 #pragma unroll
   for (int u = 0; u < LD; ++u) {
     float z[VEC];
     Elem<Tin>::unpack(v[u], z);
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) first = fmaxf(first, z[i]);
+    first[u] = fmaxf(largest(z), u == 0 ? zt : -INFINITY);
   }
-  const float low = wave_floor(first, (k + NW - 1) / NW), high = wave_max(first);
+  const float low = wave_floor(first, (k + NW - 1) / NW);
+  float high = first[0], least = INFINITY;
+#pragma unroll
+  for (int u = 0; u < LD; ++u) {
+    high = fmaxf(high, first[u]);
+    least = fminf(least, first[u] > -INFINITY ? first[u] : INFINITY);
+  }
+  high = wave_max(high);
+  least = -wave_max(-least);
   if (lead) {
     s.low[wave] = low;
     s.top[wave] = high;
+    s.bottom[wave] = least;
   }
   __syncthreads();
-  float floor0 = s.low[0], top0 = s.top[0];
+  float floor0 = s.low[0], top0 = s.top[0], bin0 = s.bottom[0];
 #pragma unroll
   for (int w = 1; w < NW; ++w) {
     floor0 = fminf(floor0, s.low[w]);
     top0 = fmaxf(top0, s.top[w]);
+    bin0 = fminf(bin0, s.bottom[w]);
   }
-  floor0 = fmaxf(floor0, kNegSentinel);  // any finite logit
-  const float width = (top0 - floor0) * (1.0f / 255.0f), scale = width > 0.0f && width < INFINITY ? 1.0f / width : 0.0f;
-  auto bin_of = [&](float z) { return min(255, static_cast<int>(fmaxf((z - floor0) * scale, 0.0f))); };
+  // Where many vectors are masked whole any finite logit is listed, and the bins
+  // start at the least vector's largest.
+  bin0 = floor0 > -INFINITY ? floor0 : bin0;
+  floor0 = fmaxf(floor0, kNegSentinel);
+  const float width = (top0 - bin0) * (1.0f / 255.0f), scale = width > 0.0f && width < INFINITY ? 1.0f / width : 0.0f;
+  auto bin_of = [&](float z) { return min(255, static_cast<int>(fmaxf((z - bin0) * scale, 0.0f))); };
   if (t == 0) s.floor = floor0;
   __syncthreads();
 
   const uint32_t every = static_cast<uint32_t>(k < 64 ? 64 : k);
-  LaneSum<true> L;
-  auto list = [&](float z, int64_t i, bool& raise) {
-    const uint32_t at = atomicAdd(&s.n, 1u);
-    if (at < static_cast<uint32_t>(kCap)) {
-      s.key[at] = place_key(z, i);
-      atomicAdd(&s.hist[bin_of(z)], 1u);
-      raise |= at % every == every - 1;
-    } else {
-      raise = true;
+  auto list = [&](const vec4u& p, int32_t at, float top, bool& raise) {
+    const uint32_t n = atomicAdd(&s.n, 1u);
+    raise |= n >= static_cast<uint32_t>(CAP) || n % every == every - 1;
+    if (n < static_cast<uint32_t>(CAP)) {
+      s.vec[n] = p;
+      s.at[n] = at;
+      atomicAdd(&s.hist[bin_of(top)], 1u);
     }
   };
-  auto raise_floor = [&](bool raise) {
-    if (!__any(raise)) return;
-    const int b = cut_bin(s.hist, static_cast<uint32_t>(k));
-    const bool full = s.n > static_cast<uint32_t>(kCap);  // list no more
-    // A sixteenth of a bin below its edge: the bins' own roundings are less.
-    const float f = full ? INFINITY : floor0 + (static_cast<float>(b) - 0.0625f) * width;
-    if ((b > 0 || full) && lead) __hip_atomic_store(&s.floor, f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-  };
+  LaneSum<true> L;
   scan::stream_stretch<Tin, BLOCK, 2, LD>(x.vectors(), x.vb, x.ve, v, [&](const vec4u* vv, int64_t j) {
     const float floor = __hip_atomic_load(&s.floor, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-    float z[2 * VEC];
-    Elem<Tin>::unpack(vv[0], z);
-    Elem<Tin>::unpack(vv[1], z + VEC);
-    const float top = L.add(z, c);
-    if (!__any(top >= floor)) return;
-    bool raise = false;
-    if (top >= floor) {
+    float z[2 * VEC], top[2];
 #pragma unroll
-      for (int i = 0; i < 2 * VEC; ++i)
-        if (z[i] >= floor) list(z[i], (j + (i / VEC) * BLOCK) * VEC + i % VEC, raise);
+    for (int u = 0; u < 2; ++u) {
+      float y[VEC];
+      Elem<Tin>::unpack(vv[u], y);
+      top[u] = largest(y);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) z[u * VEC + i] = y[i];
     }
-    raise_floor(raise);
+    const float both = fmaxf(top[0], top[1]);
+    L.add_top(z, both, c);
+    if (!__any(both >= floor)) return;
+    bool raise = false;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (top[u] >= floor) list(vv[u], (static_cast<int32_t>(j) + u * BLOCK) * VEC, top[u], raise);
+    if (!__any(raise)) return;
+    const int b = cut_bin(s.hist, static_cast<uint32_t>(k));
+    const bool full = s.n > static_cast<uint32_t>(CAP);  // list no more
+    // A sixteenth of a bin below its edge: the bins' own roundings are less.
+    const float f = full ? INFINITY : bin0 + (static_cast<float>(b) - 0.0625f) * width;
+    if ((b > 0 || full) && lead) __hip_atomic_store(&s.floor, f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
   });
   L.add1(zt, c);
-  bool unused = false;
-  if (zt >= floor0) list(zt, x.tail + t, unused);
   *sum = merge_block<BLOCK>(L, c);  // its barrier ends the listing
-  const uint32_t n = s.n;
-  if (n > static_cast<uint32_t>(kCap)) {
-    // Of a bfloat16's key the low 16 bits follow from its sign.
-    constexpr uint32_t SKIP = sizeof(Tin) == 2 ? 0x0cu : 0u;
-    const Cut cut = find_cut<BLOCK, SKIP>([&](auto fn) { x.template keys<BLOCK>(fn); }, static_cast<uint32_t>(k), s.cut);
-    __syncthreads();
+  uint32_t n = s.n;
+  auto digits = [&](auto keys) {  // exactly the k largest of the keys that keys(fn) passes
+    constexpr uint32_t SKIP = sizeof(Tin) == 2 ? 0x0cu : 0u;  // of a bfloat16's key the low 16 bits follow from its sign
+    const Cut cut = find_cut<BLOCK, SKIP>(keys, static_cast<uint32_t>(k), s.cut);
     if (t == 0) s.n = 0;
     __syncthreads();
-    x.template keys<BLOCK>([&](uint64_t key) {
-      if (!cut.takes(key)) return;
-      const uint32_t at = atomicAdd(&s.n, 1u);
-      if (at < static_cast<uint32_t>(kCap)) s.key[at] = key;
+    keys([&](uint64_t key) {
+      if (cut.takes(key)) s.key[atomicAdd(&s.n, 1u)] = key;
     });
     __syncthreads();
-    return static_cast<int>(min(s.n, static_cast<uint32_t>(k)));
+    return close_list(s.key, static_cast<int>(s.n));
+  };
+  auto row_keys = [&](auto fn) { x.template keys<BLOCK>(fn); };
+  if (n > static_cast<uint32_t>(CAP)) {
+    __syncthreads();
+    return digits(row_keys);
   }
-  if (n <= static_cast<uint32_t>(k) + 16) return static_cast<int>(n);
-  // Those from the k-th's bin on.
+  // The listed vectors' logits from the k-th's bin on.
   const int b = cut_bin(s.hist, static_cast<uint32_t>(k));
-  constexpr int PER = kCap / BLOCK;
-  uint64_t mine[PER];
+  constexpr int PER = CAP / BLOCK;
+  vec4u mine[PER];
+  int32_t at[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const uint32_t e = static_cast<uint32_t>(t + i * BLOCK);
-    mine[i] = e < n ? s.key[e] : 0;
+    mine[i] = e < n ? s.vec[e] : neg_inf_vec<Tin>();
+    at[i] = e < n ? s.at[e] : 0;
   }
   __syncthreads();
   if (t == 0) s.n = 0;
   __syncthreads();
+  auto keep = [&](float z, int32_t i) {
+    if (!(z > -INFINITY) || bin_of(z) < b) return;
+    const uint32_t m = atomicAdd(&s.n, 1u);
+    if (m < static_cast<uint32_t>(ListLds<BLOCK, KMAX>::KEYS)) s.key[m] = place_key(z, i);
+  };
 #pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (mine[i] != 0 && bin_of(key_logit(mine[i])) >= b) s.key[atomicAdd(&s.n, 1u)] = mine[i];
-  __syncthreads();
-  return static_cast<int>(s.n);
-}
-
-// The places of the n listed keys among themselves: fn(place, key) for each,
-// from 0, the largest's.
-template <int BLOCK, typename Fn>
-__device__ __forceinline__ void in_order(const uint64_t* key, int n, Fn&& fn) {
-  for (int e = threadIdx.x; e < n; e += BLOCK) {
-    const uint64_t mine = key[e];
-    int place = 0;
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) place += key[i] > mine ? 1 : 0;
-    fn(place, mine);
+  for (int i = 0; i < PER; ++i) {
+    float z[VEC];
+    Elem<Tin>::unpack(mine[i], z);
+    if (largest(z) > -INFINITY) {
+#pragma unroll
+      for (int u = 0; u < VEC; ++u) keep(z[u], at[i] + u);
+    }
   }
+  keep(zt, x.tail + t);
+  __syncthreads();
+  n = s.n;
+  if (n > static_cast<uint32_t>(ListLds<BLOCK, KMAX>::KEYS)) {
+    __syncthreads();
+    return digits(row_keys);
+  }
+  if (n <= static_cast<uint32_t>(k + k / 2 + 64)) return close_list(s.key, static_cast<int>(n));
+  constexpr int MOST = 2 * PER;
+  uint64_t key[MOST];
+#pragma unroll
+  for (int i = 0; i < MOST; ++i) {
+    const uint32_t e = static_cast<uint32_t>(t + i * BLOCK);
+    key[i] = e < n ? s.key[e] : 0;
+  }
+  return digits([&](auto fn) {
+#pragma unroll
+    for (int i = 0; i < MOST; ++i) fn(key[i]);
+  });
 }
 
 // What log-probs of a row come from: log p of a logit is (z - m) / T - lnS.
@@ -352,15 +436,114 @@ __device__ __forceinline__ void write_top(const TopArgs& a, int64_t r, const Row
   }
 }
 
-template <typename Tin, int BLOCK>
+template <typename Tin, int BLOCK, int KMAX>
 __global__ __launch_bounds__(BLOCK) void top_kernel(TopArgs a, int64_t first) {
-  __shared__ ListLds<BLOCK> s;
+  __shared__ ListLds<BLOCK, KMAX> s;
   const int64_t r = first + blockIdx.x;
   const float T = a.temperature[r];
   const Stretch<Tin> x(static_cast<const Tin*>(a.logits) + r * a.row_stride, a.V, 0, 1);
   RowSum sum;
-  const int n = list_stretch<Tin, BLOCK>(x, a.k, scale_of(T), s, &sum);
+  const int n = list_stretch<Tin, BLOCK, KMAX>(x, a.k, scale_of(T), s, &sum);
   write_top<BLOCK>(a, r, row_norm(sum, T), s.key, n);
+}
+
+// The first k tokens of a part of a row in order, 0 after the last, and the part's sum.
+template <int BLOCK>
+__device__ __forceinline__ void write_part(uint64_t* list, RowSum* to, int k, const RowSum& sum, const uint64_t* key, int n) {
+  const int t = threadIdx.x;
+  if (t == 0) *to = sum;
+  in_order<BLOCK>(key, n, [&](int place, uint64_t mine) {
+    if (place < k) list[place] = mine;
+  });
+  if (t >= n && t < k) list[t] = 0;
+}
+
+// Rows over G workgroups each: the parts' tokens and sums,
+template <typename Tin, int BLOCK, int KMAX>
+__global__ __launch_bounds__(BLOCK) void top_parts_kernel(TopArgs a, uint64_t* list, RowSum* sums) {
+  __shared__ ListLds<BLOCK, KMAX> s;
+  const int64_t r = blockIdx.x / a.G;
+  const Stretch<Tin> x(static_cast<const Tin*>(a.logits) + r * a.row_stride, a.V, blockIdx.x % a.G, a.G);
+  RowSum sum;
+  const int n = list_stretch<Tin, BLOCK, KMAX>(x, a.k, scale_of(a.temperature[r]), s, &sum);
+  write_part<BLOCK>(list + static_cast<int64_t>(blockIdx.x) * a.k, sums + blockIdx.x, a.k, sum, s.key, n);
+}
+
+// The m-th largest of the wave's values, N of each lane (0: there are fewer
+// above 0). m <= 64 N; `used` of the N are looked at.
+template <int N>
+__device__ __forceinline__ uint32_t wave_nth(const uint32_t (&v)[N], int used, int m) {
+  uint32_t at = 0;
+#pragma unroll 1
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t up = at | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+      if (N == 1 || u < used) n += __popcll(__ballot(v[u] >= up));
+    if (n >= m) at = up;
+  }
+  return at;
+}
+
+// and the rows'. Where m parts have a j-th key not below some value and m j is
+// at least k, no key below it is among the first k: each wave takes its own j.
+// From what is left the k-th is looked for as in list_stretch.
+__global__ __launch_bounds__(kRowBlock) void top_merge_kernel(TopArgs a, const uint64_t* list, const RowSum* sums) {
+  constexpr int NW = kRowBlock / kWave, PER = kMaxSplit * kMaxTop / kRowBlock;
+  __shared__ alignas(16) uint64_t key[kMaxSplit * kMaxTop + 4];
+  __shared__ alignas(16) uint32_t hist[256];
+  __shared__ CutLds cut_lds;
+  __shared__ uint32_t bound[NW], n_key;
+  const int64_t r = blockIdx.x;
+  const int t = threadIdx.x, lane = t % kWave, wave = t / kWave, N = a.G * a.k;
+  const uint64_t* mine = list + r * N;
+  uint64_t x[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) x[i] = t + i * kRowBlock < N ? mine[t + i * kRowBlock] : 0;
+  const bool part = lane < a.G;
+  const RowSum e = part ? sums[r * a.G + lane] : RowSum{-INFINITY, 0.0f};
+  const float T = a.temperature[r];
+  const int share = (a.k + a.G - 1) / a.G, j = wave == NW - 1 ? a.k : min(a.k, share << wave);
+  const uint32_t jth[1] = {part ? static_cast<uint32_t>(mine[lane * a.k + j - 1] >> 32) : 0u};
+  const uint32_t b = wave_nth(jth, 1, (a.k + j - 1) / j);
+  if (lane == 0) bound[wave] = b;
+  hist[t] = 0;
+  if (t == 0) n_key = 0;
+  __syncthreads();
+  uint32_t floor = 0;
+  for (int w = 0; w < NW; ++w) floor = max(floor, bound[w]);
+  const RowNorm norm = row_norm(merge_lanes(e, scale_of(T)), T);
+  // All keys are between the floor and the row's largest logit.
+  const float low = key_float(floor), width = (norm.m - low) * (1.0f / 255.0f);
+  const float scale = floor > 0 && width > 0.0f && width < INFINITY ? 1.0f / width : 0.0f;
+  auto bin_of = [&](uint64_t v) {
+    return scale > 0.0f ? min(255, static_cast<int>(fmaxf((key_logit(v) - low) * scale, 0.0f))) : 255;
+  };
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (static_cast<uint32_t>(x[i] >> 32) < floor) x[i] = 0;
+    if (x[i] != 0) atomicAdd(&hist[bin_of(x[i])], 1u);
+  }
+  __syncthreads();
+  const int from = cut_bin(hist, static_cast<uint32_t>(a.k));
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (x[i] != 0 && bin_of(x[i]) >= from) key[atomicAdd(&n_key, 1u)] = x[i];
+  __syncthreads();
+  if (n_key > static_cast<uint32_t>(a.k + a.k / 2 + 64)) {
+    const Cut cut = find_cut<kRowBlock, 0>([&](auto fn) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) fn(x[i]);
+    }, static_cast<uint32_t>(a.k), cut_lds);
+    if (t == 0) n_key = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (cut.takes(x[i])) key[atomicAdd(&n_key, 1u)] = x[i];
+    __syncthreads();
+  }
+  write_top<kRowBlock>(a, r, norm, key, close_list(key, static_cast<int>(n_key)));
 }
 
 // ---------------------------------------------------------------------------
@@ -375,24 +558,17 @@ __device__ __forceinline__ bool beam_live(const BeamArgs& a, int64_t r, uint32_t
   return *flags == 0;
 }
 
-// The first k tokens of each live beam's row, and its sum of exps.
-template <typename Tin>
-__global__ __launch_bounds__(kRowBlock) void beam_rows_kernel(BeamArgs a, RowSum* sums, uint64_t* list) {
-  __shared__ ListLds<kRowBlock> s;
-  const int64_t r = blockIdx.x;
+// The first k tokens of each part of the live beams' rows, and its sum of exps.
+template <typename Tin, int BLOCK, int KMAX>
+__global__ __launch_bounds__(BLOCK) void beam_rows_kernel(BeamArgs a, RowSum* sums, uint64_t* list) {
+  __shared__ ListLds<BLOCK, KMAX> s;
+  const int64_t r = blockIdx.x / a.G;
   uint32_t flags;
   if (!beam_live(a, r, &flags)) return;
-  const float T = a.temperature[r];
-  const Stretch<Tin> x(static_cast<const Tin*>(a.logits) + r * a.row_stride, a.V, 0, 1);
+  const Stretch<Tin> x(static_cast<const Tin*>(a.logits) + r * a.row_stride, a.V, blockIdx.x % a.G, a.G);
   RowSum sum;
-  int n = list_stretch<Tin, kRowBlock>(x, a.k, scale_of(T), s, &sum);
-  if (row_norm(sum, T).flags) n = 0;
-  const int t = threadIdx.x;
-  if (t == 0) sums[r] = sum;
-  in_order<kRowBlock>(s.key, n, [&](int place, uint64_t key) {
-    if (place < a.k) list[r * a.k + place] = key;
-  });
-  if (t >= n && t < a.k) list[r * a.k + t] = 0;
+  const int n = list_stretch<Tin, BLOCK, KMAX>(x, a.k, scale_of(a.temperature[r]), s, &sum);
+  write_part<BLOCK>(list + static_cast<int64_t>(blockIdx.x) * a.k, sums + blockIdx.x, a.k, sum, s.key, n);
 }
 
 // A candidate of a request in the order of the selection: score, lower beam,
@@ -407,134 +583,253 @@ struct Candidate {
   }
 };
 
-// The k best candidates of a request, by one workgroup.
+// The k best candidates of a request, by one workgroup. The parts' lists are in
+// order: where m of them have a j-th candidate not below some score and m j is
+// at least k, no candidate below it is among the best (each wave takes its own
+// j). The few that are left are counted against each other, or, where they are
+// many, selected from by digits of their scores. SMALL: a request has at most
+// kHeld candidates, which the threads read at once and hold; a chain of a few
+// reads and barriers bounds it.
+constexpr int kCounted = 512, kHeld = 4 * kBeamBlock;
+
+template <bool SMALL>
 __global__ __launch_bounds__(kBeamBlock) void beam_merge_kernel(BeamArgs a, const RowSum* sums, const uint64_t* list) {
+  constexpr int NW = kBeamBlock / kWave, HELD = SMALL ? kHeld / kBeamBlock : 1;
   __shared__ RowNorm norm[PR_MAX_BEAMS];
   __shared__ double base[PR_MAX_BEAMS];
   __shared__ int state[PR_MAX_BEAMS];  // 0: no candidates, 1: its tokens, 2: itself
+  __shared__ Candidate best[kCounted];
+  __shared__ alignas(16) uint32_t near[kCounted + 4];
+  __shared__ uint32_t held[SMALL ? kHeld : 1];
+  __shared__ uint32_t bound[NW], n_best;
   __shared__ CutLds cut_lds;
-  __shared__ Candidate best[kMaxTop];
-  __shared__ uint32_t n_best;
   const int64_t first = static_cast<int64_t>(blockIdx.x) * a.B;
-  const int t = threadIdx.x;
+  const int t = threadIdx.x, lane = t % kWave, wave = t / kWave;
+  const int per = a.G * a.k, N = a.B * per, lists = a.B * a.G;  // per: entries of a beam
+  const uint64_t* mine = list + first * per;
+  uint64_t token[HELD];
+  if constexpr (SMALL) {
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) token[i] = t + i * kBeamBlock < N ? mine[t + i * kBeamBlock] : 0;
+  }
   if (t < a.B) {
     uint32_t flags;
     const bool live = beam_live(a, first + t, &flags);
+    const float score = a.scores[first + t], T = a.temperature[first + t];
     RowNorm x{0.0, 0.0f, 1.0f, 0};
     if (live) {
-      x = row_norm(sums[first + t], a.temperature[first + t]);
+      x = row_norm(merge_parts(sums + (first + t) * a.G, a.G, scale_of(T)), T);
       flags = x.flags;
     }
     norm[t] = x;
-    base[t] = static_cast<double>(a.scores[first + t]);
-    state[t] = live ? (flags ? 0 : 1) : (flags == PR_FLAG_MASKED && a.scores[first + t] > -INFINITY ? 2 : 0);
+    base[t] = static_cast<double>(score);
+    state[t] = live ? (flags ? 0 : 1) : (flags == PR_FLAG_MASKED && score > -INFINITY ? 2 : 0);
     if (a.out.flags) a.out.flags[first + t] = flags;
   }
   if (t == 0) n_best = 0;
   __syncthreads();
-  const uint64_t* mine = list + first * a.k;
-  // Each candidate of thread t: its score's key, beam and token.
+  // The score key (0: none) of entry i of the request's lists, which reads `key`.
+  auto score_of = [&](int i, uint64_t key) -> uint64_t {
+    const int b = i / per;
+    if (state[b] == 1) return key != 0 ? score_key(base[b] + norm[b].logprob(key_logit(key))) : 0;
+    return state[b] == 2 && i == b * per ? score_key(base[b]) : 0;
+  };
+  uint64_t score[HELD];
+  if constexpr (SMALL) {
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const int e = t + i * kBeamBlock;
+      score[i] = e < N ? score_of(e, token[i]) : 0;
+      if (e < N) held[e] = near_key(score[i]);
+    }
+    __syncthreads();
+  }
+  {
+    constexpr int PER = PR_MAX_BEAMS * kMaxSplit / kWave;
+    const int share = (a.k + lists - 1) / lists, j = wave == NW - 1 ? a.k : min(a.k, share << wave);
+    const int m = (a.k + j - 1) / j, used = (lists + kWave - 1) / kWave;
+    auto jth = [&](int l) -> uint32_t {
+      if (l >= lists) return 0;
+      const int e = l * a.k + j - 1;
+      if constexpr (SMALL) return held[e];
+      return near_key(score_of(e, mine[e]));
+    };
+    uint32_t at;
+    if (used == 1) {
+      const uint32_t v[1] = {jth(lane)};
+      at = wave_nth(v, 1, m);
+    } else {
+      uint32_t v[PER];
+#pragma unroll
+      for (int u = 0; u < PER; ++u) v[u] = u < used ? jth(u * kWave + lane) : 0;
+      at = wave_nth(v, used, m);
+    }
+    if (lane == 0) bound[wave] = at;
+  }
+  __syncthreads();
+  uint32_t floor = 0;
+  for (int w = 0; w < NW; ++w) floor = max(floor, bound[w]);
+  // Each candidate of the thread from the floor on: its score's key, beam and token.
   auto candidates = [&](auto fn) {
-    for (int e = t; e < a.B * a.k; e += kBeamBlock) {
-      const int b = e / a.k;
-      if (state[b] == 1) {
-        const uint64_t key = mine[e];
-        if (key != 0) fn(score_key(base[b] + norm[b].logprob(key_logit(key))), b, key);
-      } else if (state[b] == 2 && e % a.k == 0) {
-        fn(score_key(base[b]), b, uint64_t{1});
+    if constexpr (SMALL) {
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+        if (score[i] != 0 && near_key(score[i]) >= floor) fn(score[i], (t + i * kBeamBlock) / per, token[i]);
+    } else {
+      for (int e = t; e < N; e += kBeamBlock) {
+        const uint64_t key = state[e / per] == 1 ? mine[e] : 0, s = score_of(e, key);
+        if (s != 0 && near_key(s) >= floor) fn(s, e / per, key);
       }
     }
   };
-  const Cut by_score = find_cut<kBeamBlock, 0>([&](auto fn) {
-    candidates([&](uint64_t s, int, uint64_t) { fn(s); });
-  }, static_cast<uint32_t>(a.k), cut_lds);
-  Cut by_beam{0, 0, 0, false}, by_token{0, 0, 0, false};
-  if (by_score.more) {  // equal scores: by beam, then by token
-    by_beam = find_cut<kBeamBlock, 0x7fu>([&](auto fn) {
-      candidates([&](uint64_t s, int b, uint64_t) { fn(s == by_score.value ? static_cast<uint64_t>(255 - b) : 0); });
-    }, by_score.need, cut_lds);
-    if (by_beam.more)
-      by_token = find_cut<kBeamBlock, 0>([&](auto fn) {
-        candidates([&](uint64_t s, int b, uint64_t key) {
-          fn(s == by_score.value && static_cast<uint64_t>(255 - b) == by_beam.value ? key : 0);
-        });
-      }, by_beam.need, cut_lds);
-  }
   candidates([&](uint64_t s, int b, uint64_t key) {
-    bool take = by_score.takes(s);
-    if (take && by_score.more && s == by_score.value) {
-      const uint64_t kb = static_cast<uint64_t>(255 - b);
-      take = by_beam.takes(kb) && (!by_beam.more || by_beam.above(kb) || by_token.takes(key));
-    }
-    if (!take) return;
     const uint32_t at = atomicAdd(&n_best, 1u);
-    if (at < static_cast<uint32_t>(kMaxTop)) best[at] = Candidate{s, key, b};
+    if (at < static_cast<uint32_t>(kCounted)) best[at] = Candidate{s, key, b};
   });
   __syncthreads();
-  const int n = static_cast<int>(min(n_best, static_cast<uint32_t>(a.k)));
-  if (t >= a.k) return;
-  int at = t;
-  float score = -INFINITY, lp = -INFINITY;
-  int32_t parent = -1, token = -1;
-  if (t < n) {
-    const Candidate c = best[t];
-    at = 0;
-    for (int i = 0; i < n; ++i) at += best[i].before(c) ? 1 : 0;
-    parent = c.beam;
+  if (n_best > static_cast<uint32_t>(kCounted)) {
+    const uint32_t k = static_cast<uint32_t>(a.k);
+    const Cut by_score = find_cut<kBeamBlock, 0>([&](auto fn) {
+      candidates([&](uint64_t s, int, uint64_t) { fn(s); });
+    }, k, cut_lds);
+    Cut by_beam{0, 0, 0, false}, by_token{0, 0, 0, false};
+    if (by_score.more) {  // equal scores: by beam, then by token
+      by_beam = find_cut<kBeamBlock, 0x7fu>([&](auto fn) {
+        candidates([&](uint64_t s, int b, uint64_t) { fn(s == by_score.value ? static_cast<uint64_t>(255 - b) : 0); });
+      }, by_score.need, cut_lds);
+      if (by_beam.more)
+        by_token = find_cut<kBeamBlock, 0>([&](auto fn) {
+          candidates([&](uint64_t s, int b, uint64_t key) {
+            fn(s == by_score.value && static_cast<uint64_t>(255 - b) == by_beam.value ? key : 0);
+          });
+        }, by_beam.need, cut_lds);
+    }
+    if (t == 0) n_best = 0;
+    __syncthreads();
+    candidates([&](uint64_t s, int b, uint64_t key) {
+      bool take = by_score.takes(s);
+      if (take && by_score.more && s == by_score.value) {
+        const uint64_t kb = static_cast<uint64_t>(255 - b);
+        take = by_beam.takes(kb) && (!by_beam.more || by_beam.above(kb) || by_token.takes(key));
+      }
+      if (take) best[atomicAdd(&n_best, 1u)] = Candidate{s, key, b};
+    });
+    __syncthreads();
+  }
+  const int n = static_cast<int>(n_best);
+  for (int e = t; e < n + 4; e += kBeamBlock) near[e] = e < n ? near_key(best[e].score) : 0;
+  __syncthreads();
+  auto write = [&](int at, float s, int32_t parent, int32_t v, float lp) {
+    const int64_t o = static_cast<int64_t>(blockIdx.x) * a.k + at;
+    a.out.scores[o] = s;
+    a.out.parent[o] = parent;
+    a.out.token[o] = v;
+    if (a.out.logprob) a.out.logprob[o] = lp;
+  };
+  for (int e = t; e < n; e += kBeamBlock) {
+    const uint32_t my = near[e];
+    int at = 0, same = 0;
+    for (int i = 0; i < n; i += 4) {
+      const vec4u q = *reinterpret_cast<const vec4u*>(near + i);
+      at += (q.x > my ? 1 : 0) + (q.y > my ? 1 : 0) + (q.z > my ? 1 : 0) + (q.w > my ? 1 : 0);
+      same += (q.x == my ? 1 : 0) + (q.y == my ? 1 : 0) + (q.z == my ? 1 : 0) + (q.w == my ? 1 : 0);
+    }
+    if (at >= a.k) continue;
+    const Candidate c = best[e];
+    if (same > 1)
+      for (int i = 0; i < n; ++i) at += near[i] == my && best[i].before(c) ? 1 : 0;
+    if (at >= a.k) continue;
     const bool itself = state[c.beam] == 2;
     const double l = itself ? 0.0 : norm[c.beam].logprob(key_logit(c.token));
-    token = itself ? a.done_token : key_index(c.token);
-    lp = static_cast<float>(l);
-    score = static_cast<float>(base[c.beam] + l);
+    write(at, static_cast<float>(base[c.beam] + l), c.beam, itself ? a.done_token : key_index(c.token),
+          static_cast<float>(l));
   }
-  const int64_t o = static_cast<int64_t>(blockIdx.x) * a.k + at;
-  a.out.scores[o] = score;
-  a.out.parent[o] = parent;
-  a.out.token[o] = token;
-  if (a.out.logprob) a.out.logprob[o] = lp;
+  if (t >= n && t < a.k) write(t, -INFINITY, -1, -1, -INFINITY);
 }
 
 constexpr int64_t kMostGroups = int64_t{1} << 23;  // a grid holds less than 2^32 threads
 
-template <typename Tin>
+// Workgroups along a row: about 512 in all, each with at least 512 vectors.
+// About 512 and 1,024 in all, beam search's step: 256 rows of 151,936 bfloat16
+// logits 27.7 and 28.5 us, 512 rows of 32,000 float32 logits (one workgroup a
+// row, or two) 17.0 and 23.2. At least 256 and 512 vectors, k = 256: 17 rows of
+// 50,257 bfloat16 logits 32.5 and 29.6 us.
+constexpr int64_t kGroups = 512, kLeastVectors = 512;
+
+int top_split(int64_t n_rows, int32_t V, pr_dtype dtype) {
+  if (n_rows <= 0) return 1;
+  const int64_t nvec = V / (dtype == PR_BF16 ? 8 : 4);
+  const int64_t want = (kGroups + n_rows - 1) / n_rows, most = nvec / kLeastVectors;
+  const int64_t G = want < most ? want : most;
+  return static_cast<int>(G < 1 ? 1 : G > kMaxSplit ? kMaxSplit : G);
+}
+
+size_t lists_bytes(int64_t n_rows, int G, int32_t k) {
+  return static_cast<size_t>(n_rows) * static_cast<size_t>(G) * (static_cast<size_t>(k) * sizeof(uint64_t) + sizeof(RowSum));
+}
+
+template <typename Tin, int KMAX>
 hipError_t top(const TopArgs& a, hipStream_t stream) {
+  if (a.G > 1) {
+    uint64_t* list = static_cast<uint64_t*>(a.ws);
+    RowSum* sums = reinterpret_cast<RowSum*>(list + a.n_rows * a.G * a.k);
+    hipLaunchKernelGGL((top_parts_kernel<Tin, kRowBlock, KMAX>), dim3(static_cast<unsigned>(a.n_rows * a.G)),
+                       dim3(kRowBlock), 0, stream, a, list, sums);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(top_merge_kernel, dim3(static_cast<unsigned>(a.n_rows)), dim3(kRowBlock), 0, stream, a, list, sums);
+    return hipGetLastError();
+  }
   for (int64_t at = 0; at < a.n_rows; at += kMostGroups) {
     const int64_t rows = a.n_rows - at < kMostGroups ? a.n_rows - at : kMostGroups;
-    hipLaunchKernelGGL((top_kernel<Tin, kRowBlock>), dim3(static_cast<unsigned>(rows)), dim3(kRowBlock), 0, stream, a, at);
+    hipLaunchKernelGGL((top_kernel<Tin, kRowBlock, KMAX>), dim3(static_cast<unsigned>(rows)), dim3(kRowBlock), 0, stream,
+                       a, at);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
-template <typename Tin>
+template <typename Tin, int KMAX>
 hipError_t beam(const BeamArgs& a, hipStream_t stream) {
-  const int64_t n = static_cast<int64_t>(a.n_req) * a.B;
+  const int64_t n = static_cast<int64_t>(a.n_req) * a.B * a.G;
   uint64_t* list = static_cast<uint64_t*>(a.ws);
   RowSum* sums = reinterpret_cast<RowSum*>(list + n * a.k);
-  hipLaunchKernelGGL(beam_rows_kernel<Tin>, dim3(static_cast<unsigned>(n)), dim3(kRowBlock), 0, stream, a, sums, list);
+  hipLaunchKernelGGL((beam_rows_kernel<Tin, kRowBlock, KMAX>), dim3(static_cast<unsigned>(n)), dim3(kRowBlock), 0, stream,
+                     a, sums, list);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(beam_merge_kernel, dim3(static_cast<unsigned>(a.n_req)), dim3(kBeamBlock), 0, stream, a, sums,
-                     list);
+  const dim3 reqs(static_cast<unsigned>(a.n_req));
+  if (a.B * a.G * a.k <= kHeld)
+    hipLaunchKernelGGL(beam_merge_kernel<true>, reqs, dim3(kBeamBlock), 0, stream, a, sums, list);
+  else
+    hipLaunchKernelGGL(beam_merge_kernel<false>, reqs, dim3(kBeamBlock), 0, stream, a, sums, list);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t top_workspace_bytes(int64_t, int32_t, pr_dtype, int32_t) { return 0; }
-
-hipError_t launch_top(const TopArgs& a, pr_dtype dtype, hipStream_t stream) {
-  return dtype == PR_BF16 ? top<uint16_t>(a, stream) : top<float>(a, stream);
+size_t top_workspace_bytes(int64_t n_rows, int32_t V, pr_dtype dtype, int32_t k) {
+  const int G = top_split(n_rows, V, dtype);
+  return G > 1 ? lists_bytes(n_rows, G, k) : 0;
 }
 
-size_t beam_workspace_bytes(int64_t n_rows, int32_t, pr_dtype, int32_t k) {
-  const size_t n = n_rows < 0 ? 0 : static_cast<size_t>(n_rows);
-  return n * (static_cast<size_t>(k) * sizeof(uint64_t) + sizeof(RowSum));
+hipError_t launch_top(const TopArgs& a, pr_dtype dtype, hipStream_t stream) {
+  TopArgs x = a;
+  x.G = top_split(a.n_rows, a.V, dtype);
+  if (x.k <= 64) return dtype == PR_BF16 ? top<uint16_t, 64>(x, stream) : top<float, 64>(x, stream);
+  return dtype == PR_BF16 ? top<uint16_t, kMaxTop>(x, stream) : top<float, kMaxTop>(x, stream);
+}
+
+size_t beam_workspace_bytes(int64_t n_rows, int32_t V, pr_dtype dtype, int32_t k) {
+  return n_rows < 1 ? 0 : lists_bytes(n_rows, top_split(n_rows, V, dtype), k);
 }
 
 hipError_t launch_beam(const BeamArgs& a, pr_dtype dtype, hipStream_t stream) {
-  return dtype == PR_BF16 ? beam<uint16_t>(a, stream) : beam<float>(a, stream);
+  BeamArgs x = a;
+  x.G = top_split(static_cast<int64_t>(a.n_req) * a.B, a.V, dtype);
+  if (x.k <= 64) return dtype == PR_BF16 ? beam<uint16_t, 64>(x, stream) : beam<float, 64>(x, stream);
+  return dtype == PR_BF16 ? beam<uint16_t, kMaxTop>(x, stream) : beam<float, kMaxTop>(x, stream);
 }
 
 }  // namespace pr
