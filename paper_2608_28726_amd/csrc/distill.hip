@@ -19,7 +19,7 @@
 // positive terms, compensated per lane; what follows per row and over rows is
 // in 64 bits. A gradient element is rounded to its type once.
 #include "distill.h"
-#include "row_sum.h"
+#include "held_rows.h"
 
 namespace pr {
 namespace {
@@ -110,11 +110,6 @@ __device__ __forceinline__ void write_row(const DistillArgs& a, int64_t r, const
   if (a.out.token_loss) a.out.token_loss[r] = static_cast<float>(x.loss);
   if (a.out.mass) a.out.mass[r] = static_cast<float>(x.mass);
   if (a.out.flags) a.out.flags[r] = x.flags;
-}
-
-template <typename Tin>
-__device__ __forceinline__ const Tin* row_ptr(const LossRows& a, int64_t r) {
-  return static_cast<const Tin*>(a.logits) + r * a.row_stride;
 }
 
 // Entry i of a row: its token (-1: none, or out of range), its log-prob and
@@ -333,6 +328,271 @@ __global__ __launch_bounds__(kGradBlock) void distill_grad_kernel(DistillArgs a,
   stream_grad(out + h + static_cast<int64_t>(j) * VEC, GradVec<Tin>::pack(g));
 }
 
+// The entries of a row as the wave that takes them holds them, KE a lane.
+template <int KE>
+struct Held {
+  int32_t id[KE];
+  float logq[KE];
+  uint32_t mine[KE];  // which elements of its group are entries' tokens
+  uint32_t ends;      // the same of the elements before (low byte) and after the vectors
+  uint32_t bad;
+};
+
+__device__ __forceinline__ uint32_t group_slot(const Group& g, int32_t nvec) {
+  return static_cast<uint32_t>(g.vec >= 0 ? g.vec : nvec + (g.vec == -1 ? 0 : 1));
+}
+
+// The loss of a row and its gradient in one read of the row, as the policy
+// loss's kernel for such rows: the row's vectors stay in the registers of DW
+// waves between their sum and their gradient, and one more wave takes what is
+// scalar in a row. That wave also takes the entries: a bit map of the vectors
+// that hold their tokens, made a row ahead, tells the others which vectors to
+// leave to it, in the sum and in the gradient. There are three bit maps in turn:
+// the one made while a row is summed was last read two rows before.
+template <typename Tin, int DW, int NR, int KE>
+__global__ __launch_bounds__((DW + 1) * kWave) void distill_row_kernel(DistillArgs a, double* term) {
+  constexpr int VEC = Elem<Tin>::kVec, NT = DW * kWave, MOST = NR * NT;  // vectors
+  __shared__ RowSum sh_sum[DW];
+  __shared__ float sh_A, sh_c, sh_k;
+  __shared__ int32_t rows_on[kListed], rows_off[kListed];
+  __shared__ uint32_t sh_n[DW + 1];
+  __shared__ uint64_t marks[3][MOST / 64 + 1];
+  __shared__ alignas(16) uint32_t elements[(MOST + 16) / 4];  // a byte a vector: its entries' elements; then both ends
+  static_assert(DW < kWave && NR <= kWave, "one wave merges the waves; a lane reads a bit map's word");
+  const int lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+  const int32_t V = a.rows.V;
+  const int64_t n = a.rows.n_rows, G = gridDim.x;
+  const RowDeal deal = deal_rows<DW + 1>(a.rows.weight, n, G, rows_on, rows_off, sh_n);
+  const bool listed = deal.listed;
+  const int64_t turns = listed ? deal.n_on : n > blockIdx.x ? (n - blockIdx.x - 1) / G + 1 : 0;
+  const int64_t turns_off = listed ? deal.n_off : turns;
+  auto row_of = [&](const int32_t* list, int64_t k) -> int64_t {
+    return listed ? static_cast<int64_t>(__builtin_amdgcn_readfirstlane(list[k])) : blockIdx.x + k * G;
+  };
+  // The first turn from k on whose row counts (without lists the others are passed over).
+  auto next_turn = [&](int64_t k) {
+    while (!listed && k < turns && a.rows.weight[row_of(rows_on, k)] == 0.0f) ++k;
+    return k;
+  };
+
+  if (wave == DW) {
+    auto load = [&](int64_t r, Held<KE>& e) {
+      e.bad = 0;
+#pragma unroll
+      for (int i = 0; i < KE; ++i) {
+        const Entry x = load_entry(a, r, lane + i * kWave);
+        e.id[i] = x.id;
+        e.logq[i] = x.logq;
+        e.bad |= x.bad;
+      }
+    };
+    auto mark = [&](int64_t r, Held<KE>& e, uint64_t* map) {
+      const RowView<Tin> x(a.rows, r);
+      const int32_t h = x.h, nvec = x.nvec, tail = x.tail();
+      for (int32_t i = lane; i * 16 < nvec + 2; i += kWave) reinterpret_cast<vec4u*>(elements)[i] = vec4u{0, 0, 0, 0};
+      for (int32_t i = lane; i * 64 < nvec; i += kWave) map[i] = 0;
+      wave_lds_fence();
+#pragma unroll
+      for (int i = 0; i < KE; ++i) {
+        if (e.id[i] < 0) continue;
+        const Group g = group_of<Tin>(e.id[i], h, tail, V);
+        const uint32_t slot = group_slot(g, nvec), bit = 1u << (slot % 4 * 8 + static_cast<uint32_t>(e.id[i] - g.base));
+        if (atomicOr(&elements[slot / 4], bit) & bit) e.bad |= PR_FLAG_BAD_ID;
+        if (g.vec >= 0) atomicOr(reinterpret_cast<uint32_t*>(map) + g.vec / 32, 1u << g.vec % 32);
+      }
+      wave_lds_fence();
+      const uint8_t* byte = reinterpret_cast<const uint8_t*>(elements);
+#pragma unroll
+      for (int i = 0; i < KE; ++i)
+        e.mine[i] = e.id[i] < 0 ? 0 : byte[group_slot(group_of<Tin>(e.id[i], h, tail, V), nvec)];
+      e.ends = byte[nvec] | static_cast<uint32_t>(byte[nvec + 1]) << 8;
+      wave_lds_fence();
+    };
+    Held<KE> e;
+    int64_t k = next_turn(0);
+    if (k < turns) {
+      load(row_of(rows_on, k), e);
+      mark(row_of(rows_on, k), e, marks[0]);
+    }
+    __syncthreads();
+    for (int done = 0; k < turns; ++done) {
+      const int64_t r = row_of(rows_on, k);
+      const RowView<Tin> x(a.rows, r);
+      const int32_t h = x.h, tail = x.tail();
+      const float T = a.rows.temperature[r], c = scale_of(T), w = a.rows.weight[r];
+      const int32_t s = scalar_element(lane, h, tail, V);
+      const float zs = s < V ? Elem<Tin>::load1(x.row, s) : -INFINITY;
+      const bool scalar = s < V && !(e.ends >> lane & 1u);  // no entry's
+      float z[KE];
+      vec4u v[KE];
+#pragma unroll
+      for (int i = 0; i < KE; ++i) {
+        z[i] = -INFINITY;
+        v[i] = neg_inf_vec<Tin>();
+        if (e.id[i] < 0) continue;
+        z[i] = Elem<Tin>::load1(x.row, e.id[i]);
+        const Group g = group_of<Tin>(e.id[i], h, tail, V);
+        // The entry of a group's first token takes the group's other elements.
+        const uint32_t below = (1u << (e.id[i] - g.base)) - 1u;
+        if (g.vec >= 0 && !(e.mine[i] & below)) v[i] = *x.in(g.vec, 0);
+        else e.mine[i] = ~0u;
+      }
+      // The next row's entries, while this one is on its way.
+      const int64_t k_next = next_turn(k + 1);
+      Held<KE> e_next;
+      if (k_next < turns) {
+        load(row_of(rows_on, k_next), e_next);
+        mark(row_of(rows_on, k_next), e_next, marks[(done + 1) % 3]);
+      }
+      LaneSum<false> in, out;
+      out.add1(scalar ? zs : -INFINITY, c);
+      EntrySums sums{0.0, 0.0};
+#pragma unroll
+      for (int i = 0; i < KE; ++i) {
+        in.add1(z[i], c);
+        float other[VEC];
+        Elem<Tin>::unpack(v[i], other);
+#pragma unroll
+        for (int u = 0; u < VEC; ++u) other[u] = e.mine[i] >> u & 1u ? -INFINITY : other[u];
+        out.add(other, c);
+        // A probability of 0 adds nothing, whatever the student makes of its token.
+        const double q = e.id[i] >= 0 ? exp(static_cast<double>(e.logq[i])) : 0.0;
+        sums.Q += q;
+        if (q > 0.0)
+          sums.cross += q * (static_cast<double>(e.logq[i]) - static_cast<double>(z[i]) / static_cast<double>(T));
+      }
+      sums.Q = wave_sum_d(sums.Q);
+      sums.cross = wave_sum_d(sums.cross);
+      const RowSum sum_in{in.mw, wave_sum(in.s)}, own{out.mw, wave_sum(out.s)};
+      const uint32_t bad = (__any(e.bad & PR_FLAG_BAD_ID) ? PR_FLAG_BAD_ID : 0u) |
+                           (__any(e.bad & PR_FLAG_NONFINITE) ? PR_FLAG_NONFINITE : 0u);
+      __syncthreads();
+      RowSum part{-INFINITY, 0.0f};
+      if (lane < DW) part = sh_sum[lane];
+      if (lane == DW) part = own;
+      const RowLoss loss = row_loss(a, sum_in, merge_lanes(part, c), sums, bad, T, c, w);
+      const RowDistill q = loss.grad;
+      if (lane == 0) {
+        sh_A = q.A;
+        sh_c = q.c;
+        sh_k = q.k;
+      }
+      __syncthreads();
+      if (lane == 0) {
+        write_row(a, r, loss);
+        term[r] = static_cast<double>(w) * loss.loss;
+      }
+      if (scalar) GradVec<Tin>::store1(x.out, s, q.k * fast_exp2(fmaf(zs, q.c, -q.A)));
+#pragma unroll
+      for (int i = 0; i < KE; ++i) {
+        if (e.id[i] < 0) continue;
+        GradVec<Tin>::store1(x.out, e.id[i],
+                             q.in_k * fast_exp2(fmaf(z[i], q.c, -q.in_A)) - q.q_k * expf(e.logq[i]));
+        float other[VEC];
+        Elem<Tin>::unpack(v[i], other);
+        const int32_t base = group_of<Tin>(e.id[i], h, tail, V).base;
+#pragma unroll
+        for (int u = 0; u < VEC; ++u)
+          if (!(e.mine[i] >> u & 1u))
+            GradVec<Tin>::store1(x.out, base + u, q.k * fast_exp2(fmaf(other[u], q.c, -q.A)));
+      }
+      k = k_next;
+      e = e_next;
+    }
+    for (int64_t i = 0; i < turns_off; ++i) {
+      const int64_t r = row_of(rows_off, i);
+      if (a.rows.weight[r] != 0.0f) continue;
+      const RowView<Tin> x(a.rows, r);
+      const int32_t s = scalar_element(lane, x.h, x.tail(), V);
+      if (lane == 0) {
+        write_row(a, r, masked_row());
+        term[r] = 0.0;
+      }
+      if (s < V) GradVec<Tin>::store1(x.out, s, 0.0f);
+    }
+    return;
+  }
+
+  const int t = threadIdx.x;  // below NT
+  int64_t k = next_turn(0);
+  float T_next = k < turns ? a.rows.temperature[row_of(rows_on, k)] : 1.0f;
+  __syncthreads();
+  for (int done = 0; k < turns; ++done) {
+    const int64_t r = row_of(rows_on, k);
+    const float c = scale_of(T_next);
+    const RowView<Tin> x(a.rows, r);
+    // Every lane loads for every u, past the row's end a vector of the row
+    // again, so that the loads in flight are always as many and a wave can
+    // wait for one after the other. (Held rows have vectors.)
+    auto place = [&](int u) {
+      const int32_t at = u * NT < x.nvec ? u * NT : 0;
+      return x.in(at, static_cast<uint32_t>(min(t, x.nvec - 1 - at)));
+    };
+    vec4u v[NR];
+#pragma unroll
+    for (int u = 0; u < NR; ++u) v[u] = *place(u);
+    // Which of the wave's vectors u are the entries': a word of the bit map.
+    const uint64_t words = lane < NR && (lane * DW + wave) * 64 < x.nvec ? marks[done % 3][lane * DW + wave] : 0;
+    auto marked = [&](int u) {
+      const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(words), u));
+      const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(words >> 32), u));
+      return static_cast<uint64_t>(hi) << 32 | lo;
+    };
+    LaneSum<false> L;
+#pragma unroll
+    for (int u = 0; u < NR; ++u)
+      if (u * NT < x.nvec) {
+        vec4u p = v[u];
+        if ((u + 1) * NT > x.nvec && t >= x.nvec - u * NT) p = neg_inf_vec<Tin>();
+        const uint64_t m = marked(u);
+        if (m != 0 && m >> lane & 1u) p = neg_inf_vec<Tin>();
+        float z[VEC];
+        Elem<Tin>::unpack(p, z);
+        L.add(z, c);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    const float S = wave_sum(L.s);
+    if (lane == 0) sh_sum[wave] = RowSum{L.mw, S};
+    __syncthreads();
+    k = next_turn(k + 1);
+    __syncthreads();
+    const float A = sh_A, cq = sh_c, kq = sh_k;
+    if (k < turns) T_next = a.rows.temperature[row_of(rows_on, k)];
+#pragma unroll
+    for (int u = 0; u < NR; ++u) {
+      forget(v[u]);
+      const uint64_t m = marked(u);
+      if (t < x.nvec - u * NT && !(m >> lane & 1u)) {
+        float z[VEC];
+        Elem<Tin>::unpack(v[u], z);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) z[i] = kq * fast_exp2(fmaf(z[i], cq, -A));
+        store_grad(x.to(u * NT, t), GradVec<Tin>::pack(z));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  for (int64_t i = 0; i < turns_off; ++i) {
+    const int64_t r = row_of(rows_off, i);
+    if (!listed && a.rows.weight[r] != 0.0f) continue;
+    const RowView<Tin> x(a.rows, r);
+    for (int32_t at = 0; at < x.nvec; at += NT)
+      if (t < x.nvec - at) store_grad(x.to(at, t), vec4u{0, 0, 0, 0});
+  }
+}
+
+template <typename Tin, int DW, int NR>
+hipError_t launch_held(const DistillArgs& a, int64_t most, double* term, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(a.rows.n_rows < most ? a.rows.n_rows : most)), block((DW + 1) * kWave);
+  if (a.k <= kWave)
+    hipLaunchKernelGGL((distill_row_kernel<Tin, DW, NR, 1>), grid, block, 0, stream, a, term);
+  else
+    hipLaunchKernelGGL((distill_row_kernel<Tin, DW, NR, kMaxTop / kWave>), grid, block, 0, stream, a, term);
+  return hipGetLastError();
+}
+
+constexpr int64_t kFewRows = 0;
 constexpr int64_t kMostGroups = int64_t{1} << 23;  // a grid holds less than 2^32 threads
 
 template <typename Tin>
@@ -340,6 +600,12 @@ hipError_t distill(const DistillArgs& a, hipStream_t stream) {
   const int64_t n = a.rows.n_rows;
   RowDistill* rd = static_cast<RowDistill*>(a.ws);
   double* term = reinterpret_cast<double*>(rd + n);
+  const int64_t vectors = a.rows.V / Elem<Tin>::kVec;
+  if (n > kFewRows && a.rows.grad && held_row(vectors)) {
+    const hipError_t e = vectors <= kSmallRowVectors ? launch_held<Tin, 7, 19>(a, 2 * kCUs, term, stream)
+                                                     : launch_held<Tin, 15, 20>(a, kCUs, term, stream);
+    return e == hipSuccess ? launch_loss_sum(term, n, 1.0, a.loss, stream) : e;
+  }
   for (int64_t at = 0; at < n; at += kMostGroups) {
     const int64_t rows = n - at < kMostGroups ? n - at : kMostGroups;
     hipLaunchKernelGGL(distill_stats_kernel<Tin>, dim3(static_cast<unsigned>(rows)), dim3(kStatsBlock), 0, stream, a,

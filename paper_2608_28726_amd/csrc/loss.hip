@@ -23,12 +23,11 @@
 // exponentials of 64-bit arguments (in 64 bits they took registers that hold
 // the row). A gradient element is rounded to its type once.
 #include "loss.h"
-#include "row_sum.h"
+#include "held_rows.h"
 
 namespace pr {
 namespace {
 
-constexpr int kCUs = 256;  // compute units of the device
 constexpr int kStatsBlock = 256;
 constexpr int kGradBlock = 512;
 constexpr int kSumBlock = 1024;
@@ -75,11 +74,6 @@ __device__ __forceinline__ RowGrad row_grad(double coef, double l, float A, floa
   }
   return RowGrad{A, c, static_cast<float>(-coef / static_cast<double>(S)),
                  static_cast<float>(-coef) * expm1f(static_cast<float>(l))};
-}
-
-template <typename Tin>
-__device__ __forceinline__ const Tin* row_ptr(const LossRows& a, int64_t r) {
-  return static_cast<const Tin*>(a.logits) + r * a.row_stride;
 }
 
 template <typename Tin>
@@ -300,57 +294,6 @@ __global__ __launch_bounds__(kGradBlock) void policy_parts_kernel(PolicyArgs a, 
     policy_finish(a, part, zy, nullptr);
 }
 
-// Makes the compiler forget what it knows of a vector, so that it unpacks it
-// anew in each pass instead of keeping 8 floats of each through all of them.
-__device__ __forceinline__ void forget(vec4u& v) { asm volatile("" : "+v"(v)); }
-
-// A row as the fused kernel sees it: its vectors start at the first 16-byte
-// boundary, h elements in; up to 2 x 7 elements before and after are scalars.
-template <typename Tin>
-struct RowView {
-  const Tin* row;
-  Tin* out;
-  int32_t h, nvec;
-
-  __device__ __forceinline__ RowView(const LossRows& a, int64_t r) {
-    row = row_ptr<Tin>(a, r);
-    out = static_cast<Tin*>(a.grad) + r * a.grad_stride;
-    h = static_cast<int32_t>(head_elems<Tin>(row, a.V));
-    nvec = (a.V - h) / Elem<Tin>::kVec;
-  }
-  __device__ __forceinline__ int32_t tail() const { return h + nvec * Elem<Tin>::kVec; }
-  // Vector at + t of the row and of its gradient: a place that the wave shares
-  // plus 16 t, so that an address takes one register of a lane.
-  __device__ __forceinline__ const vec4u* in(int32_t at, uint32_t t) const {
-    return reinterpret_cast<const vec4u*>(reinterpret_cast<const char*>(row + h) + static_cast<int64_t>(at) * 16 +
-                                          t * 16u);
-  }
-  __device__ __forceinline__ Tin* to(int32_t at, uint32_t t) const {
-    return reinterpret_cast<Tin*>(reinterpret_cast<char*>(out + h) + static_cast<int64_t>(at) * 16 + t * 16u);
-  }
-};
-
-// Vectors of the rows that policy_row_kernel holds, by its two sizes (two and
-// one workgroups a compute unit). Shorter rows than the least take two passes:
-// what a workgroup spends on a row beside its vectors then costs more than the
-// second read. 1.2 GB of rows that all count, held and in two passes (us, in
-// brackets the row's vectors): bfloat16 16,384 logits a row (2,048) 710 and
-// 615, 24,000 (3,000) 593 and 580, 32,000 (4,000) 535 and 575, 50,257 510 and
-// 596, 65,536 475 and 569, 70,000 (8,750, the larger size) 496 and 588, 100,000
-// 487 and 570, 151,936 484 and 574; float32 8,192 (2,048) 669 and 601, 12,000
-// (3,000) 566 and 571, 16,000 (4,000) 521 and 580, 32,000 484 and 565, 40,000
-// (10,000, the larger size) 464 and 585. Fewer rows of 32,000 bfloat16 logits:
-// 128 rows 11.7 and 13.6, 512 18.4 and 23.9, 1,000 31 and 39. Batches that the
-// last-level cache keeps between two passes are the exception, and only long
-// rows among them: of 151,936 bfloat16 logits 300 rows 62 and 54, 512 79.6 and
-// 79.8, 1,024 143 and 155.
-constexpr int64_t kLeastRowVectors = 3500, kSmallRowVectors = 19 * 7 * kWave, kRowVectors = 20 * 15 * kWave;
-bool held_row(int64_t nvec) { return nvec >= kLeastRowVectors && nvec <= kRowVectors; }
-
-// Most rows whose order policy_row_kernel works out for itself.
-constexpr int64_t kListedRows = 65536;
-constexpr int kListed = kListedRows / kCUs + 1;
-
 // The policy loss of a row and its gradient in one read of the row.
 //
 // A workgroup keeps the row in registers between its sum and its gradient, NR
@@ -383,36 +326,9 @@ __global__ __launch_bounds__((DW + 1) * kWave) void policy_row_kernel(PolicyArgs
   const int32_t V = a.rows.V;
   const int64_t n = a.rows.n_rows, G = gridDim.x;
 
-  // The workgroup's rows: of the rows that count those of rank b, b + G, ..
-  // (b the workgroup), and likewise of the others. Each thread counts a
-  // stretch of rows; the counts' prefix sums give the ranks.
-  const bool listed = n > G && n <= kListedRows;
-  uint32_t n_on = 0, n_off = 0;
-  if (listed) {
-    const uint32_t per = static_cast<uint32_t>((n + blockDim.x - 1) / blockDim.x);
-    const uint32_t lo = min(static_cast<uint32_t>(n), threadIdx.x * per), hi = min(static_cast<uint32_t>(n), lo + per);
-    uint32_t on = 0;
-    for (uint32_t i = lo; i < hi; ++i) on += a.rows.weight[i] != 0.0f ? 1u : 0u;
-    const uint32_t scan = wave_incl_scan_u(on);
-    if (lane == kWave - 1) sh_n[wave] = scan;
-    __syncthreads();
-    uint32_t rank = scan - on;
-    for (int k = 0; k <= DW; ++k) {
-      if (k < wave) rank += sh_n[k];
-      n_on += sh_n[k];
-    }
-    n_off = static_cast<uint32_t>(n) - n_on;
-    for (uint32_t i = lo; i < hi; ++i) {
-      const bool counts = a.rows.weight[i] != 0.0f;
-      const uint32_t k = counts ? rank : i - rank;
-      if (k % static_cast<uint32_t>(G) == blockIdx.x) (counts ? rows_on : rows_off)[k / G] = static_cast<int32_t>(i);
-      rank += counts ? 1u : 0u;
-    }
-    __syncthreads();
-    const uint32_t b = blockIdx.x, g = static_cast<uint32_t>(G);
-    n_on = n_on > b ? (n_on - b - 1) / g + 1 : 0u;
-    n_off = n_off > b ? (n_off - b - 1) / g + 1 : 0u;
-  }
+  const RowDeal deal = deal_rows<DW + 1>(a.rows.weight, n, G, rows_on, rows_off, sh_n);
+  const bool listed = deal.listed;
+  const uint32_t n_on = deal.n_on, n_off = deal.n_off;
   // A row for each workgroup, or too many to list: they are dealt out by row,
   // and the turn of a row that does not count is passed over.
   const int64_t turns = listed ? n_on : n > blockIdx.x ? (n - blockIdx.x - 1) / G + 1 : 0;
