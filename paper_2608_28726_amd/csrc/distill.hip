@@ -27,7 +27,7 @@ namespace {
 constexpr int kMaxTop = PR_MAX_TOP_LOGITS;
 constexpr int kStatsBlock = 256;  // a thread for each of a row's entries
 constexpr int kGradBlock = 512;
-constexpr int kWindow = 1 << 15;  // vectors of a bit map
+constexpr int kWindow = 1 << 16;  // vectors of a bit map
 static_assert(kStatsBlock >= kMaxTop && kGradBlock >= kMaxTop, "a thread for each entry");
 
 // What the gradient pass needs of a row: dz_v = k 2^fma(z_v, c, -A) outside the
@@ -167,117 +167,231 @@ __device__ __forceinline__ EntrySums sum_entries(EntrySums e) {
   return t;
 }
 
-// One workgroup per row: its sums and everything but its gradient.
+// What a part of a row adds to its loss.
+struct DistillPart {
+  RowSum in, out;
+  EntrySums entries;
+  uint32_t bad, pad;
+};
+
+// A part of a row (workgroup g of G along it): its vectors' and their entries'
+// sums; the first part also has the elements before the vectors, the last one
+// those after them. Valid in thread 0. Every part looks at every entry.
 template <typename Tin>
-__global__ __launch_bounds__(kStatsBlock) void distill_stats_kernel(DistillArgs a, double* term, RowDistill* rd,
-                                                                   int64_t first) {
+__device__ DistillPart row_part(const DistillArgs& a, int64_t r, int g, int G, float T, float c) {
   constexpr int VEC = Elem<Tin>::kVec;
-  __shared__ alignas(16) int32_t sh_id[kMaxTop];
-  __shared__ uint32_t marks[kWindow / 32];
-  __shared__ uint32_t sh_bad, sh_ends;
-  const int64_t r = first + blockIdx.x;
-  const int t = threadIdx.x;
-  const float w = a.rows.weight[r];
-  if (w == 0.0f) {
-    if (t == 0) {
-      const RowLoss x = masked_row();
-      write_row(a, r, x);
-      term[r] = 0.0;
-      rd[r] = x.grad;
-    }
-    return;
-  }
+  __shared__ alignas(16) int32_t sh_id[kMaxTop + 4];  // the entries of this part, in no order
+  __shared__ uint64_t words[kWindow / 64];
+  __shared__ uint32_t sh_bad, sh_ends, sh_n;
+  uint32_t* const marks = reinterpret_cast<uint32_t*>(words);
+  const int t = threadIdx.x, lane = t % kWave, wave = __builtin_amdgcn_readfirstlane(t / kWave);
   const int32_t V = a.rows.V;
   const Tin* row = row_ptr<Tin>(a.rows, r);
-  const float T = a.rows.temperature[r], c = scale_of(T);
   const int32_t h = static_cast<int32_t>(head_elems<Tin>(row, V)), nvec = (V - h) / VEC, tail = h + nvec * VEC;
+  const int32_t vb = static_cast<int32_t>(static_cast<int64_t>(nvec) * g / G);
+  const int32_t ve = static_cast<int32_t>(static_cast<int64_t>(nvec) * (g + 1) / G);
   const vec4u* vp = reinterpret_cast<const vec4u*>(row + h);
-  const Entry e = load_entry(a, r, t);
-  const float z = e.id >= 0 ? Elem<Tin>::load1(row, e.id) : -INFINITY;
-  const Group g = group_of<Tin>(e.id, h, tail, V);
-  sh_id[t] = e.id;
-  if (t == 0) sh_bad = sh_ends = 0;
+  vec4u v[4];
+  const int32_t first_window = ve - vb < kWindow ? ve : vb + kWindow;
+  scan::stretch_prefetch<Tin, kStatsBlock, 4>(row, h, vb, first_window, v);
+  Entry e = load_entry(a, r, t);
+  if (t == 0) sh_bad = sh_ends = sh_n = 0;
+  for (int i = t; i < kWindow / 32; i += kStatsBlock) marks[i] = 0;
   __syncthreads();
   if (e.bad) atomicOr(&sh_bad, e.bad);
-  LaneSum<true> in, out;
-  in.add1(z, c);
-  // The first entry of a group takes the group's other elements.
-  {
-    float other[VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) other[i] = -INFINITY;
-    if (e.id >= 0) {
-      uint32_t mine = 0;
-      bool owner = true, twice = false;
-      for (int i = 0; i < a.k; ++i) {
-        const int32_t o = sh_id[i], d = o - g.base;
-        if (o < 0 || d < 0 || d >= g.len) continue;
-        mine |= 1u << d;
-        if (i < t) owner = false;
-        if (i != t && o == e.id) twice = true;
-      }
-      if (twice) atomicOr(&sh_bad, PR_FLAG_BAD_ID);
-      if (owner) {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i)
-          if (i < g.len && !(mine >> i & 1u)) other[i] = Elem<Tin>::load1(row, g.base + i);
-        if (g.vec < 0) atomicOr(&sh_ends, g.vec == -1 ? 1u : 2u);
-      }
-    }
-    out.add(other, c);
+  const Group q = group_of<Tin>(e.id, h, tail, V);
+  if (q.vec >= 0 ? q.vec < vb || q.vec >= ve : q.vec == -1 ? g != 0 : g != G - 1) e.id = -1;
+  float z = -INFINITY;
+  if (e.id >= 0) {
+    z = Elem<Tin>::load1(row, e.id);
+    sh_id[atomicAdd(&sh_n, 1u)] = e.id;
+    if (q.vec >= 0 && q.vec < first_window) atomicOr(&marks[(q.vec - vb) / 32], 1u << (q.vec - vb) % 32);
+    if (q.vec < 0) atomicOr(&sh_ends, q.vec == -1 ? 1u : 2u);
   }
   __syncthreads();
+  const int n = static_cast<int>(sh_n);
   const uint32_t ends = sh_ends;
-  out.add1(t < h && !(ends & 1u) ? Elem<Tin>::load1(row, t) : -INFINITY, c);
-  out.add1(t < V - tail && !(ends & 2u) ? Elem<Tin>::load1(row, tail + t) : -INFINITY, c);
-  for (int32_t w0 = 0; w0 < nvec; w0 += kWindow) {
-    const int32_t w1 = nvec - w0 < kWindow ? nvec : w0 + kWindow;
-    for (int i = t; i < kWindow / 32; i += kStatsBlock) marks[i] = 0;
-    __syncthreads();
-    if (e.id >= 0 && g.vec >= w0 && g.vec < w1) atomicOr(&marks[(g.vec - w0) / 32], 1u << (g.vec - w0) % 32);
-    __syncthreads();
-    vec4u v[4];
-    scan::stretch_prefetch<Tin, kStatsBlock, 4>(row, h, w0, w1, v);
+  if (t < 4) sh_id[n + t] = -1;
+  LaneSum<true> in, out;
+  out.add1(g == 0 && t < h && !(ends & 1u) ? Elem<Tin>::load1(row, t) : -INFINITY, c);
+  out.add1(g == G - 1 && t < V - tail && !(ends & 2u) ? Elem<Tin>::load1(row, tail + t) : -INFINITY, c);
+  for (int32_t w0 = vb; w0 < ve; w0 += kWindow) {
+    const int32_t w1 = ve - w0 < kWindow ? ve : w0 + kWindow;
+    if (w0 != vb) {
+      for (int i = t; i < kWindow / 32; i += kStatsBlock) marks[i] = 0;
+      __syncthreads();
+      if (e.id >= 0 && q.vec >= w0 && q.vec < w1) atomicOr(&marks[(q.vec - w0) / 32], 1u << (q.vec - w0) % 32);
+      __syncthreads();
+      scan::stretch_prefetch<Tin, kStatsBlock, 4>(row, h, w0, w1, v);
+    }
+    // A word holds the marks of a wave's vectors of one round; few rounds have
+    // any, and which do is looked up for 64 rounds at once.
+    constexpr int NW = kStatsBlock / kWave;
+    uint64_t rounds = 0;
     scan::stream_stretch<Tin, kStatsBlock, 2, 4>(vp, w0, w1, v, [&](const vec4u* vv, int64_t j) {
-      float x[2 * VEC];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int32_t at = static_cast<int32_t>(j) + u * kStatsBlock - w0;
-        const bool marked = at < kWindow && (marks[at / 32] >> (at % 32) & 1u);
-        Elem<Tin>::unpack(marked ? neg_inf_vec<Tin>() : vv[u], x + u * VEC);
+      const int s = __builtin_amdgcn_readfirstlane(static_cast<int32_t>(j) - w0) / kStatsBlock;
+      if (s % 64 == 0) {
+        const int word = (s + lane) * NW + wave;
+        rounds = __ballot(word < kWindow / 64 && words[word < kWindow / 64 ? word : 0] != 0);
       }
+      vec4u p[2] = {vv[0], vv[1]};
+      if (rounds >> (s % 64) & 3u) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int word = (s + u) * NW + wave;
+          if (word < kWindow / 64 && (words[word] >> lane & 1u)) p[u] = neg_inf_vec<Tin>();
+        }
+      }
+      float x[2 * VEC];
+      Elem<Tin>::unpack(p[0], x);
+      Elem<Tin>::unpack(p[1], x + VEC);
       out.add(x, c);
     });
     __syncthreads();
   }
-  const RowSum sum_in = merge_block<kStatsBlock>(in, c);
   __syncthreads();
-  const RowSum sum_out = merge_block<kStatsBlock>(out, c);
+  in.add1(z, c);
+  // The entry of a group's first token takes the group's other elements.
+  {
+    uint32_t mine = ~0u;
+    if (e.id >= 0) {
+      mine = 0;
+      int same = 0;
+      for (int i = 0; i < n; i += 4) {
+        const vec4u o = *reinterpret_cast<const vec4u*>(sh_id + i);
+        const uint32_t base = static_cast<uint32_t>(q.base), id = static_cast<uint32_t>(e.id);
+        const uint32_t d[4] = {o.x - base, o.y - base, o.z - base, o.w - base};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) mine |= d[u] < static_cast<uint32_t>(q.len) ? 1u << d[u] : 0u;
+        same += (o.x == id ? 1 : 0) + (o.y == id ? 1 : 0) + (o.z == id ? 1 : 0) + (o.w == id ? 1 : 0);
+      }
+      if (same > 1) atomicOr(&sh_bad, PR_FLAG_BAD_ID);
+      if (mine & ((1u << (e.id - q.base)) - 1u)) mine = ~0u;
+    }
+    float other[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+      other[i] = i < q.len && !(mine >> i & 1u) ? Elem<Tin>::load1(row, q.base + i) : -INFINITY;
+    out.add(other, c);
+  }
+  DistillPart p;
+  p.in = merge_block<kStatsBlock>(in, c);
+  __syncthreads();
+  p.out = merge_block<kStatsBlock>(out, c);
   // A probability of 0 adds nothing, whatever the student makes of its token.
-  const double q = e.id >= 0 ? exp(static_cast<double>(e.logq)) : 0.0;
-  EntrySums s{q, 0.0};
-  if (q > 0.0)
-    s.cross = q * (static_cast<double>(e.logq) - static_cast<double>(z) / static_cast<double>(T));
-  s = sum_entries<kStatsBlock>(s);
-  if (t != 0) return;
-  const RowLoss x = row_loss(a, sum_in, sum_out, s, sh_bad, T, c, w);
+  const double w = e.id >= 0 ? exp(static_cast<double>(e.logq)) : 0.0;
+  EntrySums s{w, 0.0};
+  if (w > 0.0) s.cross = w * (static_cast<double>(e.logq) - static_cast<double>(z) / static_cast<double>(T));
+  p.entries = sum_entries<kStatsBlock>(s);
+  p.bad = sh_bad;
+  p.pad = 0;
+  return p;
+}
+
+// One workgroup per row: its sums and everything but its gradient.
+template <typename Tin>
+__global__ __launch_bounds__(kStatsBlock) void distill_stats_kernel(DistillArgs a, double* term, RowDistill* rd,
+                                                                   int64_t first) {
+  const int64_t r = first + blockIdx.x;
+  const float w = a.rows.weight[r];
+  RowLoss x = masked_row();
+  if (w != 0.0f) {
+    const float T = a.rows.temperature[r], c = scale_of(T);
+    const DistillPart p = row_part<Tin>(a, r, 0, 1, T, c);
+    if (threadIdx.x != 0) return;
+    x = row_loss(a, p.in, p.out, p.entries, p.bad, T, c, w);
+  } else if (threadIdx.x != 0) {
+    return;
+  }
   write_row(a, r, x);
-  term[r] = static_cast<double>(w) * x.loss;
+  term[r] = w == 0.0f ? 0.0 : static_cast<double>(w) * x.loss;
   rd[r] = x.grad;
 }
 
-// The gradients of the rows from `first` on (blockIdx.y), a vector per thread:
+// The parts of a few rows, G of them a row.
+template <typename Tin>
+__global__ __launch_bounds__(kStatsBlock) void distill_parts_kernel(DistillArgs a, DistillPart* part, int G) {
+  const int64_t r = blockIdx.x / G;
+  if (a.rows.weight[r] == 0.0f) return;
+  const float T = a.rows.temperature[r];
+  const DistillPart p = row_part<Tin>(a, r, blockIdx.x % G, G, T, scale_of(T));
+  if (threadIdx.x == 0) part[blockIdx.x] = p;
+}
+
+__device__ __forceinline__ RowSum merge_two(const RowSum& p, const RowSum& q, float c) {
+  RowSum s{fmaxf(p.m, q.m), 0.0f};
+  if (p.m != -INFINITY || p.S != p.S) s.S += p.S * fast_exp2(fmaxf(p.m * c - s.m * c, -kBig));
+  if (q.m != -INFINITY || q.S != q.S) s.S += q.S * fast_exp2(fmaxf(q.m * c - s.m * c, -kBig));
+  return s;
+}
+
+// A row's loss from its parts, by one thread,
+__device__ __forceinline__ RowLoss loss_from_parts(const DistillArgs& a, int64_t r, const DistillPart* part, int G) {
+  const float w = a.rows.weight[r];
+  if (w == 0.0f) return masked_row();
+  const float T = a.rows.temperature[r], c = scale_of(T);
+  DistillPart s = part[r * G];
+#pragma unroll 4
+  for (int g = 1; g < G; ++g) {
+    const DistillPart p = part[r * G + g];
+    s.in = merge_two(s.in, p.in, c);
+    s.out = merge_two(s.out, p.out, c);
+    s.entries.Q += p.entries.Q;
+    s.entries.cross += p.entries.cross;
+    s.bad |= p.bad;
+  }
+  return row_loss(a, s.in, s.out, s.entries, s.bad, T, c, w);
+}
+
+// and by every wave of a workgroup, a lane a part.
+__device__ __forceinline__ RowLoss loss_from_lanes(const DistillArgs& a, int64_t r, const DistillPart* part, int G) {
+  const float w = a.rows.weight[r];
+  if (w == 0.0f) return masked_row();
+  const float T = a.rows.temperature[r], c = scale_of(T);
+  const int lane = threadIdx.x % kWave;
+  DistillPart p{{-INFINITY, 0.0f}, {-INFINITY, 0.0f}, {0.0, 0.0}, 0, 0};
+  if (lane < G) p = part[r * G + lane];
+  const uint32_t bad = (__any(p.bad & PR_FLAG_BAD_ID) ? PR_FLAG_BAD_ID : 0u) |
+                       (__any(p.bad & PR_FLAG_NONFINITE) ? PR_FLAG_NONFINITE : 0u);
+  const EntrySums s{wave_sum_d(p.entries.Q), wave_sum_d(p.entries.cross)};
+  return row_loss(a, merge_lanes(p.in, c), merge_lanes(p.out, c), s, bad, T, c, w);
+}
+
+// All split rows' outputs, gradient factors (rd NULL: not wanted) and the loss,
+// by one workgroup of kGradBlock threads.
+__device__ __forceinline__ void finish_rows(const DistillArgs& a, const DistillPart* part, int G, RowDistill* rd) {
+  __shared__ double sh[kGradBlock / kWave];
+  double sum = 0.0;
+  for (int64_t r = threadIdx.x; r < a.rows.n_rows; r += kGradBlock) {
+    const RowLoss x = loss_from_parts(a, r, part, G);
+    write_row(a, r, x);
+    if (rd) rd[r] = x.grad;
+    const float w = a.rows.weight[r];
+    if (w != 0.0f) sum += static_cast<double>(w) * x.loss;
+  }
+  sum = wave_sum_d(sum);
+  if (threadIdx.x % kWave == 0) sh[threadIdx.x / kWave] = sum;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  sum = 0.0;
+  for (int w = 0; w < kGradBlock / kWave; ++w) sum += sh[w];
+  a.loss[0] = static_cast<float>(sum);
+}
+
+__global__ __launch_bounds__(kGradBlock) void distill_finish_kernel(DistillArgs a, const DistillPart* part, int G,
+                                                                   RowDistill* rd) {
+  finish_rows(a, part, G, rd);
+}
+
+// The gradient of a stretch of a row, a vector per thread of workgroup `part`:
 // short workgroups in memory order, past the caches. Each finds the entries
 // among its own vectors.
 template <typename Tin>
-__global__ __launch_bounds__(kGradBlock) void distill_grad_kernel(DistillArgs a, const RowDistill* rd, int64_t first) {
+__device__ __forceinline__ void grad_stretch(const DistillArgs& a, int64_t r, int part, const RowDistill& q) {
   constexpr int VEC = Elem<Tin>::kVec;
-  __shared__ int32_t sh_id[kMaxTop];
-  __shared__ float sh_q[kMaxTop];
-  __shared__ int sh_n;
-  const int64_t r = first + blockIdx.y;
-  const RowDistill q = rd[r];
-  const int part = blockIdx.x, t = threadIdx.x;
+  __shared__ uint32_t elements[(kGradBlock + 2 * 8) / 4];  // a byte a vector: its entries' elements; then the row's ends
+  __shared__ float value[(kGradBlock + 2) * VEC];           // of those elements: q_k q
+  const int t = threadIdx.x;
   const int32_t V = a.rows.V;
   const Tin* row = row_ptr<Tin>(a.rows, r);
   Tin* out = static_cast<Tin*>(a.rows.grad) + r * a.rows.grad_stride;
@@ -294,38 +408,54 @@ __global__ __launch_bounds__(kGradBlock) void distill_grad_kernel(DistillArgs a,
   if (j < nvec) v = __builtin_nontemporal_load(reinterpret_cast<const vec4u*>(row + h) + j);
   const float zs = s < V ? Elem<Tin>::load1(row, s) : 0.0f;
   const Entry e = load_entry(a, r, t);
-  if (t == 0) sh_n = 0;
+  if (t < static_cast<int>(sizeof(elements) / 4)) elements[t] = 0;
   __syncthreads();
   if (e.id >= 0) {
     const Group g = group_of<Tin>(e.id, h, tail, V);
     if (g.vec < 0 ? part == 0 : g.vec / kGradBlock == part) {
-      const int at = atomicAdd(&sh_n, 1);
-      sh_id[at] = e.id;
-      sh_q[at] = q.q_k * expf(e.logq);
+      const int slot = g.vec < 0 ? kGradBlock - 1 - g.vec : g.vec % kGradBlock, i = e.id - g.base;
+      atomicOr(&elements[slot / 4], 1u << (slot % 4 * 8 + i));
+      value[slot * VEC + i] = q.q_k * expf(e.logq);
     }
   }
   __syncthreads();
-  const int n = sh_n;
+  const uint8_t* byte = reinterpret_cast<const uint8_t*>(elements);
   if (s < V) {
-    float g = q.k * fast_exp2(fmaf(zs, q.c, -q.A));
-    for (int i = 0; i < n; ++i)
-      if (sh_id[i] == s) g = q.in_k * fast_exp2(fmaf(zs, q.c, -q.in_A)) - sh_q[i];
-    GradVec<Tin>::store1(out, s, g);
+    const int slot = kGradBlock + t / 8, i = t % 8;
+    GradVec<Tin>::store1(out, s, byte[slot] >> i & 1u
+                                     ? q.in_k * fast_exp2(fmaf(zs, q.c, -q.in_A)) - value[slot * VEC + i]
+                                     : q.k * fast_exp2(fmaf(zs, q.c, -q.A)));
   }
   if (j >= nvec) return;
   float z[VEC], g[VEC];
   Elem<Tin>::unpack(v, z);
 #pragma unroll
   for (int i = 0; i < VEC; ++i) g[i] = q.k * fast_exp2(fmaf(z[i], q.c, -q.A));
-  const int32_t base = h + j * VEC;
-  for (int i = 0; i < n; ++i) {
-    const int32_t d = sh_id[i] - base;
-    if (d < 0 || d >= VEC) continue;
+  const uint32_t mine = byte[t];
+  if (mine != 0) {
 #pragma unroll
-    for (int u = 0; u < VEC; ++u)
-      if (u == d) g[u] = q.in_k * fast_exp2(fmaf(z[u], q.c, -q.in_A)) - sh_q[i];
+    for (int i = 0; i < VEC; ++i)
+      if (mine >> i & 1u) g[i] = q.in_k * fast_exp2(fmaf(z[i], q.c, -q.in_A)) - value[t * VEC + i];
   }
   stream_grad(out + h + static_cast<int64_t>(j) * VEC, GradVec<Tin>::pack(g));
+}
+
+// The gradients of the rows from `first` on (blockIdx.y).
+template <typename Tin>
+__global__ __launch_bounds__(kGradBlock) void distill_grad_kernel(DistillArgs a, const RowDistill* rd, int64_t first) {
+  const int64_t r = first + blockIdx.y;
+  grad_stretch<Tin>(a, r, blockIdx.x, rd[r]);
+}
+
+// The gradients of a few split rows: each workgroup works out its own row's
+// factors instead of waiting for a kernel that does. The first workgroup of the
+// grid's last row finishes the rows.
+template <typename Tin>
+__global__ __launch_bounds__(kGradBlock) void distill_parts_grad_kernel(DistillArgs a, const DistillPart* part, int G) {
+  if (blockIdx.y + 1 < gridDim.y)
+    grad_stretch<Tin>(a, blockIdx.y, blockIdx.x, loss_from_lanes(a, blockIdx.y, part, G).grad);
+  else if (blockIdx.x == 0)
+    finish_rows(a, part, G, nullptr);
 }
 
 // The entries of a row as the wave that takes them holds them, KE a lane.
@@ -592,46 +722,78 @@ hipError_t launch_held(const DistillArgs& a, int64_t most, double* term, hipStre
   return hipGetLastError();
 }
 
-constexpr int64_t kFewRows = 0;
+// Workgroups per row for a shape (0: rows are not split): as for the policy loss.
+int distill_split(int64_t n_rows, int32_t V, pr_dtype dtype, bool grad) {
+  return policy_split(n_rows, V, dtype, grad);
+}
+
 constexpr int64_t kMostGroups = int64_t{1} << 23;  // a grid holds less than 2^32 threads
 
 template <typename Tin>
-hipError_t distill(const DistillArgs& a, hipStream_t stream) {
-  const int64_t n = a.rows.n_rows;
-  RowDistill* rd = static_cast<RowDistill*>(a.ws);
-  double* term = reinterpret_cast<double*>(rd + n);
-  const int64_t vectors = a.rows.V / Elem<Tin>::kVec;
-  if (n > kFewRows && a.rows.grad && held_row(vectors)) {
-    const hipError_t e = vectors <= kSmallRowVectors ? launch_held<Tin, 7, 19>(a, 2 * kCUs, term, stream)
-                                                     : launch_held<Tin, 15, 20>(a, kCUs, term, stream);
-    return e == hipSuccess ? launch_loss_sum(term, n, 1.0, a.loss, stream) : e;
-  }
-  for (int64_t at = 0; at < n; at += kMostGroups) {
-    const int64_t rows = n - at < kMostGroups ? n - at : kMostGroups;
-    hipLaunchKernelGGL(distill_stats_kernel<Tin>, dim3(static_cast<unsigned>(rows)), dim3(kStatsBlock), 0, stream, a,
-                       term, rd, at);
+hipError_t launch_grad(const DistillArgs& a, const RowDistill* rd, int64_t parts, hipStream_t stream) {
+  constexpr int64_t kMostY = 32768;
+  for (int64_t at = 0; at < a.rows.n_rows; at += kMostY) {
+    const int64_t rows = a.rows.n_rows - at < kMostY ? a.rows.n_rows - at : kMostY;
+    hipLaunchKernelGGL(distill_grad_kernel<Tin>, dim3(static_cast<unsigned>(parts), static_cast<unsigned>(rows)),
+                       dim3(kGradBlock), 0, stream, a, rd, at);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (a.rows.grad) {
-    constexpr int64_t kMostY = 32768;
-    const int64_t nvec = a.rows.V / Elem<Tin>::kVec, parts = nvec > 0 ? (nvec + kGradBlock - 1) / kGradBlock : 1;
-    for (int64_t at = 0; at < n; at += kMostY) {
-      const int64_t rows = n - at < kMostY ? n - at : kMostY;
-      hipLaunchKernelGGL(distill_grad_kernel<Tin>, dim3(static_cast<unsigned>(parts), static_cast<unsigned>(rows)),
-                         dim3(kGradBlock), 0, stream, a, rd, at);
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
+  return hipSuccess;
+}
+
+// The workspace: the rows' gradient factors, then their terms of the loss or,
+// where they are split, their parts.
+template <typename Tin>
+hipError_t distill(const DistillArgs& a, hipStream_t stream) {
+  const int64_t n = a.rows.n_rows;
+  const pr_dtype dtype = sizeof(Tin) == 2 ? PR_BF16 : PR_F32;
+  RowDistill* rd = static_cast<RowDistill*>(a.ws);
+  double* term = reinterpret_cast<double*>(rd + n);
+  const int64_t nvec = a.rows.V / Elem<Tin>::kVec, parts = nvec > 0 ? (nvec + kGradBlock - 1) / kGradBlock : 1;
+  const int G = distill_split(n, a.rows.V, dtype, a.rows.grad != nullptr);
+  hipError_t e = hipSuccess;
+  if (G > 0) {
+    DistillPart* part = reinterpret_cast<DistillPart*>(rd + n);
+    hipLaunchKernelGGL(distill_parts_kernel<Tin>, dim3(static_cast<unsigned>(n * G)), dim3(kStatsBlock), 0, stream, a,
+                       part, G);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (a.rows.grad && n * parts <= kFewGroups) {
+      hipLaunchKernelGGL(distill_parts_grad_kernel<Tin>,
+                         dim3(static_cast<unsigned>(parts), static_cast<unsigned>(n + 1)), dim3(kGradBlock), 0, stream,
+                         a, part, G);
+      return hipGetLastError();
     }
+    hipLaunchKernelGGL(distill_finish_kernel, dim3(1), dim3(kGradBlock), 0, stream, a, part, G,
+                       a.rows.grad ? rd : nullptr);
+    e = hipGetLastError();
+    return e == hipSuccess && a.rows.grad ? launch_grad<Tin>(a, rd, parts, stream) : e;
   }
-  return launch_loss_sum(term, n, 1.0, a.loss, stream);
+  if (n > 0 && a.rows.grad && held_row(nvec)) {
+    e = nvec <= kSmallRowVectors ? launch_held<Tin, 7, 19>(a, 2 * kCUs, term, stream)
+                                 : launch_held<Tin, 15, 20>(a, kCUs, term, stream);
+  } else {
+    for (int64_t at = 0; at < n && e == hipSuccess; at += kMostGroups) {
+      const int64_t rows = n - at < kMostGroups ? n - at : kMostGroups;
+      hipLaunchKernelGGL(distill_stats_kernel<Tin>, dim3(static_cast<unsigned>(rows)), dim3(kStatsBlock), 0, stream, a,
+                         term, rd, at);
+      e = hipGetLastError();
+    }
+    if (e == hipSuccess && a.rows.grad) e = launch_grad<Tin>(a, rd, parts, stream);
+  }
+  return e == hipSuccess ? launch_loss_sum(term, n, 1.0, a.loss, stream) : e;
 }
 
 }  // namespace
 
-size_t distill_workspace_bytes(int64_t n_rows, int32_t, pr_dtype) {
+size_t distill_workspace_bytes(int64_t n_rows, int32_t V, pr_dtype dtype) {
   const size_t n = n_rows < 0 ? 0 : static_cast<size_t>(n_rows);
-  return n * (sizeof(RowDistill) + sizeof(double));
+  int G = distill_split(n_rows, V, dtype, true);
+  const int without = distill_split(n_rows, V, dtype, false);
+  G = G < without ? without : G;
+  const size_t parts = n * static_cast<size_t>(G) * sizeof(DistillPart), terms = n * sizeof(double);
+  return n * sizeof(RowDistill) + (parts > terms ? parts : terms);
 }
 
 hipError_t launch_distill(const DistillArgs& a, pr_dtype dtype, hipStream_t stream) {

@@ -61,6 +61,18 @@ struct RowView {
 constexpr int64_t kLeastRowVectors = 3500, kSmallRowVectors = 19 * 7 * kWave, kRowVectors = 20 * 15 * kWave;
 inline bool held_row(int64_t nvec) { return nvec >= kLeastRowVectors && nvec <= kRowVectors; }
 
+// Few rows whose gradient is wanted are spread over the device although they
+// fit a workgroup: one compute unit alone takes 20 us for 304 KB. Captured
+// calls, spread and held: 16 rows of 151,936 bfloat16 logits 11.7 and 21.6 us,
+// 64 rows 19.5 and 24.2, 96 rows 24.5 and 24.9, 128 rows 29.3 and 25.7, of 40,000
+// float32 logits 32 rows 11.0 and 12.3, 64 rows 14.2 and 13.5; 16 rows of 32,000
+// float32 logits 8.5 and 11.0, 32 rows 11.2 and 11.4, 64 rows 12.6 and 12.0.
+constexpr int64_t kFewRows = 64, kFewSmallRows = 32;
+
+// Most workgroups that each work out their own row's factors: it saves a
+// launch, 1 to 2 us, and costs more than that past this many.
+constexpr int64_t kFewGroups = 512;
+
 // Most rows whose order a kernel works out for itself.
 constexpr int64_t kListedRows = 65536;
 constexpr int kListed = kListedRows / kCUs + 1;

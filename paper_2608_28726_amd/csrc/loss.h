@@ -44,6 +44,9 @@ struct PreferenceArgs {
   void* ws;
 };
 
+// Workgroups along a row for its sums, where few rows are spread over the device.
+int row_parts(int64_t n_rows, int32_t V, pr_dtype dtype);
+
 // Workgroups per row for a shape (0: rows are not split), with or without the
 // gradient, and the workspace that either takes.
 int policy_split(int64_t n_rows, int32_t V, pr_dtype dtype, bool grad);

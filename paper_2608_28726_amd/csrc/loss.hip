@@ -603,32 +603,6 @@ __global__ __launch_bounds__(kPairBlock) void preference_pair_kernel(PreferenceA
 // 400 rows 32.7 and 31.2, 126 and 124.
 constexpr int64_t kSplitRows = 256;
 
-// Workgroups along a row for its sums: about 1,024 in all, each with at least
-// 512 vectors. Preference loss, about 512, 1,024 and 2,048 in all: 128 rows of
-// 151,936 bfloat16 logits 29.3, 30.8 and 33.1 us, 200 rows of as many float32
-// logits 68.6, 66.5 and 67.9, 60 rows of 50,257 bfloat16 logits 13.8, 13.7 and
-// 13.6. At least 256, 512 and 1,024 vectors: 17 rows of 50,257 11.7, 11.4 and
-// 12.1 us, 60 rows 14.7, 13.7 and 15.0, 2 rows of 32,000 10.5, 10.2 and 10.5.
-int row_parts(int64_t n_rows, int32_t V, pr_dtype dtype) {
-  if (n_rows <= 0 || n_rows >= kSplitRows) return 1;
-  const int64_t nvec = V / (dtype == PR_BF16 ? 8 : 4);
-  const int64_t want = (1024 + n_rows - 1) / n_rows, most = nvec / 512;
-  const int64_t G = want < most ? want : most;
-  return static_cast<int>(G < 1 ? 1 : G > kMaxSplit ? kMaxSplit : G);
-}
-
-// Few rows whose gradient is wanted are spread over the device although they
-// fit a workgroup: one compute unit alone takes 20 us for 304 KB. Captured
-// calls, spread and held: 16 rows of 151,936 bfloat16 logits 11.7 and 21.6 us,
-// 64 rows 19.5 and 24.2, 96 rows 24.5 and 24.9, 128 rows 29.3 and 25.7, of 40,000
-// float32 logits 32 rows 11.0 and 12.3, 64 rows 14.2 and 13.5; 16 rows of 32,000
-// float32 logits 8.5 and 11.0, 32 rows 11.2 and 11.4, 64 rows 12.6 and 12.0.
-constexpr int64_t kFewRows = 64, kFewSmallRows = 32;
-
-// Most workgroups that each work out their own row's factors: it saves a
-// launch, 1 to 2 us, and costs more than that past this many.
-constexpr int64_t kFewGroups = 512;
-
 // Workgroups of the launch that starts at `at` of `total`.
 unsigned groups_from(int64_t at, int64_t total) {
   return static_cast<unsigned>(total - at < kMostGroups ? total - at : kMostGroups);
@@ -713,6 +687,20 @@ hipError_t preference(const PreferenceArgs& a, hipStream_t stream) {
 }
 
 }  // namespace
+
+// Workgroups along a row for its sums: about 1,024 in all, each with at least
+// 512 vectors. Preference loss, about 512, 1,024 and 2,048 in all: 128 rows of
+// 151,936 bfloat16 logits 29.3, 30.8 and 33.1 us, 200 rows of as many float32
+// logits 68.6, 66.5 and 67.9, 60 rows of 50,257 bfloat16 logits 13.8, 13.7 and
+// 13.6. At least 256, 512 and 1,024 vectors: 17 rows of 50,257 11.7, 11.4 and
+// 12.1 us, 60 rows 14.7, 13.7 and 15.0, 2 rows of 32,000 10.5, 10.2 and 10.5.
+int row_parts(int64_t n_rows, int32_t V, pr_dtype dtype) {
+  if (n_rows <= 0 || n_rows >= kSplitRows) return 1;
+  const int64_t nvec = V / (dtype == PR_BF16 ? 8 : 4);
+  const int64_t want = (1024 + n_rows - 1) / n_rows, most = nvec / 512;
+  const int64_t G = want < most ? want : most;
+  return static_cast<int>(G < 1 ? 1 : G > kMaxSplit ? kMaxSplit : G);
+}
 
 int policy_split(int64_t n_rows, int32_t V, pr_dtype dtype, bool grad) {
   if (n_rows <= 0 || n_rows >= kSplitRows) return 0;
