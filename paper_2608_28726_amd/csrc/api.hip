@@ -801,8 +801,7 @@ void pr_distill_params_default(pr_distill_params* params) {
 }
 
 size_t pr_distill_loss_workspace(pr_dtype dtype, int64_t n_rows, int32_t vocab, int32_t k) {
-  (void)k;
-  return vocab < 2 ? 0 : distill_workspace_bytes(n_rows, vocab, dtype);
+  return vocab < 2 ? 0 : distill_workspace_bytes(n_rows, vocab, dtype, k);
 }
 
 pr_status pr_distill_loss(const void* logits, pr_dtype dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,

@@ -18,7 +18,7 @@ struct DistillArgs {
   void* ws;
 };
 
-size_t distill_workspace_bytes(int64_t n_rows, int32_t V, pr_dtype dtype);
+size_t distill_workspace_bytes(int64_t n_rows, int32_t V, pr_dtype dtype, int32_t k);
 hipError_t launch_distill(const DistillArgs& a, pr_dtype dtype, hipStream_t stream);
 
 }  // namespace pr
