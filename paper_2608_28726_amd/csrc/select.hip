@@ -225,6 +225,40 @@ __device__ __forceinline__ void in_order(const uint64_t* key, int n, Fn&& fn) {
   }
 }
 
+// The same for longer lists, each key counted against those of its bin alone
+// (larger keys are in the same bin or a larger one); `to` has room for the list.
+// 280 keys took 5.8 us the other way.
+template <int BLOCK, typename Bin, typename Fn>
+__device__ __forceinline__ void in_order_by_bins(const uint64_t* key, uint64_t* to, int n, uint32_t* hist, Bin&& bin_of,
+                                                 Fn&& fn) {
+  constexpr int kFew = 128;
+  if (n <= kFew) return in_order<BLOCK>(key, n, fn);
+  __shared__ uint32_t start[256], end[256];
+  for (int b = threadIdx.x; b < 256; b += BLOCK) hist[b] = 0;
+  __syncthreads();
+  for (int e = threadIdx.x; e < n; e += BLOCK) atomicAdd(&hist[bin_of(key[e])], 1u);
+  __syncthreads();
+  if (threadIdx.x < kWave) {
+    const int b = 252 - 4 * static_cast<int>(threadIdx.x);  // bins b + 3 .. b: descending order
+    const uint32_t n3 = hist[b + 3], n2 = hist[b + 2], n1 = hist[b + 1], n0 = hist[b];
+    const uint32_t s3 = wave_incl_scan_u(n3 + n2 + n1 + n0) - (n3 + n2 + n1 + n0);
+    start[b + 3] = end[b + 3] = s3;
+    start[b + 2] = end[b + 2] = s3 + n3;
+    start[b + 1] = end[b + 1] = s3 + n3 + n2;
+    start[b] = end[b] = s3 + n3 + n2 + n1;
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < n; e += BLOCK) to[atomicAdd(&end[bin_of(key[e])], 1u)] = key[e];
+  __syncthreads();
+  for (int e = threadIdx.x; e < n; e += BLOCK) {
+    const uint64_t mine = to[e];
+    const int b = bin_of(mine);
+    int place = static_cast<int>(start[b]);
+    for (uint32_t i = start[b]; i < end[b]; ++i) place += to[i] > mine ? 1 : 0;
+    fn(place, mine);
+  }
+}
+
 // The k largest logits of a stretch and a few beside them, as keys in s.key;
 // returns how many. One pass: the first vectors of all lanes give a floor that
 // k logits reach; from there on every vector with a logit that reaches the floor
@@ -233,8 +267,16 @@ __device__ __forceinline__ void in_order(const uint64_t* key, int n, Fn&& fn) {
 // to the bin that the k-th largest counted is in. The waves do not wait for each
 // other: a floor read late lists more. Rows in which far too many vectors reach
 // the floor (many equal logits, or rising ones) are selected from by digits.
+struct Bins {
+  float low, scale;
+  __device__ __forceinline__ int of(float z) const {
+    return min(255, static_cast<int>(fmaxf((z - low) * scale, 0.0f)));
+  }
+  __device__ __forceinline__ int operator()(uint64_t key) const { return of(key_logit(key)); }
+};
+
 template <typename Tin, int BLOCK, int KMAX>
-__device__ int list_stretch(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK, KMAX>& s, RowSum* sum) {
+__device__ int list_stretch(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK, KMAX>& s, RowSum* sum, Bins* bins) {
   constexpr int VEC = Elem<Tin>::kVec, NW = BLOCK / kWave, LD = 4, CAP = ListLds<BLOCK, KMAX>::CAP;
   const int t = threadIdx.x, wave = t / kWave;
   const bool lead = t % kWave == 0;
@@ -283,7 +325,8 @@ __device__ int list_stretch(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK
   bin0 = floor0 > -INFINITY ? floor0 : bin0;
   floor0 = fmaxf(floor0, kNegSentinel);
   const float width = (top0 - bin0) * (1.0f / 255.0f), scale = width > 0.0f && width < INFINITY ? 1.0f / width : 0.0f;
-  auto bin_of = [&](float z) { return min(255, static_cast<int>(fmaxf((z - bin0) * scale, 0.0f))); };
+  *bins = Bins{bin0, scale};
+  auto bin_of = [&](float z) { return bins->of(z); };
   if (t == 0) s.floor = floor0;
   __syncthreads();
 
@@ -391,6 +434,15 @@ __device__ int list_stretch(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK
   });
 }
 
+// The places of the keys that list_stretch has left.
+template <int BLOCK, int KMAX, typename Fn>
+__device__ __forceinline__ void list_order(ListLds<BLOCK, KMAX>& s, int n, const Bins& bins, Fn&& fn) {
+  if constexpr (KMAX <= 64)
+    in_order<BLOCK>(s.key, n, fn);
+  else
+    in_order_by_bins<BLOCK>(s.key, s.key + ListLds<BLOCK, KMAX>::KEYS / 2, n, s.hist, bins, fn);
+}
+
 // What log-probs of a row come from: log p of a logit is (z - m) / T - lnS.
 struct RowNorm {
   double lnS;
@@ -414,9 +466,10 @@ __device__ __forceinline__ RowNorm row_norm(const RowSum& p, float T) {
   return x;
 }
 
-// Writes a row's first k tokens in order from the n listed ones.
-template <int BLOCK>
-__device__ __forceinline__ void write_top(const TopArgs& a, int64_t r, const RowNorm& x, const uint64_t* key, int n) {
+// Writes a row's first k tokens in order from the n listed ones. order(n, fn)
+// gives the list's places.
+template <int BLOCK, typename Order>
+__device__ __forceinline__ void write_top(const TopArgs& a, int64_t r, const RowNorm& x, int n, Order&& order) {
   const int t = threadIdx.x;
   const bool bad = x.flags != 0;
   const float nan = __uint_as_float(0x7fc00000u);
@@ -425,7 +478,7 @@ __device__ __forceinline__ void write_top(const TopArgs& a, int64_t r, const Row
     if (a.flags) a.flags[r] = x.flags;
   }
   if (bad) n = 0;
-  in_order<BLOCK>(key, n, [&](int place, uint64_t mine) {
+  order(n, [&](int place, uint64_t mine) {
     if (place >= a.k) return;
     a.ids[r * a.k + place] = key_index(mine);
     a.logprob[r * a.k + place] = static_cast<float>(x.logprob(key_logit(mine)));
@@ -443,16 +496,20 @@ __global__ __launch_bounds__(BLOCK) void top_kernel(TopArgs a, int64_t first) {
   const float T = a.temperature[r];
   const Stretch<Tin> x(static_cast<const Tin*>(a.logits) + r * a.row_stride, a.V, 0, 1);
   RowSum sum;
-  const int n = list_stretch<Tin, BLOCK, KMAX>(x, a.k, scale_of(T), s, &sum);
-  write_top<BLOCK>(a, r, row_norm(sum, T), s.key, n);
+  Bins bins;
+  const int n = list_stretch<Tin, BLOCK, KMAX>(x, a.k, scale_of(T), s, &sum, &bins);
+  write_top<BLOCK>(a, r, row_norm(sum, T), n, [&](int m, auto fn) { list_order<BLOCK, KMAX>(s, m, bins, fn); });
 }
 
 // The first k tokens of a part of a row in order, 0 after the last, and the part's sum.
-template <int BLOCK>
-__device__ __forceinline__ void write_part(uint64_t* list, RowSum* to, int k, const RowSum& sum, const uint64_t* key, int n) {
-  const int t = threadIdx.x;
+template <typename Tin, int BLOCK, int KMAX>
+__device__ __forceinline__ void write_part(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK, KMAX>& s, uint64_t* list,
+                                           RowSum* to) {
+  RowSum sum;
+  Bins bins;
+  const int t = threadIdx.x, n = list_stretch<Tin, BLOCK, KMAX>(x, k, c, s, &sum, &bins);
   if (t == 0) *to = sum;
-  in_order<BLOCK>(key, n, [&](int place, uint64_t mine) {
+  list_order<BLOCK, KMAX>(s, n, bins, [&](int place, uint64_t mine) {
     if (place < k) list[place] = mine;
   });
   if (t >= n && t < k) list[t] = 0;
@@ -464,18 +521,17 @@ __global__ __launch_bounds__(BLOCK) void top_parts_kernel(TopArgs a, uint64_t* l
   __shared__ ListLds<BLOCK, KMAX> s;
   const int64_t r = blockIdx.x / a.G;
   const Stretch<Tin> x(static_cast<const Tin*>(a.logits) + r * a.row_stride, a.V, blockIdx.x % a.G, a.G);
-  RowSum sum;
-  const int n = list_stretch<Tin, BLOCK, KMAX>(x, a.k, scale_of(a.temperature[r]), s, &sum);
-  write_part<BLOCK>(list + static_cast<int64_t>(blockIdx.x) * a.k, sums + blockIdx.x, a.k, sum, s.key, n);
+  write_part<Tin, BLOCK, KMAX>(x, a.k, scale_of(a.temperature[r]), s, list + static_cast<int64_t>(blockIdx.x) * a.k,
+                               sums + blockIdx.x);
 }
 
-// The m-th largest of the wave's values, N of each lane (0: there are fewer
-// above 0). m <= 64 N; `used` of the N are looked at.
+// The m-th largest of the wave's values, N of each lane, to its upper 20 bits (0:
+// there are fewer above 0). m <= 64 N; `used` of the N are looked at.
 template <int N>
 __device__ __forceinline__ uint32_t wave_nth(const uint32_t (&v)[N], int used, int m) {
   uint32_t at = 0;
 #pragma unroll 1
-  for (int bit = 31; bit >= 0; --bit) {
+  for (int bit = 31; bit >= 12; --bit) {
     const uint32_t up = at | 1u << bit;
     int n = 0;
 #pragma unroll
@@ -543,7 +599,10 @@ __global__ __launch_bounds__(kRowBlock) void top_merge_kernel(TopArgs a, const u
       if (cut.takes(x[i])) key[atomicAdd(&n_key, 1u)] = x[i];
     __syncthreads();
   }
-  write_top<kRowBlock>(a, r, norm, key, close_list(key, static_cast<int>(n_key)));
+  const int n = close_list(key, static_cast<int>(n_key));
+  write_top<kRowBlock>(a, r, norm, n, [&](int m, auto fn) {
+    in_order_by_bins<kRowBlock>(key, key + kMaxSplit * kMaxTop / 2, m, hist, bin_of, fn);
+  });
 }
 
 // ---------------------------------------------------------------------------
@@ -566,9 +625,8 @@ __global__ __launch_bounds__(BLOCK) void beam_rows_kernel(BeamArgs a, RowSum* su
   uint32_t flags;
   if (!beam_live(a, r, &flags)) return;
   const Stretch<Tin> x(static_cast<const Tin*>(a.logits) + r * a.row_stride, a.V, blockIdx.x % a.G, a.G);
-  RowSum sum;
-  const int n = list_stretch<Tin, BLOCK, KMAX>(x, a.k, scale_of(a.temperature[r]), s, &sum);
-  write_part<BLOCK>(list + static_cast<int64_t>(blockIdx.x) * a.k, sums + blockIdx.x, a.k, sum, s.key, n);
+  write_part<Tin, BLOCK, KMAX>(x, a.k, scale_of(a.temperature[r]), s, list + static_cast<int64_t>(blockIdx.x) * a.k,
+                               sums + blockIdx.x);
 }
 
 // A candidate of a request in the order of the selection: score, lower beam,
@@ -613,12 +671,14 @@ __global__ __launch_bounds__(kBeamBlock) void beam_merge_kernel(BeamArgs a, cons
     for (int i = 0; i < HELD; ++i) token[i] = t + i * kBeamBlock < N ? mine[t + i * kBeamBlock] : 0;
   }
   if (t < a.B) {
+    // (The sums of a beam that is not live are read all the same: at once with its score.)
+    const float score = a.scores[first + t], T = a.temperature[first + t];
+    const RowNorm y = row_norm(merge_parts(sums + (first + t) * a.G, a.G, scale_of(T)), T);
     uint32_t flags;
     const bool live = beam_live(a, first + t, &flags);
-    const float score = a.scores[first + t], T = a.temperature[first + t];
     RowNorm x{0.0, 0.0f, 1.0f, 0};
     if (live) {
-      x = row_norm(merge_parts(sums + (first + t) * a.G, a.G, scale_of(T)), T);
+      x = y;
       flags = x.flags;
     }
     norm[t] = x;
