@@ -564,16 +564,38 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, temperature=1.0, k: 
     temperature = _as_row_tensor(temperature, n, device)
     _check_row_floats(device, n, temperature=temperature)
     L = _abi.lib()
-    m = n_req * k
-    ws, ws_bytes, (best, logprob) = _loss_outputs((m, m), workspace, L.pr_beam_select_workspace(code, n_req, B, V, k),
-                                                  device)
-    parent, token, flags = torch.empty(2 * m + n, dtype=torch.int32, device=device).unsafe_split_with_sizes((m, m, n))
+    need = L.pr_beam_select_workspace(code, n_req, B, V, k)
+    # The outputs as rows of k, so that they are split off without views.
+    if workspace is not None:
+        _check_workspace(workspace, device)
+    if workspace is None or workspace.numel() * workspace.element_size() < need or workspace.data_ptr() % 16:
+        workspace, best, logprob = torch.empty((-(-need // (4 * k)) + 2 * n_req, k), device=device).unsafe_split_with_sizes(
+            (-(-need // (4 * k)), n_req, n_req))
+    else:
+        best, logprob = torch.empty((2 * n_req, k), device=device).unsafe_split_with_sizes((n_req, n_req))
+    ws_bytes = workspace.numel() * workspace.element_size()
+    parent, token = torch.empty((2 * n_req, k), dtype=torch.int32, device=device).unsafe_split_with_sizes((n_req, n_req))
+    flags = torch.empty(n, dtype=torch.int32, device=device)
     out = _abi.BeamOut(best.data_ptr(), parent.data_ptr(), token.data_ptr(), logprob.data_ptr(), flags.data_ptr())
     st = L.pr_beam_select(logits.data_ptr(), code, n_req, B, V, _row_stride(logits), temperature.data_ptr(),
-                          scores.data_ptr(), _ptr(done), done_token, k, C.byref(out), ws, ws_bytes, stream)
+                          scores.data_ptr(), _ptr(done), done_token, k, C.byref(out), workspace.data_ptr(), ws_bytes,
+                          stream)
     _abi.check("pr_beam_select", st)
-    return {"scores": best.view(n_req, k), "parent": parent.view(n_req, k), "token": token.view(n_req, k),
-            "logprob": logprob.view(n_req, k), "flags": flags}
+    return {"scores": best, "parent": parent, "token": token, "logprob": logprob, "flags": flags}
+
+
+def _beam_stride(x, rows: int, size: int, n_req: int, B: int) -> int:
+    """Elements from beam to beam of a state whose first `rows` dimensions count the beams, each of `size` elements."""
+    run = 1
+    for d, extent in zip(reversed(x.stride()[rows:]), reversed(x.shape[rows:])):
+        if extent != 1 and d != run:
+            raise ValueError("a beam's part of a state must be contiguous, and the beams' apart")
+        run *= extent
+    # One beam in all, or one of each request, may come with any stride between those that do not exist.
+    step = size if n_req * B == 1 else x.stride(0) if rows == 1 or B == 1 else x.stride(1)
+    if step < size or (rows == 2 and B > 1 and n_req > 1 and x.stride(0) != B * step):
+        raise ValueError("a beam's part of a state must be contiguous, and the beams' apart")
+    return step
 
 
 def beam_reorder(states, parent: torch.Tensor) -> None:
@@ -593,33 +615,26 @@ def beam_reorder(states, parent: torch.Tensor) -> None:
     if not 1 <= B <= _abi.PR_MAX_BEAMS:
         raise ValueError(f"parent must have 1 to {_abi.PR_MAX_BEAMS} beams")
     n = n_req * B
-    S = (_abi.BeamState * len(states))()
-    for t, x in zip(S, states):
+    fields = []  # of a BeamState each
+    for x in states:
         if x.device != device:
             raise ValueError(f"states must be tensors on {device}")
         if x.dim() >= 1 and x.shape[0] == n:
-            inner, stride, rows = x.shape[1:], x.stride(), 1
+            rows = 1
         elif x.dim() >= 2 and x.shape[:2] == parent.shape:
-            inner, stride, rows = x.shape[2:], x.stride()[1:], 2
-            if B > 1 and n_req > 1 and x.stride(0) != B * x.stride(1):
-                inner = None
+            rows = 2
         else:
             raise ValueError(f"states must be [{n}, ...] or [{n_req}, {B}, ...] tensors")
-        size = 1
-        if inner is not None:
-            for d, extent in zip(reversed(x.stride()[rows:]), reversed(inner)):
-                if extent != 1 and d != size:
-                    inner = None
-                    break
-                size *= extent
-        if n == 0 or (inner is not None and size == 0):
+        if x.numel() == 0:
             continue  # nothing to move
-        # One row, or one request of one beam, may come with any stride.
-        step = size if n == 1 else (x.stride(0) if rows == 1 or B == 1 else stride[0])
-        if inner is None or step < size:
-            raise ValueError("a beam's part of a state must be contiguous, and the beams' apart")
-        t.rows, t.row_bytes, t.row_stride = x.data_ptr(), size * x.element_size(), step * x.element_size()
-    _abi.check("pr_beam_reorder", _abi.lib().pr_beam_reorder(S, len(S), parent.data_ptr(), n_req, B, stream))
+        size = x.numel() // n
+        step = size
+        if not x.is_contiguous():
+            step = _beam_stride(x, rows, size, n_req, B)
+        item = x.element_size()
+        fields += (x.data_ptr(), size * item, step * item)
+    S = (C.c_int64 * len(fields))(*fields)
+    _abi.check("pr_beam_reorder", _abi.lib().pr_beam_reorder(S, len(fields) // 3, parent.data_ptr(), n_req, B, stream))
 
 
 # ---------------------------------------------------------------------------

@@ -215,7 +215,7 @@ def lib() -> C.CDLL:
     L.pr_beam_select_workspace.restype = sz
     L.pr_beam_select.argtypes = [vp, C.c_int, i32, i32, i32, i64, vp, vp, vp, i32, i32, C.POINTER(BeamOut), vp, sz, vp]
     L.pr_beam_select.restype = C.c_int
-    L.pr_beam_reorder.argtypes = [C.POINTER(BeamState), i32, vp, i32, i32, vp]
+    L.pr_beam_reorder.argtypes = [vp, i32, vp, i32, i32, vp]
     L.pr_beam_reorder.restype = C.c_int
     L.pr_stream_reorder.argtypes = [vp, vp, vp, i32, i32, vp]
     L.pr_stream_reorder.restype = C.c_int

@@ -75,7 +75,7 @@ def test_too_many(L):
 
 def reorder(L, states, n=3, B=2, parent=P, count=None):
     a = _abi()
-    S = (a.BeamState * max(1, len(states)))(*[a.BeamState(C.c_void_p(p), b, s) for p, b, s in states])
+    S = (a.BeamState * max(1, len(states)))(*[a.BeamState(p, b, s) for p, b, s in states])
     return L.pr_beam_reorder(S if states or count is None else None, len(states) if count is None else count, parent, n, B, None)
 
 
