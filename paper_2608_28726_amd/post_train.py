@@ -11,9 +11,14 @@ a point when it is one of a quarter of the vocabulary.
 - ``preference``: two answers are drawn for each context, the one that earned
   more is the chosen one, and the reference is the layer it started from.
 
+- ``distill``: a wider-spread teacher layer decodes an answer to each context
+  by beam search (:mod:`beam_search`), the largest logits of the contexts that
+  it passed are kept (:func:`top_logits`), and the layer learns them with
+  :func:`distill_loss`. A token earns a point when it is the teacher's.
+
 Afterwards the answers are scored and routed as in serving.
 
-    python -m paper_2608_28726_amd.post_train [policy|preference] [steps]
+    python -m paper_2608_28726_amd.post_train [policy|preference|distill] [steps]
 """
 
 from __future__ import annotations
@@ -23,8 +28,10 @@ import sys
 import torch
 
 import paper_2608_28726_amd as pr
+from paper_2608_28726_amd.beam_search import search
 
 TEMPERATURE = 1.0
+TOP, BEAMS = 32, 4  # of a teacher: the logits kept of each row, the beams of an answer
 
 
 class OutputLayer:
@@ -73,11 +80,30 @@ def _preference_step(layer, hidden, earns, weight, length, lr, seed, step, ref, 
     return out["loss"], reward.mean()
 
 
+def _teacher(hidden, vocab, length, seed):
+    """A teacher's answers to the contexts: the hidden rows along each best beam, and what is kept of its logits there."""
+    g = torch.Generator(device=hidden.device)
+    g.manual_seed(seed + 2)
+    width = hidden.shape[1]
+    weight = torch.empty(vocab, width, device=hidden.device).normal_(std=2.0 * width ** -0.5, generator=g).bfloat16()
+    answers = search(lambda h: h @ weight.t(), hidden[::length].contiguous(), vocab, BEAMS, length, seed, TEMPERATURE)
+    rows = answers["contexts"][:, 0].reshape(-1, width).contiguous()
+    return rows, pr.top_logits(rows @ weight.t(), min(TOP, vocab), TEMPERATURE)
+
+
+def _distill_step(layer, rows, top, weight, lr):
+    logits = layer.logits(rows)
+    agree = pr.top_logits(logits, 1, TEMPERATURE)["ids"][:, 0] == top["ids"][:, 0]
+    out = pr.distill_loss(logits, top["ids"], top["logprob"], TEMPERATURE, weight, grad=logits)
+    layer.step(rows, out["grad"], lr)
+    return out["loss"], agree.float().mean()
+
+
 def post_train(method: str = "policy", steps: int = 60, vocab: int = 4096, width: int = 64, requests: int = 64,
                length: int = 8, lr: float = 0.02, state_bits: int = 8, seed: int = 0, device="cuda") -> dict:
     """Runs the example; returns the losses and mean rewards of the steps and the share of answers that would ship."""
-    if method not in ("policy", "preference"):
-        raise ValueError("method must be 'policy' or 'preference'")
+    if method not in ("policy", "preference", "distill"):
+        raise ValueError("method must be 'policy', 'preference' or 'distill'")
     g = torch.Generator(device=device)
     g.manual_seed(seed + 1)
     n = requests * length
@@ -94,6 +120,13 @@ def post_train(method: str = "policy", steps: int = 60, vocab: int = 4096, width
             loss, reward = _policy_step(layer, hidden, earns, weight, length, lr, seed, step)
             losses.append(loss)
             rewards.append(reward)
+    elif method == "distill":
+        hidden, top = _teacher(hidden, vocab, length, seed)
+        weight = torch.full((n,), 1.0 / n, device=device)
+        for step in range(steps):
+            loss, reward = _distill_step(layer, hidden, top, weight, lr)
+            losses.append(loss)
+            rewards.append(reward)
     else:
         ref = layer.copy.clone()
         twice = torch.cat([hidden, hidden])
@@ -106,8 +139,9 @@ def post_train(method: str = "policy", steps: int = 60, vocab: int = 4096, width
     ids, feats, _ = pr.sample_features(layer.logits(hidden), TEMPERATURE, seed, offset=steps)
     score = pr.request_aggregate(feats, offsets)["score"]
     _, n_ship = pr.route(score, float(score.median()))
+    earned = earns[ids.long()] if method != "distill" else (ids == top["ids"][:, 0]).float()
     return {"loss": torch.cat(losses).tolist(), "reward": torch.stack(rewards).tolist(),
-            "reward_after": float(earns[ids.long()].mean()), "shipped": int(n_ship) / requests}
+            "reward_after": float(earned.mean()), "shipped": int(n_ship) / requests}
 
 
 def main(argv) -> int:
