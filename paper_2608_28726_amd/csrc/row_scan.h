@@ -330,8 +330,7 @@ __device__ __forceinline__ RowCtx row_ctx(const RowArgs& a, int64_t r, const voi
 }
 
 // Logits are read exactly once: nontemporal loads do not keep them cached.
-template <typename Vec>
-__device__ __forceinline__ vec4u load_stream(const Vec* p) {
+__device__ __forceinline__ vec4u load_stream(const vec4u* p) {
 #ifndef PR_CACHED_LOADS
   return __builtin_nontemporal_load(p);
 #else
@@ -361,8 +360,9 @@ __device__ __forceinline__ bool stretch_full(int64_t vb, int64_t ve) {
 // The first LD vectors of a lane in the vector index range [vb, ve) of a
 // row (-inf past the end). Issued before the row's other inputs are read,
 // so that their latency overlaps.
-template <typename Tin, int BLOCK, int LD, typename Vec>
-__device__ __forceinline__ void vector_prefetch(const Vec* vp, int64_t vb, int64_t ve, vec4u (&v)[LD]) {
+template <typename Tin, int BLOCK, int LD>
+__device__ __forceinline__ void stretch_prefetch(const void* row, int64_t h, int64_t vb, int64_t ve, vec4u (&v)[LD]) {
+  const vec4u* vp = reinterpret_cast<const vec4u*>(static_cast<const Tin*>(row) + h);
   const int64_t i = vb + threadIdx.x;
   if (stretch_full<BLOCK, LD>(vb, ve)) {
 #pragma unroll
@@ -374,11 +374,6 @@ __device__ __forceinline__ void vector_prefetch(const Vec* vp, int64_t vb, int64
       v[u] = j < ve ? load_stream(vp + j) : neg_inf_vec<Tin>();
     }
   }
-}
-
-template <typename Tin, int BLOCK, int LD>
-__device__ __forceinline__ void stretch_prefetch(const void* row, int64_t h, int64_t vb, int64_t ve, vec4u (&v)[LD]) {
-  vector_prefetch<Tin, BLOCK, LD>(reinterpret_cast<const vec4u*>(static_cast<const Tin*>(row) + h), vb, ve, v);
 }
 
 // The loop over the vector index range [vb, ve) of a row shared by every
@@ -393,8 +388,8 @@ __device__ __forceinline__ void stretch_prefetch(const void* row, int64_t h, int
 // of probability 0 that changes no result). A wave with fewer than LD
 // vectors in some lane holds its whole share after the prefetch. Steps of a
 // wave are reduced in increasing index order.
-template <typename Tin, int BLOCK, int U, int LD, typename Vec, typename Body>
-__device__ __forceinline__ void stream_stretch(const Vec* vp, int64_t vb, int64_t ve, vec4u (&v)[LD], Body&& body) {
+template <typename Tin, int BLOCK, int U, int LD, typename Body>
+__device__ __forceinline__ void stream_stretch(const vec4u* vp, int64_t vb, int64_t ve, vec4u (&v)[LD], Body&& body) {
   static_assert(LD % U == 0, "load depth must be a multiple of the compute width");
   int64_t i = vb + threadIdx.x;                 // the lane's vector in v[0]
   int64_t i0 = vb + wave_first_thread();        // the same for the wave's first lane (scalar)

@@ -139,6 +139,68 @@ struct Stretch {
   }
 };
 
+// The loads of a stretch and the loop over its vectors: those of scan::
+// stretch_prefetch and scan::stream_stretch (row_scan.h), for vectors of an
+// element's alignment. v holds the lane's first LD vectors; body(vv, j) reduces
+// the U vectors vv[0..U) of indices j + u BLOCK; lanes past the end see -inf.
+template <typename Tin>
+__device__ __forceinline__ vec4u load_vector(const typename Stretch<Tin>::Vec* p) {
+  return static_cast<vec4u>(__builtin_nontemporal_load(p));
+}
+
+template <typename Tin, int BLOCK, int LD>
+__device__ __forceinline__ void prefetch(const Stretch<Tin>& x, vec4u (&v)[LD]) {
+  const auto* vp = x.vectors();
+  const int32_t i = x.vb + static_cast<int32_t>(threadIdx.x);
+  if (x.vb + scan::wave_first_thread() + (kWave - 1) + (LD - 1) * BLOCK < x.ve) {
+#pragma unroll
+    for (int u = 0; u < LD; ++u) v[u] = load_vector<Tin>(vp + i + u * BLOCK);
+  } else {
+#pragma unroll
+    for (int u = 0; u < LD; ++u) {
+      const int32_t j = i + u * BLOCK;
+      v[u] = j < x.ve ? load_vector<Tin>(vp + j) : neg_inf_vec<Tin>();
+    }
+  }
+}
+
+template <typename Tin, int BLOCK, int U, int LD, typename Body>
+__device__ __forceinline__ void stream(const Stretch<Tin>& x, vec4u (&v)[LD], Body&& body) {
+  const auto* vp = x.vectors();
+  const int64_t ve = x.ve;
+  int64_t i = x.vb + static_cast<int32_t>(threadIdx.x);
+  int64_t i0 = x.vb + scan::wave_first_thread();
+  if (i0 + (kWave - 1) + (LD - 1) * BLOCK < ve) {
+    // Two buffers: the loads of one are issued before the other is reduced.
+    for (; i0 + (kWave - 1) + (3 * LD - 1) * BLOCK < ve; i += 2 * LD * BLOCK, i0 += 2 * LD * BLOCK) {
+      vec4u w[LD];
+#pragma unroll
+      for (int u = 0; u < LD; ++u) w[u] = load_vector<Tin>(vp + i + (LD + u) * BLOCK);
+#pragma unroll
+      for (int c = 0; c < LD; c += U) body(v + c, i + c * BLOCK);
+#pragma unroll
+      for (int u = 0; u < LD; ++u) v[u] = load_vector<Tin>(vp + i + (2 * LD + u) * BLOCK);
+#pragma unroll
+      for (int c = 0; c < LD; c += U) body(w + c, i + (LD + c) * BLOCK);
+    }
+    for (; i0 < ve; i += LD * BLOCK, i0 += LD * BLOCK) {
+      vec4u w[LD];
+#pragma unroll
+      for (int u = 0; u < LD; ++u) {
+        const int64_t j = i + (LD + u) * BLOCK;
+        w[u] = j < ve ? load_vector<Tin>(vp + j) : neg_inf_vec<Tin>();
+      }
+#pragma unroll
+      for (int c = 0; c < LD; c += U) body(v + c, i + c * BLOCK);
+#pragma unroll
+      for (int u = 0; u < LD; ++u) v[u] = w[u];
+    }
+  } else if (i0 < ve) {
+#pragma unroll
+    for (int c = 0; c < LD; c += U) body(v + c, i + c * BLOCK);
+  }
+}
+
 // What a stretch lists: vectors, later keys in their place. KMAX: the largest k
 // that the lists are made for (a row of ordinary logits lists about
 // k (1 + log(the row / the first vectors)) vectors).
@@ -262,11 +324,12 @@ __device__ __forceinline__ void in_order_by_bins(const uint64_t* key, uint64_t* 
 // The k largest logits of a stretch and a few beside them, as keys in s.key;
 // returns how many. One pass: the first vectors of all lanes give a floor that
 // k logits reach; from there on every vector with a logit that reaches the floor
-// is listed, and its largest logit counted in 256 bins between the floor and the
-// largest of the first vectors; the wave that lists a k-th one raises the floor
-// to the bin that the k-th largest counted is in. The waves do not wait for each
-// other: a floor read late lists more. Rows in which far too many vectors reach
-// the floor (many equal logits, or rising ones) are selected from by digits.
+// is listed, and its largest logit counted in 256 bins from the floor on; the
+// wave that lists a k-th one raises the floor to the bin that the k-th largest
+// counted is in. The waves do not wait for each other: a floor read late lists
+// more. Where more vectors reach the floor than are held (rising logits), the
+// stretch is read again with the floor that those give; where that does not help
+// (many equal logits), it is selected from by digits.
 struct Bins {
   float low, scale;
   __device__ __forceinline__ int of(float z) const {
@@ -281,7 +344,7 @@ __device__ int list_stretch(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK
   const int t = threadIdx.x, wave = t / kWave;
   const bool lead = t % kWave == 0;
   vec4u v[LD];
-  scan::vector_prefetch<Tin, BLOCK, LD>(x.vectors(), x.vb, x.ve, v);
+  prefetch<Tin, BLOCK>(x, v);
   const float zt = x.tail_logit(t);
   for (int i = t; i < 256; i += BLOCK) s.hist[i] = 0;
   if (t == 0) s.n = 0;
@@ -324,7 +387,9 @@ __device__ int list_stretch(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK
   // start at the least vector's largest.
   bin0 = floor0 > -INFINITY ? floor0 : bin0;
   floor0 = fmaxf(floor0, kNegSentinel);
-  const float width = (top0 - bin0) * (1.0f / 255.0f), scale = width > 0.0f && width < INFINITY ? 1.0f / width : 0.0f;
+  // Half as far again above the first vectors' largest: where the k-th of a long
+  // row is above that one, the floor would not come near it.
+  const float width = (top0 - bin0) * (1.5f / 255.0f), scale = width > 0.0f && width < INFINITY ? 1.0f / width : 0.0f;
   *bins = Bins{bin0, scale};
   auto bin_of = [&](float z) { return bins->of(z); };
   if (t == 0) s.floor = floor0;
@@ -340,8 +405,18 @@ __device__ int list_stretch(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK
       atomicAdd(&s.hist[bin_of(top)], 1u);
     }
   };
+  auto edge = [&](int b) {  // a sixteenth of a bin below it: the bins' own roundings are less
+    return bin0 + (static_cast<float>(b) - 0.0625f) * width;
+  };
+  auto raise_floor = [&](bool raise) {
+    if (!__any(raise)) return;
+    const int b = cut_bin(s.hist, static_cast<uint32_t>(k));
+    const bool full = s.n > static_cast<uint32_t>(CAP);  // list no more
+    if ((b > 0 || full) && lead)
+      __hip_atomic_store(&s.floor, full ? INFINITY : edge(b), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  };
   LaneSum<true> L;
-  scan::stream_stretch<Tin, BLOCK, 2, LD>(x.vectors(), x.vb, x.ve, v, [&](const vec4u* vv, int64_t j) {
+  stream<Tin, BLOCK, 2>(x, v, [&](const vec4u* vv, int64_t j) {
     const float floor = __hip_atomic_load(&s.floor, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     float z[2 * VEC], top[2];
 #pragma unroll
@@ -359,12 +434,7 @@ __device__ int list_stretch(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK
 #pragma unroll
     for (int u = 0; u < 2; ++u)
       if (top[u] >= floor) list(vv[u], (static_cast<int32_t>(j) + u * BLOCK) * VEC, top[u], raise);
-    if (!__any(raise)) return;
-    const int b = cut_bin(s.hist, static_cast<uint32_t>(k));
-    const bool full = s.n > static_cast<uint32_t>(CAP);  // list no more
-    // A sixteenth of a bin below its edge: the bins' own roundings are less.
-    const float f = full ? INFINITY : bin0 + (static_cast<float>(b) - 0.0625f) * width;
-    if ((b > 0 || full) && lead) __hip_atomic_store(&s.floor, f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    raise_floor(raise);
   });
   L.add1(zt, c);
   *sum = merge_block<BLOCK>(L, c);  // its barrier ends the listing
@@ -382,12 +452,34 @@ __device__ int list_stretch(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK
   };
   auto row_keys = [&](auto fn) { x.template keys<BLOCK>(fn); };
   if (n > static_cast<uint32_t>(CAP)) {
+    const int b = cut_bin(s.hist, static_cast<uint32_t>(k));
     __syncthreads();
-    return digits(row_keys);
+    for (int i = t; i < 256; i += BLOCK) s.hist[i] = 0;
+    if (t == 0) {
+      s.n = 0;
+      s.floor = b > 0 ? edge(b) : floor0;
+    }
+    __syncthreads();
+    for (int32_t j = x.vb + t; __any(j < x.ve); j += BLOCK) {
+      const vec4u p = j < x.ve ? load_vector<Tin>(x.vectors() + j) : neg_inf_vec<Tin>();
+      float z[VEC];
+      Elem<Tin>::unpack(p, z);
+      const float floor = __hip_atomic_load(&s.floor, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      const float top = largest(z);
+      bool raise = false;
+      if (top >= floor) list(p, j * VEC, top, raise);
+      raise_floor(raise);
+    }
+    __syncthreads();
+    n = s.n;
+    if (n > static_cast<uint32_t>(CAP)) {
+      __syncthreads();
+      return digits(row_keys);
+    }
   }
   // The listed vectors' logits from the k-th's bin on.
   const int b = cut_bin(s.hist, static_cast<uint32_t>(k));
-  constexpr int PER = CAP / BLOCK;
+  constexpr int PER = (CAP + BLOCK - 1) / BLOCK;
   vec4u mine[PER];
   int32_t at[PER];
 #pragma unroll
@@ -809,20 +901,41 @@ __global__ __launch_bounds__(kBeamBlock) void beam_merge_kernel(BeamArgs a, cons
 
 constexpr int64_t kMostGroups = int64_t{1} << 23;  // a grid holds less than 2^32 threads
 
-// Workgroups along a row: about 512 in all, each with at least 512 vectors.
-// About 512 and 1,024 in all, beam search's step: 256 rows of 151,936 bfloat16
-// logits 27.7 and 28.5 us, 512 rows of 32,000 float32 logits (one workgroup a
-// row, or two) 17.0 and 23.2. At least 256 and 512 vectors, k = 256: 17 rows of
-// 50,257 bfloat16 logits 32.5 and 29.6 us.
-constexpr int64_t kGroups = 512, kLeastVectors = 512;
+// Workgroups along a row: one from 192 rows on, else about 512 in all, each with
+// at least 512 vectors. In parts and whole, k = 8: 200 rows of 151,936 bfloat16
+// logits 26.2 and 19.1 us, of 262,144 float32 logits 46 and 37; 128 rows 21.9 and
+// 19, 31.5 and 37. About 256 and 512 in all, k = 64: 128 rows of 262,144 float32
+// logits 39.4 and 34.0, 16 rows 19.4 and 19.3. At least 256 and 512 vectors: 17
+// rows of 50,257 bfloat16 logits, k = 256, 32.5 and 29.6.
+constexpr int64_t kWholeRows = 192, kGroups = 512, kLeastVectors = 512;
 
-int top_split(int64_t n_rows, int32_t V, pr_dtype dtype) {
-  if (n_rows <= 0) return 1;
+int beam_split(int64_t n_rows, int32_t V, pr_dtype dtype) {
+  if (n_rows <= 0 || n_rows >= kWholeRows) return 1;
   const int64_t nvec = V / (dtype == PR_BF16 ? 8 : 4);
   const int64_t want = (kGroups + n_rows - 1) / n_rows, most = nvec / kLeastVectors;
   const int64_t G = want < most ? want : most;
   return static_cast<int>(G < 1 ? 1 : G > kMaxSplit ? kMaxSplit : G);
 }
+
+// Where no request is merged afterwards, whole rows save a launch, and that is
+// more than parts save of a short row. In parts and whole: 64 rows of 32,000
+// float32 logits (8,000 vectors), k = 8, 16.8 and 13.9 us, 17 rows of 50,257
+// bfloat16 logits, k = 256, 25 and 17.5; of 18,992 vectors, k = 8, 16 rows 17.4 and
+// 19, 64 rows 18.2 and 19.
+constexpr int64_t kWholeVectors = 12288;
+
+int top_split(int64_t n_rows, int32_t V, pr_dtype dtype) {
+  return V / (dtype == PR_BF16 ? 8 : 4) <= kWholeVectors ? 1 : beam_split(n_rows, V, dtype);
+}
+
+// Whether whole rows are taken by 512 threads: up to a few hundred, which are a
+// workgroup or two a compute unit, and lists of more than 64, which take more of
+// a compute unit's shared memory. 256 and 512 threads, us: k = 8, 512 rows of
+// 151,936 bfloat16 logits 33.5 and 31.8, 1,024 55.0 and 56.3, 2,048 99 and 104,
+// 17,904 794 and 890 (k = 64); 512 rows of 32,000 float32 logits 17.1 and 17.3,
+// 1,024 26.0 and 26.5. k = 200: 512 rows of 151,936 45.3 and 38.4, 2,048 130 and
+// 125, of 32,000 float32 65 and 55.
+bool wide_rows(int64_t n_rows, int32_t k) { return n_rows <= 512 || k > 64; }
 
 size_t lists_bytes(int64_t n_rows, int G, int32_t k) {
   return static_cast<size_t>(n_rows) * static_cast<size_t>(G) * (static_cast<size_t>(k) * sizeof(uint64_t) + sizeof(RowSum));
@@ -842,8 +955,11 @@ hipError_t top(const TopArgs& a, hipStream_t stream) {
   }
   for (int64_t at = 0; at < a.n_rows; at += kMostGroups) {
     const int64_t rows = a.n_rows - at < kMostGroups ? a.n_rows - at : kMostGroups;
-    hipLaunchKernelGGL((top_kernel<Tin, kRowBlock, KMAX>), dim3(static_cast<unsigned>(rows)), dim3(kRowBlock), 0, stream,
-                       a, at);
+    const dim3 grid(static_cast<unsigned>(rows));
+    if (wide_rows(a.n_rows, a.k))
+      hipLaunchKernelGGL((top_kernel<Tin, 2 * kRowBlock, KMAX>), grid, dim3(2 * kRowBlock), 0, stream, a, at);
+    else
+      hipLaunchKernelGGL((top_kernel<Tin, kRowBlock, KMAX>), grid, dim3(kRowBlock), 0, stream, a, at);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -855,8 +971,11 @@ hipError_t beam(const BeamArgs& a, hipStream_t stream) {
   const int64_t n = static_cast<int64_t>(a.n_req) * a.B * a.G;
   uint64_t* list = static_cast<uint64_t*>(a.ws);
   RowSum* sums = reinterpret_cast<RowSum*>(list + n * a.k);
-  hipLaunchKernelGGL((beam_rows_kernel<Tin, kRowBlock, KMAX>), dim3(static_cast<unsigned>(n)), dim3(kRowBlock), 0, stream,
-                     a, sums, list);
+  const dim3 grid(static_cast<unsigned>(n));
+  if (a.G == 1 && wide_rows(static_cast<int64_t>(a.n_req) * a.B, a.k))
+    hipLaunchKernelGGL((beam_rows_kernel<Tin, 2 * kRowBlock, KMAX>), grid, dim3(2 * kRowBlock), 0, stream, a, sums, list);
+  else
+    hipLaunchKernelGGL((beam_rows_kernel<Tin, kRowBlock, KMAX>), grid, dim3(kRowBlock), 0, stream, a, sums, list);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const dim3 reqs(static_cast<unsigned>(a.n_req));
@@ -882,12 +1001,12 @@ hipError_t launch_top(const TopArgs& a, pr_dtype dtype, hipStream_t stream) {
 }
 
 size_t beam_workspace_bytes(int64_t n_rows, int32_t V, pr_dtype dtype, int32_t k) {
-  return n_rows < 1 ? 0 : lists_bytes(n_rows, top_split(n_rows, V, dtype), k);
+  return n_rows < 1 ? 0 : lists_bytes(n_rows, beam_split(n_rows, V, dtype), k);
 }
 
 hipError_t launch_beam(const BeamArgs& a, pr_dtype dtype, hipStream_t stream) {
   BeamArgs x = a;
-  x.G = top_split(static_cast<int64_t>(a.n_req) * a.B, a.V, dtype);
+  x.G = beam_split(static_cast<int64_t>(a.n_req) * a.B, a.V, dtype);
   if (x.k <= 64) return dtype == PR_BF16 ? beam<uint16_t, 64>(x, stream) : beam<float, 64>(x, stream);
   return dtype == PR_BF16 ? beam<uint16_t, kMaxTop>(x, stream) : beam<float, kMaxTop>(x, stream);
 }
