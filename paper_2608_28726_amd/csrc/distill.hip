@@ -57,12 +57,53 @@ struct EntrySums {
   double Q, cross;  // sum q, sum q (log q - u)
 };
 
-// A row's loss from its sums. part: of the tokens of the entries and of the others.
+// What a row comes to: `in` are the tokens of the entries, `out` the others.
 struct RowLoss {
   double loss, mass;
   uint32_t flags;
   RowDistill grad;
 };
+
+__device__ __forceinline__ uint32_t row_flags(const RowSum& in, const RowSum& out, uint32_t bad, float T) {
+  uint32_t flags = bad;
+  if (!temperature_ok(T)) flags |= PR_FLAG_BAD_TP;
+  const float m = fmaxf(in.m, out.m);
+  if (!(fabsf(in.S) < INFINITY) || !(fabsf(out.S) < INFINITY) || m == INFINITY || m == -INFINITY)
+    flags |= PR_FLAG_NONFINITE;
+  if (!flags && fabsf(m) > ldexpf(T, 100)) flags |= PR_FLAG_BAD_TP;
+  return flags;
+}
+
+// Whether the rest is a term, and its q.
+__device__ __forceinline__ double rest_q(const DistillArgs& a, const RowSum& out, double Q) {
+  return a.tail == PR_TAIL_REST && out.S > 0.0f ? fmax(0.0, 1.0 - Q) : 0.0;
+}
+
+// The gradient's factors. The sums are S 2^A of each part, so P and r_p come
+// from two exponentials and a division in float32, without a logarithm: the
+// waves that hold a row wait for this.
+__device__ __forceinline__ RowDistill row_factors(const DistillArgs& a, const RowSum& in, const RowSum& out, double Q,
+                                                  uint32_t flags, float T, float c, float w) {
+  const float nan = __uint_as_float(0x7fc00000u);
+  if (flags) return RowDistill{0.0f, nan, 0.0f, nan, 0.0f, nan, {0, 0}};
+  RowDistill g;
+  g.c = c;
+  g.A = out.S > 0.0f ? out.m * c : 0.0f;
+  g.in_A = in.S > 0.0f ? in.m * c : 0.0f;
+  const float A = fmaxf(in.S > 0.0f ? g.in_A : kNegSentinel, out.S > 0.0f ? g.A : kNegSentinel);
+  // Of each part: its scale beside the larger, and its sum so scaled.
+  const float si = in.S > 0.0f ? fast_exp2(fmaxf(g.in_A - A, -kBig)) : 0.0f;
+  const float so = out.S > 0.0f ? fast_exp2(fmaxf(g.A - A, -kBig)) : 0.0f;
+  const double pi = static_cast<double>(in.S * si), po = static_cast<double>(out.S * so), all = pi + po;
+  const double rq = rest_q(a, out, Q), scale = a.tail == PR_TAIL_RENORM ? (Q > 0.0 ? 1.0 / Q : 0.0) : 1.0;
+  const double q = a.tail == PR_TAIL_RENORM ? (Q > 0.0 ? 1.0 : 0.0) : Q;
+  const double coef = a.grad_scale * static_cast<double>(w) / static_cast<double>(T), each = coef / all;
+  g.k = out.S > 0.0f ? static_cast<float>(each * (q * po - rq * pi) / static_cast<double>(out.S)) : 0.0f;
+  g.in_k = static_cast<float>(each * (q + rq) * static_cast<double>(si));
+  g.q_k = static_cast<float>(coef * scale);
+  g.pad[0] = g.pad[1] = 0;
+  return g;
+}
 
 // log of a sum of exps, in 64 bits. S is relative to A = round(m c), whose
 // exact residual goes off its logarithm.
@@ -74,45 +115,27 @@ __device__ __forceinline__ double log_sum(const RowSum& p, float T, float c) {
          delta * 0.69314718055994530942;
 }
 
+// The loss and the student's probability of the entries' tokens.
+__device__ __forceinline__ void row_terms(const DistillArgs& a, const RowSum& in, const RowSum& out, const EntrySums& e,
+                                          float T, float c, RowLoss& x) {
+  if (x.flags) {
+    x.loss = x.mass = __longlong_as_double(0x7ff8000000000000ll);
+    return;
+  }
+  const double li = log_sum(in, T, c), lo = log_sum(out, T, c);
+  const double hi = fmax(li, lo), lse = hi + log1p(exp(fmin(li, lo) - hi)), rq = rest_q(a, out, e.Q);
+  x.mass = exp(li - lse);
+  x.loss = e.cross + e.Q * lse;
+  if (a.tail == PR_TAIL_RENORM) x.loss = e.Q > 0.0 ? x.loss / e.Q - log(e.Q) : 0.0;
+  if (rq > 0.0) x.loss += rq * (log(rq) - (lo - lse));
+}
+
 __device__ __forceinline__ RowLoss row_loss(const DistillArgs& a, const RowSum& in, const RowSum& out, const EntrySums& e,
                                             uint32_t bad, float T, float c, float w) {
   RowLoss x;
-  x.flags = bad;
-  if (!temperature_ok(T)) x.flags |= PR_FLAG_BAD_TP;
-  const float m = fmaxf(in.m, out.m);
-  if (!(fabsf(in.S) < INFINITY) || !(fabsf(out.S) < INFINITY) || m == INFINITY || m == -INFINITY)
-    x.flags |= PR_FLAG_NONFINITE;
-  if (!x.flags && fabsf(m) > ldexpf(T, 100)) x.flags |= PR_FLAG_BAD_TP;
-  if (x.flags) {
-    const float nan = __uint_as_float(0x7fc00000u);
-    x.loss = x.mass = __longlong_as_double(0x7ff8000000000000ll);
-    x.grad = RowDistill{0.0f, nan, 0.0f, nan, 0.0f, nan, {0, 0}};
-    return x;
-  }
-  const double li = log_sum(in, T, c), lo = log_sum(out, T, c);
-  const double hi = fmax(li, lo), lse = hi + log1p(exp(fmin(li, lo) - hi));
-  const double P = exp(li - lse), rp = exp(lo - lse);
-  const bool norm = a.tail == PR_TAIL_RENORM;
-  double Q = e.Q, rq = 0.0, scale = 1.0;
-  x.loss = e.cross + Q * lse;
-  if (norm) {
-    scale = Q > 0.0 ? 1.0 / Q : 0.0;
-    x.loss = Q > 0.0 ? x.loss / Q - log(Q) : 0.0;
-    Q = Q > 0.0 ? 1.0 : 0.0;
-  } else if (a.tail == PR_TAIL_REST && out.S > 0.0f) {
-    rq = fmax(0.0, 1.0 - Q);
-    if (rq > 0.0) x.loss += rq * (log(rq) - (lo - lse));
-  }
-  x.mass = P;
-  const double coef = a.grad_scale * static_cast<double>(w) / static_cast<double>(T);
-  RowDistill& g = x.grad;
-  g.c = c;
-  g.A = out.S > 0.0f ? out.m * c : 0.0f;
-  g.k = out.S > 0.0f ? static_cast<float>(coef * (Q * rp - rq * P) / static_cast<double>(out.S)) : 0.0f;
-  g.in_A = in.S > 0.0f ? in.m * c : 0.0f;
-  g.in_k = in.S > 0.0f ? static_cast<float>(coef * (Q + rq) * P / static_cast<double>(in.S)) : 0.0f;
-  g.q_k = static_cast<float>(coef * scale);
-  g.pad[0] = g.pad[1] = 0;
+  x.flags = row_flags(in, out, bad, T);
+  x.grad = row_factors(a, in, out, e.Q, x.flags, T, c, w);
+  row_terms(a, in, out, e, T, c, x);
   return x;
 }
 
@@ -674,14 +697,17 @@ __global__ __launch_bounds__((DW + 1) * kWave) void distill_row_kernel(DistillAr
       RowSum part{-INFINITY, 0.0f};
       if (lane < DW) part = sh_sum[lane];
       if (lane == DW) part = own;
-      const RowLoss loss = row_loss(a, sum_in, merge_lanes(part, c), sums, bad, T, c, w);
-      const RowDistill q = loss.grad;
+      const RowSum sum_out = merge_lanes(part, c);
+      RowLoss loss;
+      loss.flags = row_flags(sum_in, sum_out, bad, T);
+      const RowDistill q = row_factors(a, sum_in, sum_out, sums.Q, loss.flags, T, c, w);
       if (lane == 0) {
         sh_A = q.A;
         sh_c = q.c;
         sh_k = q.k;
       }
       __syncthreads();
+      row_terms(a, sum_in, sum_out, sums, T, c, loss);
       if (lane == 0) {
         write_row(a, r, loss);
         term[r] = static_cast<double>(w) * loss.loss;
