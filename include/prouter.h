@@ -413,7 +413,9 @@ pr_status pr_stream_create(int32_t max_slots, int32_t max_len, const pr_agg_para
  * pr_token_features), and for each row r the slot slot_ids[r] (device
  * int32 [n_active]) gains one token: count, running sums and minima of A,
  * and the token's A is appended to the slot's history (needed for the exact
- * quantile). A slot may appear at most once per step (duplicates race).
+ * quantile). A slot may appear at most once per step (duplicates race); a slot id
+ * outside [0, max_slots) leaves the states alone (the row's features are
+ * computed all the same).
  * Tokens past max_len are counted in sums and minima but not kept, and the
  * slot's quantile becomes NaN. In bounded-memory mode (max_len == 0) the
  * token instead updates the slot's P-square markers. out may be NULL (features not returned).
@@ -463,7 +465,8 @@ pr_status pr_stream_reset_slots(pr_stream* state, const int32_t* slots, int32_t 
  * call (pr_beam_reorder for a state's slots). slots, parent: device int32
  * [n_req][n_beams]; no slot twice. An entry whose parent lies outside
  * [0, n_beams), or whose slot or parent's slot is not one of the state's, leaves
- * its slot as it is. 1 <= n_beams <= PR_MAX_BEAMS. Ordered like steps on the same slots.
+ * its slot as it is. 1 <= n_beams <= PR_MAX_BEAMS. Ordered like steps on the same
+ * slots; the state's device must be the current one (PR_ERR_INVALID_ARG).
  */
 pr_status pr_stream_reorder(pr_stream* state, const int32_t* slots, const int32_t* parent, int32_t n_req,
                             int32_t n_beams, void* stream);
@@ -559,8 +562,9 @@ typedef struct pr_beam_state {
  *   states    host array of n_states (read during the call), device memory.
  *             No two may overlap (PR_ERR_INVALID_ARG; rows of two states may
  *             lie side by side in one stride). 0 <= row_bytes <= row_stride.
- *   parent    int32 [n_req][n_beams], device, with any repetition. An entry
- *             outside [0, n_beams) leaves its row as it is.
+ *   parent    int32 [n_req][n_beams], device, with any repetition, in memory
+ *             apart from the states' (PR_ERR_INVALID_ARG). An entry outside
+ *             [0, n_beams) leaves its row as it is.
  * Nothing is allocated; only rows that change are written. One launch per 96
  * states. 1 <= n_beams <= PR_MAX_BEAMS, n_req * n_beams < 2^31.
  */

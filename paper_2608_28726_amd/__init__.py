@@ -606,7 +606,8 @@ def beam_reorder(states, parent: torch.Tensor) -> None:
     ``parent[i, b]`` was. ``parent`` int32 [n_req, n_beams] (as
     :func:`beam_select` returns it with k = n_beams); an entry outside
     [0, n_beams) leaves its beam as it is. A beam's part of a tensor must be
-    contiguous; beams may lie apart. No two tensors may overlap.
+    contiguous; beams may lie apart. No two tensors, ``parent`` among them, may
+    overlap.
     """
     states = [states] if isinstance(states, torch.Tensor) else list(states)
     device = parent.device

@@ -579,6 +579,9 @@ pr_status pr_stream_reorder(pr_stream* state, const int32_t* slots, const int32_
   if (st != PR_OK) return st;
   if (n_req == 0) return PR_OK;
   if (!slots || !parent) return PR_ERR_INVALID_ARG;
+  int device = 0;
+  if (hipGetDevice(&device) != hipSuccess) return PR_ERR_HIP;
+  if (device != state->device) return PR_ERR_INVALID_ARG;
   const StreamDev& d = state->dev;
   StateList list{};
   auto add = [&](void* p, int64_t bytes) {
@@ -685,6 +688,12 @@ pr_status pr_beam_reorder(const pr_beam_state* states, int32_t n_states, const i
   }
   if (n_req == 0 || n_states == 0) return PR_OK;
   if (!parent) return PR_ERR_INVALID_ARG;
+  const uintptr_t p0 = reinterpret_cast<uintptr_t>(parent), p1 = p0 + static_cast<uintptr_t>(n) * sizeof(int32_t);
+  for (int32_t j = 0; j < n_states; ++j) {
+    const uintptr_t s0 = reinterpret_cast<uintptr_t>(states[j].rows);
+    const uintptr_t s1 = s0 + static_cast<uintptr_t>((n - 1) * states[j].row_stride + states[j].row_bytes);
+    if (states[j].row_bytes > 0 && s0 < p1 && p0 < s1) return PR_ERR_INVALID_ARG;
+  }
   try {
     // By their first byte: a state can share bytes only with those that start before its end.
     std::vector<pr_beam_state> by(states, states + n_states);

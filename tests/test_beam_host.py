@@ -73,7 +73,7 @@ def test_too_many(L):
     assert distill(L, n=(1 << 26) + 1) == a.PR_ERR_UNSUPPORTED
 
 
-def reorder(L, states, n=3, B=2, parent=P, count=None):
+def reorder(L, states, n=3, B=2, parent=C.c_void_p(1 << 20), count=None):
     a = _abi()
     S = (a.BeamState * max(1, len(states)))(*[a.BeamState(p, b, s) for p, b, s in states])
     return L.pr_beam_reorder(S if states or count is None else None, len(states) if count is None else count, parent, n, B, None)
@@ -87,6 +87,7 @@ def reorder(L, states, n=3, B=2, parent=P, count=None):
     [(4096, 8, 32), (4096 + 4, 8, 32)],      # side by side, but over each other
     [(4096, 8, 32), (4096 + 28, 8, 32)],     # the second's row ends in the first's next
     [(4096, 8, 32), (4096 + 8, 8, 24)],      # other strides
+    [((1 << 20) - 40, 8, 8)],                # the parents are among the rows
 ])
 def test_reorder_refusals(L, states):
     assert reorder(L, states) == _abi().PR_ERR_INVALID_ARG
