@@ -161,8 +161,8 @@ __device__ __forceinline__ Entry load_entry(const DistillArgs& a, int64_t r, int
   Entry e{-1, -INFINITY, 0};
   if (i >= a.k) return e;
   const float lq = a.top_logprob[r * a.top_stride + i];
+  const int32_t id = a.top_ids[r * a.top_stride + i];  // at once with it
   if (lq == -INFINITY) return e;
-  const int32_t id = a.top_ids[r * a.top_stride + i];
   if (!(lq < INFINITY)) e.bad |= PR_FLAG_NONFINITE;
   if (id < 0 || id >= a.rows.V) e.bad |= PR_FLAG_BAD_ID;
   if (!e.bad) {
@@ -314,7 +314,7 @@ __device__ DistillPart row_part(const DistillArgs& a, int64_t r, int g, int G, f
   // (An id that is there twice leaves gaps, in a row that is NaN.)
   if (sorted) {
     for (int32_t i = t; i <= sorted->parts; i += kStatsBlock) {
-      const int32_t from = h + i * kGradBlock * VEC;
+      const int64_t from = h + static_cast<int64_t>(i) * (kGradBlock * VEC);
       int lo = 0, len = i == 0 ? 0 : n;
       if (i == sorted->parts) lo = n, len = 0;
       while (len > 0) {  // the first entry not below `from`
@@ -575,8 +575,16 @@ __device__ __forceinline__ uint32_t group_slot(const Group& g, int32_t nvec) {
 // that hold their tokens, made a row ahead, tells the others which vectors to
 // leave to it, in the sum and in the gradient. There are three bit maps in turn:
 // the one made while a row is summed was last read two rows before.
+// Reads 2 and writes 2 bytes a bfloat16 logit, of which it reaches 5.0 TB/s:
+// 16,972 rows of 151,936 logits with 64 entries, 15,279 of them counting, 1,950
+// to 1,980 us; 512 rows of 32,000 float32 logits with 20 entries 24.7. With up to 64 entries
+// the extra wave keeps pace with the others; with 65 to 256 a lane has up to 4
+// and the row waits for them (4,096 rows of 151,936: 64 entries 534 us, 65 581,
+// 256 706). Two of the smaller workgroups then share a compute unit only where
+// the launch bound asks for it: 512 rows of 50,257 bfloat16 logits with 256
+// entries 34.6 us, without it 41.6.
 template <typename Tin, int DW, int NR, int KE>
-__global__ __launch_bounds__((DW + 1) * kWave) void distill_row_kernel(DistillArgs a, double* term) {
+__global__ __launch_bounds__((DW + 1) * kWave, 4) void distill_row_kernel(DistillArgs a, double* term) {
   constexpr int VEC = Elem<Tin>::kVec, NT = DW * kWave, MOST = NR * NT;  // vectors
   __shared__ RowSum sh_sum[DW];
   __shared__ float sh_A, sh_c, sh_k;
@@ -827,9 +835,38 @@ hipError_t launch_held(const DistillArgs& a, int64_t most, double* term, hipStre
 // 262,144 float32 logits: 205 us, without it 224.
 constexpr unsigned kUnusedLds = 20000;
 
-// Workgroups per row for a shape (0: rows are not split): as for the policy loss.
-int distill_split(int64_t n_rows, int32_t V, pr_dtype dtype, bool grad) {
-  return policy_split(n_rows, V, dtype, grad);
+// Whether rows are held in a workgroup's registers. Shorter ones than for the
+// policy loss are, as the pass that sums rows and puts their entries in order
+// costs more here. 600 MB of rows, held and in two passes, with 20, 64 and 256
+// entries (us, in brackets a row's vectors): bfloat16 4,096 logits a row (512)
+// 1,098 and 999, 1,120 and 1,538, 2,437 and 4,540; 8,192 (1,024) 683 and 614,
+// 713 and 871, 1,430 and 2,334; 12,000 (1,500) 510 and 516, 542 and 682, 1,062
+// and 1,657; 16,384 (2,048) 397 and 435, 427 and 552, 829 and 1,256; 32,000 270
+// and 370, 289 and 431, 508 and 764; float32 4,096 619 and 585, 648 and 836,
+// 1,081 and 2,240; 16,000 255 and 354, 267 and 425, 405 and 758. 2,048 rows of
+// 4,096 bfloat16 logits: 35 and 41, 34 and 58, 67 and 149.
+constexpr int64_t kLeastHeld = 512, kLeastHeldFewEntries = 1500, kFewEntries = 32, kManyRows = 8192;
+bool held(int64_t n_rows, int64_t nvec, int32_t k) {
+  const bool short_rows = nvec < kLeastHeldFewEntries && k <= kFewEntries && n_rows >= kManyRows;
+  return nvec >= kLeastHeld && nvec <= kRowVectors && !short_rows;
+}
+
+// Workgroups per row for a shape (0: rows are not split). Few rows that could be
+// held are spread over the device as long as that is faster. Spread and held, 20
+// and 256 entries (us): 16,384 bfloat16 logits (2,048 vectors) 48 rows 11.0 and
+// 11.2, 12.5 and 17.1, 128 rows 14.8 and 11.7, 16.7 and 17.6; 50,257 of them
+// (6,282) 8 rows 12.9 and 14.2, 13.7 and 19.0, 32 rows 15.0 and 14.7, 15.7 and
+// 19.4; 32,000 float32 logits (8,000) 4 rows 12.6 and 12.6, 13.6 and 15.9, 32
+// rows 16.2 and 13.2, 17.2 and 16.6; the larger size: 40,000 float32 logits
+// (10,000) 24 rows 14.6 and 14.7, 15.3 and 18.4, 32 rows 17.7 and 14.9, 18.6 and
+// 18.5; 151,936 bfloat16 logits (18,992) 48 rows 24.7 and 26.5, 26.8 and 31.2,
+// 64 rows 29.3 and 27.4, 31.2 and 32.3.
+int distill_split(int64_t n_rows, int32_t V, pr_dtype dtype, bool grad, int32_t k) {
+  if (n_rows <= 0 || n_rows >= kSplitRows) return 0;
+  const int64_t nvec = V / (dtype == PR_BF16 ? 8 : 4);
+  const bool few = nvec <= kSmallRowVectors ? n_rows * nvec <= (k <= kWave ? 100000 : 250000)
+                                            : n_rows <= nvec / 400;
+  return grad && held(n_rows, nvec, k) && !few ? 0 : row_parts(n_rows, V, dtype);
 }
 
 constexpr int64_t kMostGroups = int64_t{1} << 23;  // a grid holds less than 2^32 threads
@@ -849,7 +886,7 @@ hipError_t distill(const DistillArgs& a, hipStream_t stream) {
   RowDistill* rd = static_cast<RowDistill*>(a.ws);
   double* term = reinterpret_cast<double*>(rd + n);
   const int64_t nvec = a.rows.V / Elem<Tin>::kVec, parts = grad_parts<Tin>(a.rows.V);
-  const int G = distill_split(n, a.rows.V, dtype, a.rows.grad != nullptr);
+  const int G = distill_split(n, a.rows.V, dtype, a.rows.grad != nullptr, a.k);
   hipError_t e = hipSuccess;
   if (G > 0) {
     DistillPart* part = reinterpret_cast<DistillPart*>(rd + n);
@@ -870,7 +907,7 @@ hipError_t distill(const DistillArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL(distill_grad_kernel<Tin>, grid, dim3(kGradBlock), 0, stream, a, rd);
     return hipGetLastError();
   }
-  if (n > 0 && a.rows.grad && held_row(nvec)) {
+  if (n > 0 && a.rows.grad && held(n, nvec, a.k)) {
     e = nvec <= kSmallRowVectors ? launch_held<Tin, 7, 19>(a, 2 * kCUs, term, stream)
                                  : launch_held<Tin, 15, 20>(a, kCUs, term, stream);
   } else {
@@ -901,11 +938,12 @@ hipError_t distill(const DistillArgs& a, hipStream_t stream) {
 
 size_t distill_workspace_bytes(int64_t n_rows, int32_t V, pr_dtype dtype, int32_t k) {
   const size_t n = n_rows < 0 ? 0 : static_cast<size_t>(n_rows), entries = k < 0 ? 0 : static_cast<size_t>(k);
-  const size_t most = static_cast<size_t>(std::max(distill_split(n_rows, V, dtype, true),
-                                                   distill_split(n_rows, V, dtype, false)));
+  const size_t most = static_cast<size_t>(std::max(distill_split(n_rows, V, dtype, true, k),
+                                                   distill_split(n_rows, V, dtype, false, k)));
   const size_t parts = static_cast<size_t>(dtype == PR_BF16 ? grad_parts<uint16_t>(V) : grad_parts<float>(V));
   size_t rows = n * sizeof(double);
-  if (!held_row(V / (dtype == PR_BF16 ? 8 : 4))) rows += n * (entries * sizeof(SortedEntry) + (parts + 1) * sizeof(int32_t));
+  if (!held(n_rows, V / (dtype == PR_BF16 ? 8 : 4), k))
+    rows += n * (entries * sizeof(SortedEntry) + (parts + 1) * sizeof(int32_t));
   return n * sizeof(RowDistill) + std::max(n * most * sizeof(DistillPart), rows);
 }
 

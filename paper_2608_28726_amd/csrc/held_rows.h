@@ -61,6 +61,13 @@ struct RowView {
 constexpr int64_t kLeastRowVectors = 3500, kSmallRowVectors = 19 * 7 * kWave, kRowVectors = 20 * 15 * kWave;
 inline bool held_row(int64_t nvec) { return nvec >= kLeastRowVectors && nvec <= kRowVectors; }
 
+// Below this many rows a row may be spread over workgroups. Spread and whole,
+// preference loss: 64 rows of 50,257 bfloat16 logits 14.4 and 17.1 us, of
+// 151,936 float32 logits 30.5 and 41.0; 128 rows 17.5 and 19.6, 47.2 and 53.7;
+// 200 rows 23.1 and 22.3, 66.8 and 68.5; 256 rows 25.1 and 24.7, 83.1 and 80.5;
+// 400 rows 32.7 and 31.2, 126 and 124.
+constexpr int64_t kSplitRows = 256;
+
 // Few rows whose gradient is wanted are spread over the device although they
 // fit a workgroup: one compute unit alone takes 20 us for 304 KB. Captured
 // calls, spread and held: 16 rows of 151,936 bfloat16 logits 11.7 and 21.6 us,

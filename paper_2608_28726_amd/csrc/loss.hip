@@ -596,13 +596,6 @@ __global__ __launch_bounds__(kPairBlock) void preference_pair_kernel(PreferenceA
   }
 }
 
-// Below this many rows a row may be spread over workgroups. Spread and whole,
-// preference loss: 64 rows of 50,257 bfloat16 logits 14.4 and 17.1 us, of
-// 151,936 float32 logits 30.5 and 41.0; 128 rows 17.5 and 19.6, 47.2 and 53.7;
-// 200 rows 23.1 and 22.3, 66.8 and 68.5; 256 rows 25.1 and 24.7, 83.1 and 80.5;
-// 400 rows 32.7 and 31.2, 126 and 124.
-constexpr int64_t kSplitRows = 256;
-
 // Workgroups of the launch that starts at `at` of `total`.
 unsigned groups_from(int64_t at, int64_t total) {
   return static_cast<unsigned>(total - at < kMostGroups ? total - at : kMostGroups);

@@ -91,6 +91,15 @@ SHAPES = [
     (70, 20000, 31, torch.float32, 0, 0),
     (300, 40000, 48, torch.bfloat16, 0, 3),
 ]
+# On either side of where rows are held by a workgroup or spread over several.
+SHAPES += [(n, V, k, dtype, 0, start)
+           for n, k, start in ((300, 33, 0), (300, 256, 1))
+           for V, dtype in ((4095, torch.bfloat16), (4096, torch.bfloat16), (2051, torch.float32))] + [
+    (8200, 4096, 32, torch.bfloat16, 0, 1), (8200, 2051, 33, torch.float32, 0, 0),
+    (12, 32000, 64, torch.float32, 0, 0), (13, 32000, 64, torch.float32, 0, 3), (31, 32000, 65, torch.float32, 0, 1),
+    (32, 32000, 65, torch.float32, 0, 0), (25, 40003, 20, torch.float32, 0, 0), (26, 40003, 20, torch.float32, 0, 1),
+    (255, 4100, 20, torch.bfloat16, 0, 1), (255, 4090, 256, torch.bfloat16, 0, 1),
+]
 
 
 @pytest.mark.parametrize("tail", ["rest", "drop", "renorm"])
