@@ -33,18 +33,23 @@ constexpr int kWindow = 1 << 16;  // vectors of a bit map
 static_assert(kStatsBlock >= kMaxTop && kGradBlock >= kMaxTop, "a thread for each entry");
 
 // What the gradient pass needs of a row: dz_v = k 2^fma(z_v, c, -A) outside the
-// entries, in_k 2^fma(z_v, c, -in_A) - q_k q_i in them. All factors 0: the
+// entries, in_k 2^fma(z_v, c, -in_A) - q_k q_i in them, the products in 64 bits:
+// where student and teacher agree little is left of the two. All factors 0: the
 // gradient is zero and the row is not read.
 struct alignas(16) RowDistill {
-  float A, k, in_A, in_k, c, q_k;
-  uint32_t pad[2];
+  float A, k, in_A, c;
+  double in_k, q_k;
+
+  __device__ __forceinline__ float in_entry(float z, double q) const {
+    return static_cast<float>(in_k * static_cast<double>(fast_exp2(fmaf(z, c, -in_A))) - q_k * q);
+  }
 };
 
 // A row's entries by token for the gradient pass: those of its workgroup p along
 // the row are begin[p] .. begin[p + 1] - 1.
 struct SortedEntry {
   int32_t id;
-  float q;
+  double q;
 };
 struct SortedRows {
   SortedEntry* entry;  // [n_rows][k]
@@ -85,7 +90,7 @@ __device__ __forceinline__ double rest_q(const DistillArgs& a, const RowSum& out
 __device__ __forceinline__ RowDistill row_factors(const DistillArgs& a, const RowSum& in, const RowSum& out, double Q,
                                                   uint32_t flags, float T, float c, float w) {
   const float nan = __uint_as_float(0x7fc00000u);
-  if (flags) return RowDistill{0.0f, nan, 0.0f, nan, 0.0f, nan, {0, 0}};
+  if (flags) return RowDistill{0.0f, nan, 0.0f, 0.0f, nan, nan};
   RowDistill g;
   g.c = c;
   g.A = out.S > 0.0f ? out.m * c : 0.0f;
@@ -94,14 +99,14 @@ __device__ __forceinline__ RowDistill row_factors(const DistillArgs& a, const Ro
   // Of each part: its scale beside the larger, and its sum so scaled.
   const float si = in.S > 0.0f ? fast_exp2(fmaxf(g.in_A - A, -kBig)) : 0.0f;
   const float so = out.S > 0.0f ? fast_exp2(fmaxf(g.A - A, -kBig)) : 0.0f;
-  const double pi = static_cast<double>(in.S * si), po = static_cast<double>(out.S * so), all = pi + po;
+  const double pi = static_cast<double>(in.S) * static_cast<double>(si);
+  const double po = static_cast<double>(out.S) * static_cast<double>(so), all = pi + po;
   const double rq = rest_q(a, out, Q), scale = a.tail == PR_TAIL_RENORM ? (Q > 0.0 ? 1.0 / Q : 0.0) : 1.0;
   const double q = a.tail == PR_TAIL_RENORM ? (Q > 0.0 ? 1.0 : 0.0) : Q;
   const double coef = a.grad_scale * static_cast<double>(w) / static_cast<double>(T), each = coef / all;
   g.k = out.S > 0.0f ? static_cast<float>(each * (q * po - rq * pi) / static_cast<double>(out.S)) : 0.0f;
-  g.in_k = static_cast<float>(each * (q + rq) * static_cast<double>(si));
-  g.q_k = static_cast<float>(coef * scale);
-  g.pad[0] = g.pad[1] = 0;
+  g.in_k = each * (q + rq) * static_cast<double>(si);
+  g.q_k = coef * scale;
   return g;
 }
 
@@ -140,7 +145,7 @@ __device__ __forceinline__ RowLoss row_loss(const DistillArgs& a, const RowSum& 
 }
 
 __device__ __forceinline__ RowLoss masked_row() {
-  return RowLoss{0.0, 0.0, PR_FLAG_MASKED, RowDistill{0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, {0, 0}}};
+  return RowLoss{0.0, 0.0, PR_FLAG_MASKED, RowDistill{0.0f, 0.0f, 0.0f, 0.0f, 0.0, 0.0}};
 }
 
 __device__ __forceinline__ void write_row(const DistillArgs& a, int64_t r, const RowLoss& x) {
@@ -296,7 +301,7 @@ __device__ DistillPart row_part(const DistillArgs& a, int64_t r, int g, int G, f
         rank += (o.x < id ? 1 : 0) + (o.y < id ? 1 : 0) + (o.z < id ? 1 : 0) + (o.w < id ? 1 : 0);
       }
       if (sorted) {
-        sorted->entry[r * a.k + rank] = SortedEntry{e.id, expf(e.logq)};
+        sorted->entry[r * a.k + rank] = SortedEntry{e.id, exp(static_cast<double>(e.logq))};
         by_id[rank] = e.id;
       }
       if (same > 1) atomicOr(&sh_bad, PR_FLAG_BAD_ID);
@@ -338,7 +343,7 @@ __device__ DistillPart row_part(const DistillArgs& a, int64_t r, int g, int G, f
 }
 
 // One workgroup per row: its sums and everything but its gradient. The read
-// bounds it where rows are long: 1,028 counting of 2,048 rows of 262,144 float32
+// bounds it where rows are long: 1,045 counting of 2,048 rows of 262,144 float32
 // logits with 128 entries 207 us (5.3 TB/s); where they are short, their entries.
 template <typename Tin>
 __global__ __launch_bounds__(kStatsBlock) void distill_stats_kernel(DistillArgs a, double* term, RowDistill* rd,
@@ -442,7 +447,7 @@ template <typename Tin>
 __device__ __forceinline__ void grad_stretch(const DistillArgs& a, int64_t r, int part, const RowDistill& q) {
   constexpr int VEC = Elem<Tin>::kVec;
   __shared__ uint32_t elements[(kGradBlock + 2 * 8) / 4];  // a byte a vector: its entries' elements; then the row's ends
-  __shared__ float value[(kGradBlock + 2) * VEC];           // of those elements: q_k q
+  __shared__ double value[(kGradBlock + 2) * VEC];          // of those elements: q
   const int t = threadIdx.x;
   const int32_t V = a.rows.V;
   const Tin* row = row_ptr<Tin>(a.rows, r);
@@ -451,7 +456,7 @@ __device__ __forceinline__ void grad_stretch(const DistillArgs& a, int64_t r, in
   const int32_t j = part * kGradBlock + t;
   const bool ends = part == 0 && t < 16;
   const int32_t s = ends ? scalar_element(t, h, tail, V) : V;
-  if (q.k == 0.0f && q.in_k == 0.0f && q.q_k == 0.0f) {
+  if (q.k == 0.0f && q.in_k == 0.0 && q.q_k == 0.0) {
     if (s < V) GradVec<Tin>::store1(out, s, 0.0f);
     if (j < nvec) stream_grad(out + h + static_cast<int64_t>(j) * VEC, vec4u{0, 0, 0, 0});
     return;
@@ -467,7 +472,7 @@ __device__ __forceinline__ void grad_stretch(const DistillArgs& a, int64_t r, in
     if (g.vec < 0 ? part == 0 : g.vec / kGradBlock == part) {
       const int slot = g.vec < 0 ? kGradBlock - 1 - g.vec : g.vec % kGradBlock, i = e.id - g.base;
       atomicOr(&elements[slot / 4], 1u << (slot % 4 * 8 + i));
-      value[slot * VEC + i] = q.q_k * expf(e.logq);
+      value[slot * VEC + i] = exp(static_cast<double>(e.logq));
     }
   }
   __syncthreads();
@@ -475,7 +480,7 @@ __device__ __forceinline__ void grad_stretch(const DistillArgs& a, int64_t r, in
   if (s < V) {
     const int slot = kGradBlock + t / 8, i = t % 8;
     GradVec<Tin>::store1(out, s, byte[slot] >> i & 1u
-                                     ? q.in_k * fast_exp2(fmaf(zs, q.c, -q.in_A)) - value[slot * VEC + i]
+                                     ? q.in_entry(zs, value[slot * VEC + i])
                                      : q.k * fast_exp2(fmaf(zs, q.c, -q.A)));
   }
   if (j >= nvec) return;
@@ -487,7 +492,7 @@ __device__ __forceinline__ void grad_stretch(const DistillArgs& a, int64_t r, in
   if (mine != 0) {
 #pragma unroll
     for (int i = 0; i < VEC; ++i)
-      if (mine >> i & 1u) g[i] = q.in_k * fast_exp2(fmaf(z[i], q.c, -q.in_A)) - value[t * VEC + i];
+      if (mine >> i & 1u) g[i] = q.in_entry(z[i], value[t * VEC + i]);
   }
   stream_grad(out + h + static_cast<int64_t>(j) * VEC, GradVec<Tin>::pack(g));
 }
@@ -511,7 +516,7 @@ __global__ __launch_bounds__(kGradBlock) void distill_sorted_grad_kernel(Distill
   int32_t s = V;
   if (t < 8 && part == 0 && t < h) s = t;
   if (t >= 8 && t < 16 && part == sorted.parts - 1 && t - 8 < V - tail) s = tail + t - 8;
-  if (q.k == 0.0f && q.in_k == 0.0f && q.q_k == 0.0f) {
+  if (q.k == 0.0f && q.in_k == 0.0 && q.q_k == 0.0) {
     if (s < V) GradVec<Tin>::store1(out, s, 0.0f);
     if (j < nvec) stream_grad(out + h + static_cast<int64_t>(j) * VEC, vec4u{0, 0, 0, 0});
     return;
@@ -523,7 +528,7 @@ __global__ __launch_bounds__(kGradBlock) void distill_sorted_grad_kernel(Distill
     const float z = Elem<Tin>::load1(row, s);
     float g = q.k * fast_exp2(fmaf(z, q.c, -q.A));
     for (int32_t i = from; i < to; ++i)
-      if (entry[i].id == s) g = q.in_k * fast_exp2(fmaf(z, q.c, -q.in_A)) - q.q_k * entry[i].q;
+      if (entry[i].id == s) g = q.in_entry(z, entry[i].q);
     GradVec<Tin>::store1(out, s, g);
   }
   if (j >= nvec) return;
@@ -535,9 +540,12 @@ __global__ __launch_bounds__(kGradBlock) void distill_sorted_grad_kernel(Distill
   for (int32_t i = from; i < to; ++i) {
     const int32_t d = entry[i].id - base;
     if (d < 0 || d >= VEC) continue;
+    float zd = z[0];
 #pragma unroll
-    for (int u = 0; u < VEC; ++u)
-      if (u == d) g[u] = q.in_k * fast_exp2(fmaf(z[u], q.c, -q.in_A)) - q.q_k * entry[i].q;
+    for (int u = 1; u < VEC; ++u) zd = u == d ? z[u] : zd;
+    const float gd = q.in_entry(zd, entry[i].q);
+#pragma unroll
+    for (int u = 0; u < VEC; ++u) g[u] = u == d ? gd : g[u];
   }
   stream_grad(out + h + static_cast<int64_t>(j) * VEC, GradVec<Tin>::pack(g));
 }
@@ -580,7 +588,7 @@ __device__ __forceinline__ uint32_t group_slot(const Group& g, int32_t nvec) {
 // leave to it, in the sum and in the gradient. There are three bit maps in turn:
 // the one made while a row is summed was last read two rows before.
 // Reads 2 and writes 2 bytes a bfloat16 logit, of which it reaches 5.0 TB/s:
-// 16,972 rows of 151,936 logits with 64 entries, 15,279 of them counting, 1,950
+// 16,972 rows of 151,936 logits with 64 entries, 15,193 of them counting, 1,950
 // to 1,980 us; 512 rows of 32,000 float32 logits with 20 entries 24.7. With up to 64 entries
 // the extra wave keeps pace with the others; with 65 to 256 a lane has up to 4
 // and the row waits for them (4,096 rows of 151,936: 64 entries 534 us, 65 581,
@@ -686,6 +694,7 @@ __global__ __launch_bounds__((DW + 1) * kWave, 4) void distill_row_kernel(Distil
       LaneSum<false> in, out;
       out.add1(scalar ? zs : -INFINITY, c);
       EntrySums sums{0.0, 0.0};
+      double q_of[KE];
 #pragma unroll
       for (int i = 0; i < KE; ++i) {
         in.add1(z[i], c);
@@ -695,10 +704,10 @@ __global__ __launch_bounds__((DW + 1) * kWave, 4) void distill_row_kernel(Distil
         for (int u = 0; u < VEC; ++u) other[u] = e.mine[i] >> u & 1u ? -INFINITY : other[u];
         out.add(other, c);
         // A probability of 0 adds nothing, whatever the student makes of its token.
-        const double q = e.id[i] >= 0 ? exp(static_cast<double>(e.logq[i])) : 0.0;
-        sums.Q += q;
-        if (q > 0.0)
-          sums.cross += q * (static_cast<double>(e.logq[i]) - static_cast<double>(z[i]) / static_cast<double>(T));
+        q_of[i] = e.id[i] >= 0 ? exp(static_cast<double>(e.logq[i])) : 0.0;
+        sums.Q += q_of[i];
+        if (q_of[i] > 0.0)
+          sums.cross += q_of[i] * (static_cast<double>(e.logq[i]) - static_cast<double>(z[i]) / static_cast<double>(T));
       }
       sums.Q = wave_sum_d(sums.Q);
       sums.cross = wave_sum_d(sums.cross);
@@ -728,8 +737,7 @@ __global__ __launch_bounds__((DW + 1) * kWave, 4) void distill_row_kernel(Distil
 #pragma unroll
       for (int i = 0; i < KE; ++i) {
         if (e.id[i] < 0) continue;
-        GradVec<Tin>::store1(x.out, e.id[i],
-                             q.in_k * fast_exp2(fmaf(z[i], q.c, -q.in_A)) - q.q_k * expf(e.logq[i]));
+        GradVec<Tin>::store1(x.out, e.id[i], q.in_entry(z[i], q_of[i]));
         float other[VEC];
         Elem<Tin>::unpack(v[i], other);
         const int32_t base = group_of<Tin>(e.id[i], h, tail, V).base;
@@ -835,7 +843,7 @@ hipError_t launch_held(const DistillArgs& a, int64_t most, double* term, hipStre
 
 // Shared memory that distill_stats_kernel asks for and does not use, so that no
 // more than 5 of its workgroups share a compute unit: where many rows do not
-// count, those that do are dealt out more evenly. 1,028 counting of 2,048 rows of
+// count, those that do are dealt out more evenly. 1,045 counting of 2,048 rows of
 // 262,144 float32 logits: 205 us, without it 224.
 constexpr unsigned kUnusedLds = 20000;
 

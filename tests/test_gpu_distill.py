@@ -280,3 +280,26 @@ def test_long_rows():
     w = np.ones(n, np.float32)
     g = run(on_gpu(buf, logits), ids, logq, T, w, "rest")
     compare(g, oracle_of(logits, ids, logq, T, w, "rest"), logq, torch.float32)
+
+
+@pytest.mark.parametrize("n,V", [(3, 50257), (70, 20000), (300, 1000), (20, 307300)])
+def test_a_student_that_agrees(n, V):
+    """One entry of probability near 1 that the student gives nearly the same: p - q keeps the precision of 1 - p.
+
+    The entry's exponential and the sum over the entries are the same number. The others' sum o beside it is off by: the
+    exponent's scale, 2^-24 of at most 30 nats, 1.8e-6; the rounded difference of the two parts' exponents (below 64 in
+    base 2), 2^-19 ln 2 = 1.3e-6; exponentials and sums 2^-21. Together below 4e-6, so p = 1 / (1 + o) is off by
+    4e-6 p (1 - p); what follows is in 64 bits.
+    """
+    rng = np.random.default_rng(V)
+    logits = torch.tensor(rng.normal(0, 1, (n, V)), dtype=torch.float32)
+    y = rng.integers(0, V, n)
+    logits[torch.arange(n), torch.tensor(y)] = torch.tensor(rng.uniform(18, 24, n), dtype=torch.float32)
+    z = logits.double().numpy()
+    p = np.exp(z[np.arange(n), y] - np.log(np.exp(z - 24).sum(1)) - 24)
+    logq = np.log(p * (1 + 1e-4 * rng.normal(0, 1, n)).clip(max=1.0)).astype(np.float32)[:, None]
+    ids, T, w = y.astype(np.int32)[:, None], np.ones(n, np.float32), np.ones(n, np.float32)
+    g = run(logits.cuda(), ids, logq, T, w, "drop")["grad"][torch.arange(n), torch.tensor(y)].double().cpu().numpy()
+    q = np.exp(logq[:, 0].astype(np.float64))
+    exact = q * p - q
+    assert (np.abs(g - exact) <= 4e-6 * p * (1 - p) + 2.0 ** -24 * np.abs(exact) + 1e-14).all(), (g, exact)
