@@ -658,7 +658,7 @@ def _check_row_floats(device, n: int, **tensors):
 
 def _rows_apart(t, V: int) -> bool:
     """Whether a 2-D tensor's rows are contiguous and do not overlap."""
-    return t.stride(1) == 1 and (t.shape[0] <= 1 or t.stride(0) >= V)
+    return (V == 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= V)
 
 
 def _check_loss(logits, ids, temperature, grad):
