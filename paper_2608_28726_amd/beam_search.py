@@ -36,7 +36,8 @@ def beam_search(next_logits, n_req: int, n_beams: int, length: int, temperature:
 
     Returns a dict with ``tokens`` (int32 [n_req, n_beams, length], best beam
     first, -1 after the end), ``scores`` (float32 [n_req, n_beams], sums of
-    log-probs) and ``done`` (bool, whether a beam reached ``end``).
+    log-probs) and ``done`` (bool, whether a beam reached ``end``). A beam that
+    does not exist (there were fewer candidates) has a score of -inf and no tokens.
     """
     n = n_req * n_beams
     scores = torch.full((n_req, n_beams), -torch.inf, device=device)
@@ -59,7 +60,9 @@ def beam_search(next_logits, n_req: int, n_beams: int, length: int, temperature:
         tokens[:, t] = token
         if end is not None:
             done |= (token == end).view(n_req, n_beams)
-    return {"tokens": tokens.view(n_req, n_beams, length), "scores": scores, "done": done}
+    there = scores > -torch.inf
+    tokens = torch.where(there[..., None], tokens.view(n_req, n_beams, length), -1)
+    return {"tokens": tokens, "scores": scores, "done": done & there}
 
 
 class Contexts:

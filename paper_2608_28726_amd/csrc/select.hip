@@ -333,7 +333,7 @@ __device__ __forceinline__ void in_order_by_bins(const uint64_t* key, uint64_t* 
 struct Bins {
   float low, scale;
   __device__ __forceinline__ int of(float z) const {
-    return min(255, static_cast<int>(fmaxf((z - low) * scale, 0.0f)));
+    return static_cast<int>(fminf(fmaxf((z - low) * scale, 0.0f), 255.0f));
   }
   __device__ __forceinline__ int operator()(uint64_t key) const { return of(key_logit(key)); }
 };
@@ -694,7 +694,7 @@ __global__ __launch_bounds__(kRowBlock) void top_merge_kernel(TopArgs a, const u
   const float low = key_float(floor), width = (norm.m - low) * (1.0f / 255.0f);
   const float scale = floor > 0 && width > 0.0f && width < INFINITY ? 1.0f / width : 0.0f;
   auto bin_of = [&](uint64_t v) {
-    return scale > 0.0f ? min(255, static_cast<int>(fmaxf((key_logit(v) - low) * scale, 0.0f))) : 255;
+    return scale > 0.0f ? static_cast<int>(fminf(fmaxf((key_logit(v) - low) * scale, 0.0f), 255.0f)) : 255;
   };
 #pragma unroll
   for (int i = 0; i < PER; ++i) {

@@ -136,3 +136,23 @@ def test_examples_run(capsys):
     assert bs.main(["5", "3", "4"]) == 0
     assert "answers ship" in capsys.readouterr().out
     assert pt.main(["distill", "2"]) == 0
+
+
+def test_beams_that_cease_to_exist():
+    """Rows that are NaN leave a request without candidates: no tokens, no end, and the other request goes on."""
+    n_req, B, V, length = 2, 3, 20, 4
+    first, after = table(n_req, V, length, 5)
+    d_first, d_after = torch.tensor(first).cuda(), torch.tensor(after).cuda()
+
+    def next_logits(t, tokens):
+        if t == 0:
+            return d_first.repeat_interleave(B, 0)
+        z = d_after[t][tokens.clamp(min=0).long()]
+        if t == 2:
+            z[:B] = math.nan
+        return z
+
+    out = bs.beam_search(next_logits, n_req, B, length, 1.0, end=None)
+    assert (out["scores"][0] == -math.inf).all() and (out["tokens"][0] == -1).all() and not out["done"].any()
+    scores, tokens, _, _ = plain_search(first[1:], after, 1, B, length, 1.0, None)
+    assert np.array_equal(out["tokens"][1].cpu().numpy(), tokens[0])
