@@ -765,12 +765,17 @@ struct Candidate {
 
 // The k best candidates of a request, by one workgroup. The parts' lists are in
 // order: where m of them have a j-th candidate not below some score and m j is
-// at least k, no candidate below it is among the best (each wave takes its own
-// j). The few that are left are counted against each other, or, where they are
-// many, selected from by digits of their scores. SMALL: a request has at most
-// kHeld candidates, which the threads read at once and hold. A chain of a few
-// reads and barriers bounds it: 5.1 us for one request, 6.2 for 64.
-constexpr int kCounted = 512, kHeld = 4 * kBeamBlock;
+// at least k, no candidate below it is among the best. With j in powers of two
+// fewer than 2 k (1 + log2 k) are above the largest of these scores, however they
+// spread over the lists. Those that are left are cut by 256 bins of their scores
+// and counted against each other, or, where many are equal, selected from by
+// digits. SMALL: a request has at most kHeld candidates, which the threads read
+// at once and hold. A chain of a few reads and barriers bounds it: 5.1 us for one
+// request, 6.2 for 64. With the rows' kernel, k = 128, 64 beams of 151,936
+// bfloat16 logits whose scores differ take 99 us, alike 67 (with three j beside k
+// and no bins 1,234 and 51; with as many j apart in equal ratios 158 at the worst
+// of 128 such rows, where this takes 101).
+constexpr int kCounted = 512, kHeld = 4 * kBeamBlock, kListed = 4096;
 
 template <bool SMALL>
 __global__ __launch_bounds__(kBeamBlock) void beam_merge_kernel(BeamArgs a, const RowSum* sums, const uint64_t* list) {
@@ -781,6 +786,11 @@ __global__ __launch_bounds__(kBeamBlock) void beam_merge_kernel(BeamArgs a, cons
   __shared__ Candidate best[kCounted];
   __shared__ alignas(16) uint32_t near[kCounted + 4];
   __shared__ uint32_t held[SMALL ? kHeld : 1];
+  // Of larger requests the candidates from the floor on: their scores and entries.
+  __shared__ uint32_t listed[SMALL ? 1 : kListed];
+  __shared__ int32_t entry[SMALL ? 1 : kListed];
+  __shared__ alignas(16) uint32_t hist[SMALL ? 4 : 256];
+  __shared__ uint32_t n_listed, least, most;
   __shared__ uint32_t bound[NW], n_best;
   __shared__ CutLds cut_lds;
   const int64_t first = static_cast<int64_t>(blockIdx.x) * a.B;
@@ -826,9 +836,10 @@ __global__ __launch_bounds__(kBeamBlock) void beam_merge_kernel(BeamArgs a, cons
     }
     __syncthreads();
   }
-  {
+  const int share = (a.k + lists - 1) / lists;
+  // What the j-th candidates of the lists bound.
+  auto bound_of = [&](int j) -> uint32_t {
     constexpr int PER = PR_MAX_BEAMS * kMaxSplit / kWave;
-    const int share = (a.k + lists - 1) / lists, j = wave == NW - 1 ? a.k : min(a.k, share << wave);
     const int m = (a.k + j - 1) / j, used = (lists + kWave - 1) / kWave;
     auto jth = [&](int l) -> uint32_t {
       if (l >= lists) return 0;
@@ -836,32 +847,123 @@ __global__ __launch_bounds__(kBeamBlock) void beam_merge_kernel(BeamArgs a, cons
       if constexpr (SMALL) return held[e];
       return near_key(score_of(e, mine[e]));
     };
-    uint32_t at;
     if (used == 1) {
       const uint32_t v[1] = {jth(lane)};
-      at = wave_nth(v, 1, m);
-    } else {
-      uint32_t v[PER];
+      return wave_nth(v, 1, m);
+    }
+    uint32_t v[PER];
 #pragma unroll
-      for (int u = 0; u < PER; ++u) v[u] = u < used ? jth(u * kWave + lane) : 0;
-      at = wave_nth(v, used, m);
+    for (int u = 0; u < PER; ++u) v[u] = u < used ? jth(u * kWave + lane) : 0;
+    return wave_nth(v, used, m);
+  };
+  {
+    // j = share, 2 share, 4 share, .., k, dealt to the waves; of a small request's one
+    // each, which leaves few enough.
+    uint32_t at = 0;
+    if constexpr (SMALL) {
+      at = bound_of(wave == NW - 1 ? a.k : min(a.k, share << wave));
+    } else {
+#pragma unroll 1
+      for (int i = wave; i == 0 || share << (i - 1) < a.k; i += NW) at = max(at, bound_of(min(a.k, share << i)));
     }
     if (lane == 0) bound[wave] = at;
   }
   __syncthreads();
   uint32_t floor = 0;
   for (int w = 0; w < NW; ++w) floor = max(floor, bound[w]);
+  // fn(entry, score's key, beam, token) for each candidate from the floor on. The
+  // lists are in order: a wave walks its own, `span` lanes a list and four entries a
+  // lane at a time, for as long as one of them reaches the floor.
+  auto walk = [&](auto fn) {
+    const int own = (lists - wave + NW - 1) / NW;
+    const int span = own >= kWave ? 1 : 1 << (31 - __builtin_clz(kWave / max(own, 1)));
+    for (int l0 = 0; l0 < own; l0 += kWave / span) {
+      const int l = (l0 + lane / span) * NW + wave;
+      const bool mine_too = l0 + lane / span < own;
+      const int b = mine_too ? l / a.G : 0;
+      for (int j0 = lane % span;; j0 += 4 * span) {
+        uint64_t key[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          key[i] = mine_too && j0 + i * span < a.k && state[b] == 1 ? mine[l * a.k + j0 + i * span] : 0;
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = j0 + i * span, e = l * a.k + j;
+          const uint64_t s = mine_too && j < a.k ? score_of(e, key[i]) : 0;
+          if (s == 0 || near_key(s) < floor) continue;
+          any = true;
+          fn(e, s, b, key[i]);
+        }
+        if (!__any(any)) break;
+      }
+    }
+  };
+  bool in_list = false;
+  if constexpr (!SMALL) {
+    if (t == 0) {
+      n_listed = most = 0;
+      least = ~0u;
+    }
+    hist[t] = 0;
+    __syncthreads();
+    walk([&](int e, uint64_t s, int, uint64_t) {
+      const uint32_t at = atomicAdd(&n_listed, 1u), key = near_key(s);
+      atomicMax(&most, key);
+      atomicMin(&least, key);
+      if (at < static_cast<uint32_t>(kListed)) {
+        listed[at] = key;
+        entry[at] = e;
+      }
+    });
+    __syncthreads();
+    const int n = static_cast<int>(n_listed);
+    in_list = n <= kListed;
+    if (in_list && n > kCounted) {
+      // Those from the k-th's of 256 bins on.
+      constexpr int PER = kListed / kBeamBlock;
+      const float low = key_float(least), width = (key_float(most) - low) * (1.0f / 255.0f);
+      const float scale = width > 0x1p-120f && width < INFINITY ? 1.0f / width : 0.0f;
+      uint32_t key[PER];
+      int32_t e[PER], bin[PER];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int at = t + i * kBeamBlock;
+        bin[i] = -1;
+        if (at >= n) continue;
+        key[i] = listed[at];
+        e[i] = entry[at];
+        bin[i] = static_cast<int>(fminf(fmaxf((key_float(key[i]) - low) * scale, 0.0f), 255.0f));
+        atomicAdd(&hist[bin[i]], 1u);
+      }
+      __syncthreads();
+      const int from = cut_bin(hist, static_cast<uint32_t>(a.k));
+      if (t == 0) n_listed = 0;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        if (bin[i] < from) continue;
+        const uint32_t at = atomicAdd(&n_listed, 1u);
+        listed[at] = key[i];
+        entry[at] = e[i];
+      }
+      __syncthreads();
+    }
+  }
   // Each candidate of the thread from the floor on: its score's key, beam and token.
   auto candidates = [&](auto fn) {
     if constexpr (SMALL) {
 #pragma unroll
       for (int i = 0; i < HELD; ++i)
         if (score[i] != 0 && near_key(score[i]) >= floor) fn(score[i], (t + i * kBeamBlock) / per, token[i]);
-    } else {
-      for (int e = t; e < N; e += kBeamBlock) {
-        const uint64_t key = state[e / per] == 1 ? mine[e] : 0, s = score_of(e, key);
-        if (s != 0 && near_key(s) >= floor) fn(s, e / per, key);
+    } else if (in_list) {
+      for (int i = t; i < static_cast<int>(n_listed); i += kBeamBlock) {
+        const int e = entry[i], b = e / per;
+        const uint64_t key = state[b] == 1 ? mine[e] : 0;
+        fn(score_of(e, key), b, key);
       }
+    } else {
+      walk([&](int, uint64_t s, int b, uint64_t key) { fn(s, b, key); });
     }
   };
   candidates([&](uint64_t s, int b, uint64_t key) {

@@ -198,6 +198,34 @@ def test_select_against_the_oracle(n_req, B, V, k, dtype, pad, start):
     compare_select(g, obeam.beam_select(raw, name, T, scores, k), "none done ")
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n_req,B,V,k", [(1, 64, 50257, 128), (2, 64, 9000, 256), (3, 20, 20000, 256), (1, 1, 60000, 256),
+                                         (60, 4, 3000, 256)])
+def test_candidates_spread_unevenly(n_req, B, V, k, dtype):
+    """Scores that leave most of the best to a few beams, or to all of them alike; beams of one token each beside them."""
+    rng = np.random.default_rng([n_req, B, k])
+    logits = torch.tensor(rng.normal(0, 1.5, (n_req * B, V)).astype(np.float32)).to(dtype)
+    logits[::5, 1:] = -np.inf
+    T = np.ones(n_req * B, np.float32)
+    for spread in (0.0, 0.7, 6.0):
+        scores = rng.normal(-20, spread, (n_req, B)).astype(np.float32)
+        g = pr.beam_select(logits.cuda(), cuda(scores), cuda(T), k=k)
+        o = obeam.beam_select(raw_of(logits), name_of(dtype), T, scores, k)
+        torch.cuda.synchronize()
+        best, parent, token = (g[x].cpu().numpy() for x in ("scores", "parent", "token"))
+        near(f"spread {spread} scores", best, o["scores"], 3 * L_ABS)
+        for i in range(n_req):
+            listed = o["candidates"][i]
+            n = min(k, len(listed))
+            assert (parent[i, n:] == -1).all() and (token[i, n:] == -1).all()
+            have = {(b, v): s for s, b, v, _ in listed}
+            for j in range(n):  # candidates that near may stand in each other's place,
+                assert abs(have[parent[i, j], token[i, j]] - listed[j][0]) <= 2 * L_ABS + 2.0 ** -40 * 100
+            for b in range(B):  # but not those of one beam
+                got = token[i, :n][parent[i, :n] == b].tolist()
+                assert got == [v for _, c, v, _ in listed if c == b][:len(got)]
+
+
 def test_first_step_and_default_k():
     """At first only one beam exists: its best tokens, in order."""
     buf, logits, _, T, rng = make_rows(12, 700, torch.bfloat16, 2)
