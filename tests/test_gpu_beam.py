@@ -226,6 +226,19 @@ def test_candidates_spread_unevenly(n_req, B, V, k, dtype):
                 assert got == [v for _, c, v, _ in listed if c == b][:len(got)]
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("first", [0, 3])
+def test_many_equal_candidates(first, dtype):
+    """64 beams of equal logits: 16,384 candidates, all of one score, come out by beam and token."""
+    B, V, k = 64, 300, 256
+    scores = np.zeros((2, B), np.float32)
+    scores[:, :first] = -np.inf
+    g = pr.beam_select(torch.zeros(2 * B, V, dtype=dtype, device="cuda"), cuda(scores), k=k)
+    torch.cuda.synchronize()
+    assert (g["parent"] == first).all() and torch.equal(g["token"][1], torch.arange(k, dtype=torch.int32, device="cuda"))
+    near("scores", g["scores"].cpu().numpy(), np.full((2, k), -np.log(V)), 3 * L_ABS)
+
+
 def test_first_step_and_default_k():
     """At first only one beam exists: its best tokens, in order."""
     buf, logits, _, T, rng = make_rows(12, 700, torch.bfloat16, 2)
