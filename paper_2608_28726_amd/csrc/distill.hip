@@ -344,7 +344,7 @@ __device__ DistillPart row_part(const DistillArgs& a, int64_t r, int g, int G, f
 
 // One workgroup per row: its sums and everything but its gradient. The read
 // bounds it where rows are long: 1,045 counting of 2,048 rows of 262,144 float32
-// logits with 128 entries 207 us (5.3 TB/s); where they are short, their entries.
+// logits with 128 entries 209 us (5.3 TB/s); where they are short, their entries.
 template <typename Tin>
 __global__ __launch_bounds__(kStatsBlock) void distill_stats_kernel(DistillArgs a, double* term, RowDistill* rd,
                                                                    SortedRows sorted, int64_t first) {
@@ -365,7 +365,7 @@ __global__ __launch_bounds__(kStatsBlock) void distill_stats_kernel(DistillArgs 
 }
 
 // The parts of a few rows, G of them a row: 17 rows of 50,257 bfloat16 logits with
-// 256 entries 7.9 us, most of it a chain of barriers.
+// 256 entries 7.7 us, most of it a chain of barriers.
 template <typename Tin>
 __global__ __launch_bounds__(kStatsBlock) void distill_parts_kernel(DistillArgs a, DistillPart* part, int G) {
   const int64_t r = blockIdx.x / G;
@@ -499,7 +499,7 @@ __device__ __forceinline__ void grad_stretch(const DistillArgs& a, int64_t r, in
 
 // The gradients of the rows from `first` on (blockIdx.y), from factors that a
 // kernel before has written; the first variant's entries are sorted. It moves the
-// bytes of a copy: the 2,048 rows above 516 us (6.3 TB/s).
+// bytes of a copy: the 2,048 rows above 507 us (6.4 TB/s).
 template <typename Tin>
 __global__ __launch_bounds__(kGradBlock) void distill_sorted_grad_kernel(DistillArgs a, const RowDistill* rd,
                                                                         SortedRows sorted, int64_t first) {
@@ -556,7 +556,7 @@ __global__ __launch_bounds__(kGradBlock) void distill_grad_kernel(DistillArgs a,
 }
 
 // The gradients of a few split rows: each workgroup works out its own row's
-// factors instead of waiting for a kernel that does (the 17 rows above: 6.1 us).
+// factors instead of waiting for a kernel that does (the 17 rows above: 5.8 us).
 // The first workgroup of the grid's last row finishes the rows.
 template <typename Tin>
 __global__ __launch_bounds__(kGradBlock) void distill_parts_grad_kernel(DistillArgs a, const DistillPart* part, int G) {
