@@ -772,9 +772,8 @@ struct Candidate {
 // digits. SMALL: a request has at most kHeld candidates, which the threads read
 // at once and hold. A chain of a few reads and barriers bounds it: 5.1 us for one
 // request, 6.2 for 64. With the rows' kernel, k = 128, 64 beams of 151,936
-// bfloat16 logits whose scores differ take 99 us, alike 67 (with three j beside k
-// and no bins 1,234 and 51; with as many j apart in equal ratios 158 at the worst
-// of 128 such rows, where this takes 101).
+// bfloat16 logits whose scores differ take 77 us, alike 59. (Rows in eight parts:
+// 99 and 67; with three j beside k and no bins 1,234 and 51.)
 constexpr int kCounted = 512, kHeld = 4 * kBeamBlock, kListed = 4096;
 
 template <bool SMALL>
@@ -1033,31 +1032,46 @@ __global__ __launch_bounds__(kBeamBlock) void beam_merge_kernel(BeamArgs a, cons
 
 constexpr int64_t kMostGroups = int64_t{1} << 23;  // a grid holds less than 2^32 threads
 
-// Workgroups along a row: one from 192 rows on, else about 512 in all, each with
-// at least 512 vectors. In parts and whole, k = 8: 200 rows of 151,936 bfloat16
-// logits 26.2 and 19.1 us, of 262,144 float32 logits 46 and 37; 128 rows 21.9 and
-// 19, 31.5 and 37. About 256 and 512 in all, k = 64: 128 rows of 262,144 float32
+// Workgroups along a row that is taken in parts: about 512 in all, each with at
+// least 512 vectors. About 256 and 512 in all, k = 64: 128 rows of 262,144 float32
 // logits 39.4 and 34.0, 16 rows 19.4 and 19.3. At least 256 and 512 vectors: 17
 // rows of 50,257 bfloat16 logits, k = 256, 32.5 and 29.6.
-constexpr int64_t kWholeRows = 192, kGroups = 512, kLeastVectors = 512;
+constexpr int64_t kGroups = 512, kLeastVectors = 512;
 
-int beam_split(int64_t n_rows, int32_t V, pr_dtype dtype) {
-  if (n_rows <= 0 || n_rows >= kWholeRows) return 1;
-  const int64_t nvec = V / (dtype == PR_BF16 ? 8 : 4);
+int row_groups(int64_t n_rows, int64_t nvec) {
   const int64_t want = (kGroups + n_rows - 1) / n_rows, most = nvec / kLeastVectors;
   const int64_t G = want < most ? want : most;
   return static_cast<int>(G < 1 ? 1 : G > kMaxSplit ? kMaxSplit : G);
 }
 
-// Where no request is merged afterwards, whole rows save a launch, and that is
-// more than parts save of a short row. In parts and whole: 64 rows of 32,000
-// float32 logits (8,000 vectors), k = 8, 16.8 and 13.9 us, 17 rows of 50,257
-// bfloat16 logits, k = 256, 25 and 17.5; of 18,992 vectors, k = 8, 16 rows 17.4 and
-// 19, 64 rows 18.2 and 19.
-constexpr int64_t kWholeVectors = 12288;
+// Workgroups along a beam's row. Longer lists are whole rows', as the merge takes
+// all lists of a request. In parts and whole, requests of 4 beams: of 151,936
+// bfloat16 logits k = 4, 64 rows 19.4 and 24.8 us, 128 rows 23.2 and 25.4, 160
+// rows 25.7 and 25.5, k = 16, 64 rows 23.9 and 28.4, k = 64, 44.5 and 40.1, k =
+// 256, 141 and 105; of 32,000 float32 logits k = 4, 64 rows 14.9 and 17.4, k = 64,
+// 28.7 and 20.3; of 262,144 float32 logits (65,536 vectors) k = 64, 16 rows 30.6
+// and 37.9, 64 rows 36.9 and 39.6, k = 128, 47.9 and 45.9.
+constexpr int64_t kWholeBeams = 160, kLongVectors = 32768;
 
-int top_split(int64_t n_rows, int32_t V, pr_dtype dtype) {
-  return V / (dtype == PR_BF16 ? 8 : 4) <= kWholeVectors ? 1 : beam_split(n_rows, V, dtype);
+int beam_split(int64_t n_rows, int32_t V, pr_dtype dtype, int32_t k) {
+  const int64_t nvec = V / (dtype == PR_BF16 ? 8 : 4);
+  if (n_rows <= 0 || n_rows >= kWholeBeams || k > (nvec < kLongVectors ? 32 : 64)) return 1;
+  return row_groups(n_rows, nvec);
+}
+
+// And along a row of which no request's beams are merged: whole rows save a
+// launch, which is more than parts save of a short row or of many. In parts and
+// whole: 64 rows of 32,000 float32 logits (8,000 vectors), k = 8, 16.8 and 13.9;
+// of 18,992 vectors, k = 16, 32 rows 18.2 and 20.1, 64 rows 19.6 and 20.6, 96 rows
+// 22.7 and 20.9, k = 256, 16 rows 25.6 and 27.7, 64 rows 32.4 and 27.9; of 65,536
+// vectors, k = 16, 96 rows 31.0 and 31.4, 160 rows 39.0 and 35.1, k = 256, 64 rows
+// 32.5 and 43.3, 160 rows 48.9 and 43.9.
+constexpr int64_t kWholeVectors = 12288, kWholeRows = 128;
+
+int top_split(int64_t n_rows, int32_t V, pr_dtype dtype, int32_t k) {
+  const int64_t nvec = V / (dtype == PR_BF16 ? 8 : 4);
+  const int64_t most = (nvec / 256 < kWholeRows ? nvec / 256 : kWholeRows) / (k > 64 && nvec <= kLongVectors ? 2 : 1);
+  return n_rows <= 0 || nvec <= kWholeVectors || n_rows >= most ? 1 : row_groups(n_rows, nvec);
 }
 
 // Whether whole rows are taken by 512 threads: up to a few hundred, which are a
@@ -1121,24 +1135,24 @@ hipError_t beam(const BeamArgs& a, hipStream_t stream) {
 }  // namespace
 
 size_t top_workspace_bytes(int64_t n_rows, int32_t V, pr_dtype dtype, int32_t k) {
-  const int G = top_split(n_rows, V, dtype);
+  const int G = top_split(n_rows, V, dtype, k);
   return G > 1 ? lists_bytes(n_rows, G, k) : 0;
 }
 
 hipError_t launch_top(const TopArgs& a, pr_dtype dtype, hipStream_t stream) {
   TopArgs x = a;
-  x.G = top_split(a.n_rows, a.V, dtype);
+  x.G = top_split(a.n_rows, a.V, dtype, a.k);
   if (x.k <= 64) return dtype == PR_BF16 ? top<uint16_t, 64>(x, stream) : top<float, 64>(x, stream);
   return dtype == PR_BF16 ? top<uint16_t, kMaxTop>(x, stream) : top<float, kMaxTop>(x, stream);
 }
 
 size_t beam_workspace_bytes(int64_t n_rows, int32_t V, pr_dtype dtype, int32_t k) {
-  return n_rows < 1 ? 0 : lists_bytes(n_rows, beam_split(n_rows, V, dtype), k);
+  return n_rows < 1 ? 0 : lists_bytes(n_rows, beam_split(n_rows, V, dtype, k), k);
 }
 
 hipError_t launch_beam(const BeamArgs& a, pr_dtype dtype, hipStream_t stream) {
   BeamArgs x = a;
-  x.G = beam_split(static_cast<int64_t>(a.n_req) * a.B, a.V, dtype);
+  x.G = beam_split(static_cast<int64_t>(a.n_req) * a.B, a.V, dtype, a.k);
   if (x.k <= 64) return dtype == PR_BF16 ? beam<uint16_t, 64>(x, stream) : beam<float, 64>(x, stream);
   return dtype == PR_BF16 ? beam<uint16_t, kMaxTop>(x, stream) : beam<float, kMaxTop>(x, stream);
 }
