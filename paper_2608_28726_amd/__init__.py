@@ -569,10 +569,12 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, temperature=1.0, k: 
     if workspace is not None:
         _check_workspace(workspace, device)
     if workspace is None or workspace.numel() * workspace.element_size() < need or workspace.data_ptr() % 16:
-        workspace, best, logprob = torch.empty((-(-need // (4 * k)) + 2 * n_req, k), device=device).unsafe_split_with_sizes(
-            (-(-need // (4 * k)), n_req, n_req))
+        rows = -(-need // (4 * k))
+        workspace, best, logprob = torch.empty((rows + 2 * n_req, k), dtype=torch.float32,
+                                               device=device).unsafe_split_with_sizes((rows, n_req, n_req))
     else:
-        best, logprob = torch.empty((2 * n_req, k), device=device).unsafe_split_with_sizes((n_req, n_req))
+        best, logprob = torch.empty((2 * n_req, k), dtype=torch.float32, device=device).unsafe_split_with_sizes(
+            (n_req, n_req))
     ws_bytes = workspace.numel() * workspace.element_size()
     parent, token = torch.empty((2 * n_req, k), dtype=torch.int32, device=device).unsafe_split_with_sizes((n_req, n_req))
     flags = torch.empty(n, dtype=torch.int32, device=device)

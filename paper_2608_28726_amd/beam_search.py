@@ -40,7 +40,7 @@ def beam_search(next_logits, n_req: int, n_beams: int, length: int, temperature:
     does not exist (there were fewer candidates) has a score of -inf and no tokens.
     """
     n = n_req * n_beams
-    scores = torch.full((n_req, n_beams), -torch.inf, device=device)
+    scores = torch.full((n_req, n_beams), -torch.inf, dtype=torch.float32, device=device)
     scores[:, 0] = 0.0  # one beam to begin with
     tokens = torch.full((n, length), -1, dtype=torch.int32, device=device)
     done = torch.zeros(n_req, n_beams, dtype=torch.bool, device=device)
@@ -72,7 +72,7 @@ class Contexts:
         g = torch.Generator(device=hidden.device)
         g.manual_seed(seed)
         width = hidden.shape[1]
-        self.embedding = torch.empty(vocab, width, device=hidden.device).normal_(generator=g).bfloat16()
+        self.embedding = torch.empty(vocab, width, dtype=torch.float32, device=hidden.device).normal_(generator=g).bfloat16()
         self.hidden = hidden.repeat_interleave(n_beams, 0)
         self.seen = torch.zeros(self.hidden.shape[0], length, width, dtype=hidden.dtype, device=hidden.device)
 
@@ -110,8 +110,9 @@ def main(argv) -> int:
     vocab, width, device = 32000, 256, "cuda"
     g = torch.Generator(device=device)
     g.manual_seed(1)
-    weight = torch.empty(vocab, width, device=device).normal_(std=2.0 * width ** -0.5, generator=g).bfloat16()
-    hidden = torch.empty(requests, width, device=device).normal_(generator=g).bfloat16()
+    weight = torch.empty(vocab, width, dtype=torch.float32, device=device).normal_(std=2.0 * width ** -0.5, generator=g)
+    weight = weight.bfloat16()
+    hidden = torch.empty(requests, width, dtype=torch.float32, device=device).normal_(generator=g).bfloat16()
     out = search(lambda h: h @ weight.t(), hidden, vocab, beams, length, seed=2)
     best = out["confidence"][:, 0].contiguous()
     tau, _ = pr.calibrate_threshold(best, 0.5)

@@ -40,7 +40,7 @@ class OutputLayer:
     def __init__(self, vocab: int, width: int, state_bits: int, seed: int, device):
         g = torch.Generator(device=device)
         g.manual_seed(seed)
-        self.weight = torch.empty(vocab, width, device=device).normal_(std=width ** -0.5, generator=g)
+        self.weight = torch.empty(vocab, width, dtype=torch.float32, device=device).normal_(std=width ** -0.5, generator=g)
         self.copy = self.weight.bfloat16()
         self.opt = pr.AdamW([self.weight], copies=[self.copy], state_bits=state_bits, seed=seed)
 
@@ -85,7 +85,8 @@ def _teacher(hidden, vocab, length, seed):
     g = torch.Generator(device=hidden.device)
     g.manual_seed(seed + 2)
     width = hidden.shape[1]
-    weight = torch.empty(vocab, width, device=hidden.device).normal_(std=2.0 * width ** -0.5, generator=g).bfloat16()
+    weight = torch.empty(vocab, width, dtype=torch.float32, device=hidden.device).normal_(std=2.0 * width ** -0.5, generator=g)
+    weight = weight.bfloat16()
     answers = search(lambda h: h @ weight.t(), hidden[::length].contiguous(), vocab, BEAMS, length, seed, TEMPERATURE)
     rows = answers["contexts"][:, 0].reshape(-1, width).contiguous()
     return rows, pr.top_logits(rows @ weight.t(), min(TOP, vocab), TEMPERATURE)
@@ -107,22 +108,22 @@ def post_train(method: str = "policy", steps: int = 60, vocab: int = 4096, width
     g = torch.Generator(device=device)
     g.manual_seed(seed + 1)
     n = requests * length
-    hidden = torch.empty(n, width, device=device).normal_(generator=g)
+    hidden = torch.empty(n, width, dtype=torch.float32, device=device).normal_(generator=g)
     hidden[:, 0] = 2.0  # what every context has in common
     hidden = hidden.bfloat16()
-    earns = (torch.rand(vocab, generator=g, device=device) < 0.25).float()
+    earns = (torch.rand(vocab, generator=g, dtype=torch.float32, device=device) < 0.25).float()
     layer = OutputLayer(vocab, width, state_bits, seed, device)
     offsets = torch.arange(0, n + 1, length, dtype=torch.int32, device=device)
     losses, rewards = [], []
     if method == "policy":
-        weight = torch.full((n,), 1.0 / n, device=device)
+        weight = torch.full((n,), 1.0 / n, dtype=torch.float32, device=device)
         for step in range(steps):
             loss, reward = _policy_step(layer, hidden, earns, weight, length, lr, seed, step)
             losses.append(loss)
             rewards.append(reward)
     elif method == "distill":
         hidden, top = _teacher(hidden, vocab, length, seed)
-        weight = torch.full((n,), 1.0 / n, device=device)
+        weight = torch.full((n,), 1.0 / n, dtype=torch.float32, device=device)
         for step in range(steps):
             loss, reward = _distill_step(layer, hidden, top, weight, lr)
             losses.append(loss)
@@ -130,7 +131,7 @@ def post_train(method: str = "policy", steps: int = 60, vocab: int = 4096, width
     else:
         ref = layer.copy.clone()
         twice = torch.cat([hidden, hidden])
-        weight = torch.ones(2 * n, device=device)
+        weight = torch.ones(2 * n, dtype=torch.float32, device=device)
         pairs = torch.arange(0, 2 * n + 1, length, dtype=torch.int32, device=device)
         for step in range(steps):
             loss, reward = _preference_step(layer, twice, earns, weight, length, lr, seed, step, ref, pairs)
