@@ -741,14 +741,13 @@ __device__ __forceinline__ bool beam_live(const BeamArgs& a, int64_t r, uint32_t
 // 256 rows of 151,936 bfloat16 logits 20.7 us (3.8 TB/s), 410 live of 512 rows of
 // 262,144 float32 logits 69 us (6.2 TB/s).
 template <typename Tin, int BLOCK, int KMAX>
-__global__ __launch_bounds__(BLOCK) void beam_rows_kernel(BeamArgs a, RowSum* sums, uint64_t* list) {
+__global__ __launch_bounds__(BLOCK) void beam_rows_kernel(BeamArgs a, RowSum* sums, uint64_t* list, int64_t first) {
   __shared__ ListLds<BLOCK, KMAX> s;
-  const int64_t r = blockIdx.x / a.G;
+  const int64_t r = first + blockIdx.x / a.G, at = first + blockIdx.x;  // first: 0 unless G = 1
   uint32_t flags;
   if (!beam_live(a, r, &flags)) return;
   const Stretch<Tin> x(static_cast<const Tin*>(a.logits) + r * a.row_stride, a.V, blockIdx.x % a.G, a.G);
-  write_part<Tin, BLOCK, KMAX>(x, a.k, scale_of(a.temperature[r]), s, list + static_cast<int64_t>(blockIdx.x) * a.k,
-                               sums + blockIdx.x);
+  write_part<Tin, BLOCK, KMAX>(x, a.k, scale_of(a.temperature[r]), s, list + at * a.k, sums + at);
 }
 
 // A candidate of a request in the order of the selection: score, lower beam,
@@ -1030,7 +1029,18 @@ __global__ __launch_bounds__(kBeamBlock) void beam_merge_kernel(BeamArgs a, cons
   if (t >= n && t < a.k) write(t, -INFINITY, -1, -1, -INFINITY);
 }
 
-constexpr int64_t kMostGroups = int64_t{1} << 23;  // a grid holds less than 2^32 threads
+// Most workgroups of a launch: one that has 2^32 threads or more along x does not run.
+constexpr int64_t most_groups(int block) { return (int64_t{1} << 31) / block; }
+// fn(first, groups) for each of the launches that `groups` workgroups take.
+template <typename Fn>
+hipError_t in_launches(int64_t groups, int block, Fn&& fn) {
+  for (int64_t at = 0; at < groups; at += most_groups(block)) {
+    fn(at, dim3(static_cast<unsigned>(groups - at < most_groups(block) ? groups - at : most_groups(block))));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
 
 // Workgroups along a row that is taken in parts: about 512 in all, each with at
 // least 512 vectors. About 256 and 512 in all, k = 64: 128 rows of 262,144 float32
@@ -1099,17 +1109,13 @@ hipError_t top(const TopArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL(top_merge_kernel, dim3(static_cast<unsigned>(a.n_rows)), dim3(kRowBlock), 0, stream, a, list, sums);
     return hipGetLastError();
   }
-  for (int64_t at = 0; at < a.n_rows; at += kMostGroups) {
-    const int64_t rows = a.n_rows - at < kMostGroups ? a.n_rows - at : kMostGroups;
-    const dim3 grid(static_cast<unsigned>(rows));
-    if (wide_rows(a.n_rows, a.k))
+  const bool wide = wide_rows(a.n_rows, a.k);
+  return in_launches(a.n_rows, wide ? 2 * kRowBlock : kRowBlock, [&](int64_t at, dim3 grid) {
+    if (wide)
       hipLaunchKernelGGL((top_kernel<Tin, 2 * kRowBlock, KMAX>), grid, dim3(2 * kRowBlock), 0, stream, a, at);
     else
       hipLaunchKernelGGL((top_kernel<Tin, kRowBlock, KMAX>), grid, dim3(kRowBlock), 0, stream, a, at);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  });
 }
 
 template <typename Tin, int KMAX>
@@ -1117,12 +1123,15 @@ hipError_t beam(const BeamArgs& a, hipStream_t stream) {
   const int64_t n = static_cast<int64_t>(a.n_req) * a.B * a.G;
   uint64_t* list = static_cast<uint64_t*>(a.ws);
   RowSum* sums = reinterpret_cast<RowSum*>(list + n * a.k);
-  const dim3 grid(static_cast<unsigned>(n));
-  if (a.G == 1 && wide_rows(static_cast<int64_t>(a.n_req) * a.B, a.k))
-    hipLaunchKernelGGL((beam_rows_kernel<Tin, 2 * kRowBlock, KMAX>), grid, dim3(2 * kRowBlock), 0, stream, a, sums, list);
-  else
-    hipLaunchKernelGGL((beam_rows_kernel<Tin, kRowBlock, KMAX>), grid, dim3(kRowBlock), 0, stream, a, sums, list);
-  const hipError_t e = hipGetLastError();
+  const bool wide = a.G == 1 && wide_rows(static_cast<int64_t>(a.n_req) * a.B, a.k);
+  // (Rows in parts are few: one launch, so that `at` is a row wherever it is not 0.)
+  const hipError_t e = in_launches(n, wide ? 2 * kRowBlock : kRowBlock, [&](int64_t at, dim3 grid) {
+    if (wide)
+      hipLaunchKernelGGL((beam_rows_kernel<Tin, 2 * kRowBlock, KMAX>), grid, dim3(2 * kRowBlock), 0, stream, a, sums,
+                         list, at);
+    else
+      hipLaunchKernelGGL((beam_rows_kernel<Tin, kRowBlock, KMAX>), grid, dim3(kRowBlock), 0, stream, a, sums, list, at);
+  });
   if (e != hipSuccess) return e;
   const dim3 reqs(static_cast<unsigned>(a.n_req));
   if (a.B * a.G * a.k <= kHeld)
