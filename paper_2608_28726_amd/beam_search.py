@@ -28,7 +28,7 @@ def beam_search(next_logits, n_req: int, n_beams: int, length: int, temperature:
 
     ``next_logits(t, tokens)`` returns the logit rows [n_req * n_beams, V] of
     step t; ``tokens`` (int32 [n_req * n_beams], None at step 0) are those that
-    the beams were continued with, -1 for beams that do not exist. ``states``:
+    the beams were continued with, -1 for beams that have ended or do not exist. ``states``:
     tensors that belong to the beams (:func:`beam_reorder`), reordered in place
     before the next step. ``stream`` and ``slots`` (int32 [n_req, n_beams]):
     the verifier's state and each beam's slot in it; the rows that
@@ -37,7 +37,7 @@ def beam_search(next_logits, n_req: int, n_beams: int, length: int, temperature:
     Returns a dict with ``tokens`` (int32 [n_req, n_beams, length], best beam
     first, -1 after the end), ``scores`` (float32 [n_req, n_beams], sums of
     log-probs) and ``done`` (bool, whether a beam reached ``end``). A beam that
-    does not exist (there were fewer candidates) has a score of -inf and no tokens.
+    does not exist (there were fewer candidates) has a score of -inf and no tokens, and its slot is empty.
     """
     n = n_req * n_beams
     scores = torch.full((n_req, n_beams), -torch.inf, dtype=torch.float32, device=device)
@@ -61,6 +61,9 @@ def beam_search(next_logits, n_req: int, n_beams: int, length: int, temperature:
         if end is not None:
             done |= (token == end).view(n_req, n_beams)
     there = scores > -torch.inf
+    if stream is not None:
+        # What a beam had seen before it ceased to exist is no answer's.
+        stream.reset(torch.where(there, -1, slots).view(-1))
     tokens = torch.where(there[..., None], tokens.view(n_req, n_beams, length), -1)
     return {"tokens": tokens, "scores": scores, "done": done & there}
 
@@ -92,7 +95,7 @@ def search(layer, hidden: torch.Tensor, vocab: int, n_beams: int, length: int, s
            end: int | None = None) -> dict:
     """Beam search of an output layer (``layer(hidden)`` gives logit rows) from each of the hidden states. Besides what
     :func:`beam_search` returns: ``contexts`` [n_req, n_beams, length, width], and of every beam the verifier's summary
-    ``confidence`` [n_req, n_beams]."""
+    ``confidence`` [n_req, n_beams], NaN where there is no beam (no such answer ships)."""
     n_req = hidden.shape[0]
     contexts = Contexts(hidden, vocab, n_beams, length, seed)
     stream = pr.StreamState(n_req * n_beams, length)

@@ -156,3 +156,34 @@ def test_beams_that_cease_to_exist():
     assert (out["scores"][0] == -math.inf).all() and (out["tokens"][0] == -1).all() and not out["done"].any()
     scores, tokens, _, _ = plain_search(first[1:], after, 1, B, length, 1.0, None)
     assert np.array_equal(out["tokens"][1].cpu().numpy(), tokens[0])
+
+
+@pytest.mark.parametrize("max_len", [0, 4])
+def test_the_verifier_of_beams_that_cease_to_exist(max_len):
+    """A request that loses its candidates, one that goes on, and one that never had as many as beams: the verifier has
+    seen the beams that are there, and no answer of the others ships."""
+    n_req, B, V, length = 3, 3, 20, 4
+    first, after = table(n_req, V, length, 5)
+    d_first, d_after = torch.tensor(first).cuda(), torch.tensor(after).cuda()
+
+    def next_logits(t, tokens):
+        z = d_first.repeat_interleave(B, 0) if t == 0 else d_after[t][tokens.clamp(min=0).long()]
+        if t == 2:
+            z[:B] = math.nan
+        z[2 * B:, 2:] = -math.inf  # two tokens: two beams after the first
+        return z
+
+    stream = pr.StreamState(n_req * B, max_len)
+    slots = torch.arange(n_req * B, dtype=torch.int32, device="cuda").view(n_req, B)
+    out = bs.beam_search(next_logits, n_req, B, 1, 1.0, None, (), stream, slots)
+    there = out["scores"] > -math.inf
+    assert there[0].all() and there[2].tolist() == [True, True, False]
+    score = stream.finish(slots.view(-1), 0.0)["score"].view(n_req, B)
+    assert torch.equal(score.isnan(), ~there)
+    out = bs.beam_search(next_logits, n_req, B, length, 1.0, None, (), stream, slots)
+    there = out["scores"] > -math.inf
+    assert not there[0].any() and there[1].all()
+    verdict = stream.finish(slots.view(-1), 0.0)
+    assert torch.equal(verdict["score"].view(n_req, B).isnan(), ~there)
+    assert not verdict["ship"].view(n_req, B)[~there].any()
+    stream.close()
