@@ -1091,7 +1091,9 @@ int top_split(int64_t n_rows, int32_t V, pr_dtype dtype, int32_t k) {
 // 17,904 794 and 890 (k = 64); 512 rows of 32,000 float32 logits 17.1 and 17.3,
 // 1,024 26.0 and 26.5. k = 200: 512 rows of 151,936 45.3 and 38.4, 2,048 130 and
 // 125, of 32,000 float32 65 and 55.
-bool wide_rows(int64_t n_rows, int32_t k) { return n_rows <= 512 || k > 64; }
+bool wide_rows(int64_t n_rows) { return n_rows <= 512; }
+template <int KMAX>
+constexpr int kManyBlock = KMAX <= 64 ? kRowBlock : 2 * kRowBlock;  // of more rows
 
 size_t lists_bytes(int64_t n_rows, int G, int32_t k) {
   return static_cast<size_t>(n_rows) * static_cast<size_t>(G) * (static_cast<size_t>(k) * sizeof(uint64_t) + sizeof(RowSum));
@@ -1109,12 +1111,13 @@ hipError_t top(const TopArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL(top_merge_kernel, dim3(static_cast<unsigned>(a.n_rows)), dim3(kRowBlock), 0, stream, a, list, sums);
     return hipGetLastError();
   }
-  const bool wide = wide_rows(a.n_rows, a.k);
-  return in_launches(a.n_rows, wide ? 2 * kRowBlock : kRowBlock, [&](int64_t at, dim3 grid) {
+  constexpr int MANY = kManyBlock<KMAX>;
+  const bool wide = wide_rows(a.n_rows);
+  return in_launches(a.n_rows, wide ? 2 * kRowBlock : MANY, [&](int64_t at, dim3 grid) {
     if (wide)
       hipLaunchKernelGGL((top_kernel<Tin, 2 * kRowBlock, KMAX>), grid, dim3(2 * kRowBlock), 0, stream, a, at);
     else
-      hipLaunchKernelGGL((top_kernel<Tin, kRowBlock, KMAX>), grid, dim3(kRowBlock), 0, stream, a, at);
+      hipLaunchKernelGGL((top_kernel<Tin, MANY, KMAX>), grid, dim3(MANY), 0, stream, a, at);
   });
 }
 
@@ -1123,14 +1126,15 @@ hipError_t beam(const BeamArgs& a, hipStream_t stream) {
   const int64_t n = static_cast<int64_t>(a.n_req) * a.B * a.G;
   uint64_t* list = static_cast<uint64_t*>(a.ws);
   RowSum* sums = reinterpret_cast<RowSum*>(list + n * a.k);
-  const bool wide = a.G == 1 && wide_rows(static_cast<int64_t>(a.n_req) * a.B, a.k);
+  constexpr int MANY = kManyBlock<KMAX>;
+  const bool wide = a.G == 1 && wide_rows(static_cast<int64_t>(a.n_req) * a.B);
   // (Rows in parts are few: one launch, so that `at` is a row wherever it is not 0.)
-  const hipError_t e = in_launches(n, wide ? 2 * kRowBlock : kRowBlock, [&](int64_t at, dim3 grid) {
+  const hipError_t e = in_launches(n, wide ? 2 * kRowBlock : MANY, [&](int64_t at, dim3 grid) {
     if (wide)
       hipLaunchKernelGGL((beam_rows_kernel<Tin, 2 * kRowBlock, KMAX>), grid, dim3(2 * kRowBlock), 0, stream, a, sums,
                          list, at);
     else
-      hipLaunchKernelGGL((beam_rows_kernel<Tin, kRowBlock, KMAX>), grid, dim3(kRowBlock), 0, stream, a, sums, list, at);
+      hipLaunchKernelGGL((beam_rows_kernel<Tin, MANY, KMAX>), grid, dim3(MANY), 0, stream, a, sums, list, at);
   });
   if (e != hipSuccess) return e;
   const dim3 reqs(static_cast<unsigned>(a.n_req));
