@@ -72,3 +72,27 @@ def test_select_of_as_many_beams_as_are_allowed(k):
         compare_select(got, o)
     with pytest.raises(pr.ProuterError):
         pr.beam_select(torch.zeros(MANY + 1, 2, dtype=torch.bfloat16, device="cuda"), torch.zeros(MANY + 1, 1, device="cuda"))
+
+
+def test_distillation_of_more_rows_than_a_launch_holds():
+    """2^23 + 37 rows, whose sums take two launches and whose gradients 257, against the same rows in two calls; the
+    last ones against the oracle."""
+    n, V, k = MANY + 37, 5, 2
+    z, g = rows(n, V, torch.float32, 9)
+    top = pr.top_logits(z.flip(1).contiguous(), k, 1.0)
+    w = torch.rand(n, device="cuda", generator=g)
+    w[torch.rand(n, device="cuda", generator=g) < 0.2] = 0.0
+    T = torch.rand(n, device="cuda", generator=g) + 0.5
+    whole = pr.distill_loss(z, top["ids"], top["logprob"], T, w)
+    half = n // 2
+    for part in (slice(0, half), slice(half, n)):
+        some = pr.distill_loss(z[part], top["ids"][part], top["logprob"][part], T[part], w[part])
+        torch.cuda.synchronize()
+        for name in ("token_loss", "mass", "flags", "grad"):
+            assert torch.equal(whole[name][part], some[name]), (name, part)
+    part = slice(n - 50, n)
+    raw = raw_of(z[part].cpu())
+    o = odist.distill_loss(raw, "f32", *(x[part].cpu().numpy() for x in (top["ids"], top["logprob"], T, w)))
+    # A row's loss and gradient are off by the log-probs' 2e-6 and a rounding (its terms are at most a few units).
+    assert np.abs(whole["token_loss"][part].cpu().numpy() - o["token_loss"]).max() <= 1e-5
+    assert np.abs(whole["grad"][part].cpu().numpy() - o["grad"]).max() <= 1e-5
