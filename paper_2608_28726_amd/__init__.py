@@ -70,16 +70,17 @@ def _dtype_code(logits: torch.Tensor) -> int:
     raise TypeError(f"logits must be float32 or bfloat16, got {logits.dtype}")
 
 
-def _check_sizes(t, name: str):
+def _check_sizes(shape, name: str):
     """The library counts rows and tokens in 32 bits, and ctypes passes the lower 32 of a larger number on."""
-    if max(t.shape) >= 1 << 31:
-        raise ValueError(f"{name} must have fewer than 2^31 rows and columns, got {list(t.shape)}")
+    rows, columns = shape
+    if (rows | columns) >> 31:
+        raise ValueError(f"{name} must have fewer than 2^31 rows and columns, got {list(shape)}")
 
 
 def _check_rows(logits, sampled_ids, temperature, top_p):
     if not logits.is_cuda or logits.dim() != 2 or logits.stride(1) != 1:
         raise ValueError("logits must be a 2-D CUDA tensor with unit stride along the vocabulary")
-    _check_sizes(logits, "logits")
+    _check_sizes(logits.shape, "logits")
     shape = (logits.shape[0],)
     for name, t, dt in (("sampled_ids", sampled_ids, torch.int32), ("temperature", temperature, torch.float32),
                         ("top_p", top_p, torch.float32)):
@@ -507,7 +508,7 @@ def _check_logits(logits):
         raise ValueError("logits must be a 2-D CUDA tensor with unit stride along the vocabulary")
     code = _dtype_code(logits)
     stream = _check_current(logits.device, "logits")
-    _check_sizes(logits, "logits")
+    _check_sizes(logits.shape, "logits")
     if not _rows_apart(logits, logits.shape[1]):
         raise ValueError("logits must be a 2-D CUDA tensor with unit stride along the vocabulary and rows apart")
     return stream, logits.device, code
@@ -516,7 +517,7 @@ def _check_logits(logits):
 def _check_parents(parent, device):
     if parent.dtype != torch.int32 or parent.dim() != 2 or not parent.is_contiguous() or parent.device != device:
         raise ValueError(f"parent must be a contiguous int32 [n_req, n_beams] tensor on {device}")
-    _check_sizes(parent, "parent")
+    _check_sizes(parent.shape, "parent")
     return parent.shape
 
 
@@ -686,7 +687,7 @@ def _check_loss(logits, ids, temperature, grad):
     device = logits.device
     code = _dtype_code(logits)
     stream = _check_current(device, "logits")
-    _check_sizes(logits, "logits")
+    _check_sizes(logits.shape, "logits")
     if not _rows_apart(logits, V):
         raise ValueError("logits must be a 2-D CUDA tensor with unit stride along the vocabulary and rows apart")
     if ids is not None:
