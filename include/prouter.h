@@ -463,10 +463,12 @@ pr_status pr_stream_reset_slots(pr_stream* state, const int32_t* slots, int32_t 
  * Beam search over streamed requests: slot slots[i * n_beams + b] takes the
  * state that slot slots[i * n_beams + parent[i * n_beams + b]] had before the
  * call (pr_beam_reorder for a state's slots). slots, parent: device int32
- * [n_req][n_beams]; no slot twice. An entry whose parent lies outside
+ * [n_req][n_beams]; no slot twice (duplicates race). An entry whose parent lies outside
  * [0, n_beams), or whose slot or parent's slot is not one of the state's, leaves
  * its slot as it is. 1 <= n_beams <= PR_MAX_BEAMS. Ordered like steps on the same
- * slots; the state's device must be the current one (PR_ERR_INVALID_ARG).
+ * slots; the state's device must be the current one (PR_ERR_INVALID_ARG). A slot
+ * that changes is read and written whole, max_len * 16 + 280 bytes, however many
+ * tokens it has seen.
  */
 pr_status pr_stream_reorder(pr_stream* state, const int32_t* slots, const int32_t* parent, int32_t n_req,
                             int32_t n_beams, void* stream);

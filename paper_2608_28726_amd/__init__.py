@@ -478,8 +478,8 @@ class StreamState:
 
     def reorder(self, slots: torch.Tensor, parent: torch.Tensor) -> None:
         """Beam search (``pr_stream_reorder``): slot ``slots[i, b]`` takes the state that slot
-        ``slots[i, parent[i, b]]`` had; int32 [n_req, n_beams] tensors, no slot twice. A parent outside
-        [0, n_beams) leaves its slot as it is."""
+        ``slots[i, parent[i, b]]`` had; int32 [n_req, n_beams] tensors, no slot twice (duplicates race). A parent
+        outside [0, n_beams) leaves its slot as it is. A slot that changes moves its whole history, ``max_len`` tokens."""
         stream = _check_current(slots.device, "slots")
         n_req, B = _check_parents(parent, slots.device)
         if slots.dtype != torch.int32 or slots.shape != parent.shape or not slots.is_contiguous():

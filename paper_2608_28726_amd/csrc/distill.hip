@@ -592,7 +592,7 @@ __device__ __forceinline__ uint32_t group_slot(const Group& g, int32_t nvec) {
 // to 1,980 us; 512 rows of 32,000 float32 logits with 20 entries 24.7. With up to 64 entries
 // the extra wave keeps pace with the others; with 65 to 256 a lane has up to 4
 // and the row waits for them (4,096 rows of 151,936: 64 entries 534 us, 65 581,
-// 256 706). Two of the smaller workgroups then share a compute unit only where
+// 256 706), the more so as 9 to 34 of its registers are spilled to scratch. Two of the smaller workgroups then share a compute unit only where
 // the launch bound asks for it: 512 rows of 50,257 bfloat16 logits with 256
 // entries 34.6 us, without it 41.6.
 template <typename Tin, int DW, int NR, int KE>

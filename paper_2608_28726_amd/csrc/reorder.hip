@@ -20,7 +20,10 @@ typedef uint32_t Bytes16 __attribute__((ext_vector_type(4), aligned(1)));
 // cache and a thread holds few rows. Cached and past the caches, us: 64 requests
 // of 4 beams, eight states of 128 tokens of 512 bytes (134 MB) 27.7 and 33.4, of
 // 256 tokens 52.6 and 65.8, of 512 tokens (537 MB) 134.8 and 129.2; as many bytes
-// as 32 x 8 beams 162 and 167, 16 x 16 187 and 197, 8 x 32 223 and 220.
+// as 32 x 8 beams 162 and 167, 16 x 16 187 and 197, 8 x 32 223 and 220, 4 x 64
+// (cached) 235: from 9 beams on the row numbers, which all lanes share, exceed the
+// scalar registers (79, 308 and 863 are spilled with up to 16, 32 and 64 beams),
+// and with more than 16 the rows' vectors leave 3 and 1 waves a SIMD.
 constexpr int64_t kCachedStates = 400'000'000;
 
 // Workgroups along a row: 8, 16, 32 and 64 of them took 154, 140, 129 and 129 us

@@ -348,7 +348,9 @@ struct Bins {
 // again with the floor that those give; where that does not help (many equal
 // logits, or ever larger ones), it is selected from by digits. 512 rows of
 // 151,936 bfloat16 logits, 8 of each, take 30 us, 59 where the first 16,384 are
-// masked, 303 where they rise, 446 where all are equal. bins: the last bins.
+// masked, 303 where they rise, 446 where all are equal. A lane has four vectors in
+// flight until the floor is made, 16 rounds of ballots and two barriers; its next
+// loads are issued behind them. bins: the last bins.
 template <typename Tin, int BLOCK, int KMAX>
 __device__ int list_stretch(const Stretch<Tin>& x, int k, float c, ListLds<BLOCK, KMAX>& s, RowSum* sum, Bins* bins) {
   constexpr int VEC = Elem<Tin>::kVec, NW = BLOCK / kWave, LD = 4, CAP = ListLds<BLOCK, KMAX>::CAP;
@@ -607,7 +609,7 @@ __device__ __forceinline__ void write_top(const TopArgs& a, int64_t r, const Row
 
 // One workgroup per row. The read bounds it: 16,972 rows of 151,936 bfloat16
 // logits, 64 of each, 799 us (6.46 TB/s); 512 rows of 32,000 float32 logits, 20 of
-// each, 16.6 us, of which a chain of barriers about 5.
+// each, 16.6 us, of which a chain of barriers, which the loads wait for, about 5.
 template <typename Tin, int BLOCK, int KMAX>
 __global__ __launch_bounds__(BLOCK) void top_kernel(TopArgs a, int64_t first) {
   __shared__ ListLds<BLOCK, KMAX> s;
@@ -766,13 +768,16 @@ struct Candidate {
 // order: where m of them have a j-th candidate not below some score and m j is
 // at least k, no candidate below it is among the best. With j in powers of two
 // fewer than 2 k (1 + log2 k) are above the largest of these scores, however they
-// spread over the lists. Those that are left are cut by 256 bins of their scores
-// and counted against each other, or, where many are equal, selected from by
-// digits. SMALL: a request has at most kHeld candidates, which the threads read
-// at once and hold. A chain of a few reads and barriers bounds it: 5.1 us for one
-// request, 6.2 for 64. With the rows' kernel, k = 128, 64 beams of 151,936
-// bfloat16 logits whose scores differ take 77 us, alike 59. (Rows in eight parts:
-// 99 and 67; with three j beside k and no bins 1,234 and 51.)
+// spread over the lists; the bound itself keeps 20 bits of a float32 score's key
+// (11 of its fraction: 0.008 nats at -20, 0.5 at -2,000), and candidates that are
+// equal or in that band below it are looked at too. Of larger requests up to
+// kListed are cut by 256 bins of their scores; what is left is counted against each
+// other, or, where it is more than kCounted, selected from by digits. SMALL: a
+// request has at most kHeld candidates, which the threads read at once and hold. A
+// chain of a few reads and barriers bounds it: 5.1 us for one request, 6.2 for 64.
+// With the rows' kernel, k = 128, 64 beams of 151,936 bfloat16 logits whose scores
+// differ take 77 us, alike 59. (Rows in eight parts: 99 and 67; with three j beside
+// k and no bins 1,234 and 51.)
 constexpr int kCounted = 512, kHeld = 4 * kBeamBlock, kListed = 4096;
 
 template <bool SMALL>
@@ -1087,8 +1092,8 @@ int top_split(int64_t n_rows, int32_t V, pr_dtype dtype, int32_t k) {
 // Whether whole rows are taken by 512 threads: up to a few hundred, which are a
 // workgroup or two a compute unit, and lists of more than 64, which take more of
 // a compute unit's shared memory. 256 and 512 threads, us: k = 8, 512 rows of
-// 151,936 bfloat16 logits 33.5 and 31.8, 1,024 55.0 and 56.3, 2,048 99 and 104,
-// 17,904 794 and 890 (k = 64); 512 rows of 32,000 float32 logits 17.1 and 17.3,
+// 151,936 bfloat16 logits 33.5 and 31.8, 1,024 55.3 and 57.6, 2,048 101 and 108,
+// 16,972 806 and 865 (k = 64); 512 rows of 32,000 float32 logits 17.1 and 17.3,
 // 1,024 26.0 and 26.5. k = 200: 512 rows of 151,936 45.3 and 38.4, 2,048 130 and
 // 125, of 32,000 float32 65 and 55.
 bool wide_rows(int64_t n_rows) { return n_rows <= 512; }
