@@ -40,8 +40,8 @@ def row_logprobs(raw, dtype, T):
         return None, math.nan, flags
     u = decode_logits(raw, dtype).astype(np.float64) / float(np.float32(T))
     m = u.max()
-    lse = m + math.log(math.fsum(np.exp(u - m)))
-    return u - lse, lse, 0
+    rest = math.log(math.fsum(np.exp(u - m)))
+    return (u - m) - rest, m + rest, 0
 
 
 def top_logits(raw, dtype, T, k) -> dict:

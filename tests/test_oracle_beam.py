@@ -158,3 +158,12 @@ def test_beam_flags():
 def test_reorder():
     x = np.arange(12).reshape(6, 2)
     assert obeam.reorder(x, [[2, 0, 0], [1, -1, 3]]).tolist() == [[4, 5], [0, 1], [0, 1], [8, 9], [8, 9], [10, 11]]
+
+
+@pytest.mark.parametrize("shift", [0.0, 1e10, -1e25])
+def test_log_probs_of_rows_far_from_zero(shift):
+    """Log-probs do not depend on what a row's logits have in common (here all V are equal)."""
+    V = 400
+    lp, lse, flags = odist.row_logprobs(np.full(V, shift, np.float32), "f32", 1.0)
+    assert flags == 0 and np.abs(lp + np.log(V)).max() <= 1e-12
+    assert abs(lse - (float(np.float32(shift)) + np.log(V))) <= 1e-15 * (1.0 + abs(shift))
