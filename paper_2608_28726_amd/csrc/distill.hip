@@ -33,15 +33,17 @@ constexpr int kWindow = 1 << 16;  // vectors of a bit map
 static_assert(kStatsBlock >= kMaxTop && kGradBlock >= kMaxTop, "a thread for each entry");
 
 // What the gradient pass needs of a row: dz_v = k 2^fma(z_v, c, -A) outside the
-// entries, in_k 2^fma(z_v, c, -in_A) - q_k q_i in them, the products in 64 bits:
+// entries, in_k 2^fma(z_v, in_c, -in_A) - q_k q_i in them (either part relative to
+// its own largest logit), the products in 64 bits:
 // where student and teacher agree little is left of the two. All factors 0: the
 // gradient is zero and the row is not read.
 struct alignas(16) RowDistill {
-  float A, k, in_A, c;
+  float A, k, c, in_A;
   double in_k, q_k;
+  float in_c;
 
   __device__ __forceinline__ float in_entry(float z, double q) const {
-    return static_cast<float>(in_k * static_cast<double>(fast_exp2(fmaf(z, c, -in_A))) - q_k * q);
+    return static_cast<float>(in_k * static_cast<double>(fast_exp2(fmaf(z, in_c, -in_A))) - q_k * q);
   }
 };
 
@@ -57,10 +59,18 @@ struct SortedRows {
   int32_t parts;
 };
 
-// Sums over the entries.
+// Sums over the entries. u is taken relative to the largest of their logits
+// (entry_ref), so that what a row's logits have in common, however large, is no
+// part of the loss's terms.
 struct EntrySums {
   double Q, cross;  // sum q, sum q (log q - u)
 };
+__device__ __forceinline__ float entry_ref(const RowSum& in) { return in.m > -INFINITY ? in.m : 0.0f; }
+// cross relative to `top`, the largest logit of the entries of all parts, from one part's.
+__device__ __forceinline__ double cross_from(const EntrySums& e, const RowSum& in, float top, float T) {
+  if (in.m == -INFINITY || in.m == top) return e.cross;
+  return e.cross - e.Q * ((static_cast<double>(in.m) - static_cast<double>(top)) / static_cast<double>(T));
+}
 
 // What a row comes to: `in` are the tokens of the entries, `out` the others.
 struct RowLoss {
@@ -90,15 +100,17 @@ __device__ __forceinline__ double rest_q(const DistillArgs& a, const RowSum& out
 __device__ __forceinline__ RowDistill row_factors(const DistillArgs& a, const RowSum& in, const RowSum& out, double Q,
                                                   uint32_t flags, float T, float c, float w) {
   const float nan = __uint_as_float(0x7fc00000u);
-  if (flags) return RowDistill{0.0f, nan, 0.0f, 0.0f, nan, nan};
+  if (flags) return RowDistill{0.0f, nan, 0.0f, 0.0f, nan, nan, 0.0f};
   RowDistill g;
-  g.c = c;
-  g.A = out.S > 0.0f ? out.m * c : 0.0f;
-  g.in_A = in.S > 0.0f ? in.m * c : 0.0f;
-  const float A = fmaxf(in.S > 0.0f ? g.in_A : kNegSentinel, out.S > 0.0f ? g.A : kNegSentinel);
+  const RowRef ro = row_ref(out.S > 0.0f ? out.m : 0.0f, c), ri = row_ref(in.S > 0.0f ? in.m : 0.0f, c);
+  g.c = ro.c;
+  g.A = ro.A;
+  g.in_c = ri.c;
+  g.in_A = ri.A;
+  const float top = fmaxf(in.m, out.m);
   // Of each part: its scale beside the larger, and its sum so scaled.
-  const float si = in.S > 0.0f ? fast_exp2(fmaxf(g.in_A - A, -kBig)) : 0.0f;
-  const float so = out.S > 0.0f ? fast_exp2(fmaxf(g.A - A, -kBig)) : 0.0f;
+  const float si = in.S > 0.0f ? fast_exp2(ref_shift(in.m, top, c)) : 0.0f;
+  const float so = out.S > 0.0f ? fast_exp2(ref_shift(out.m, top, c)) : 0.0f;
   const double pi = static_cast<double>(in.S) * static_cast<double>(si);
   const double po = static_cast<double>(out.S) * static_cast<double>(so), all = pi + po;
   const double rq = rest_q(a, out, Q), scale = a.tail == PR_TAIL_RENORM ? (Q > 0.0 ? 1.0 / Q : 0.0) : 1.0;
@@ -110,13 +122,13 @@ __device__ __forceinline__ RowDistill row_factors(const DistillArgs& a, const Ro
   return g;
 }
 
-// log of a sum of exps, in 64 bits. S is relative to A = round(m c), whose
-// exact residual goes off its logarithm.
-__device__ __forceinline__ double log_sum(const RowSum& p, float T, float c) {
+// log of a sum of exps of u relative to the logit `from`, in 64 bits. S is relative
+// to the reference's A, whose exact residual goes off its logarithm.
+__device__ __forceinline__ double log_sum(const RowSum& p, float from, float T, float c) {
   if (!(p.S > 0.0f)) return -__longlong_as_double(0x7ff0000000000000ll);
-  const float A = p.m * c;
-  const double delta = static_cast<double>(fmaf(p.m, c, -A));
-  return static_cast<double>(p.m) / static_cast<double>(T) + log(static_cast<double>(p.S)) -
+  const RowRef ref = row_ref(p.m, c);
+  const double delta = static_cast<double>(fmaf(p.m, ref.c, -ref.A));
+  return (static_cast<double>(p.m) - static_cast<double>(from)) / static_cast<double>(T) + log(static_cast<double>(p.S)) -
          delta * 0.69314718055994530942;
 }
 
@@ -127,7 +139,8 @@ __device__ __forceinline__ void row_terms(const DistillArgs& a, const RowSum& in
     x.loss = x.mass = __longlong_as_double(0x7ff8000000000000ll);
     return;
   }
-  const double li = log_sum(in, T, c), lo = log_sum(out, T, c);
+  const float from = entry_ref(in);
+  const double li = log_sum(in, from, T, c), lo = log_sum(out, from, T, c);
   const double hi = fmax(li, lo), lse = hi + log1p(exp(fmin(li, lo) - hi)), rq = rest_q(a, out, e.Q);
   x.mass = exp(li - lse);
   x.loss = e.cross + e.Q * lse;
@@ -145,7 +158,7 @@ __device__ __forceinline__ RowLoss row_loss(const DistillArgs& a, const RowSum& 
 }
 
 __device__ __forceinline__ RowLoss masked_row() {
-  return RowLoss{0.0, 0.0, PR_FLAG_MASKED, RowDistill{0.0f, 0.0f, 0.0f, 0.0f, 0.0, 0.0}};
+  return RowLoss{0.0, 0.0, PR_FLAG_MASKED, RowDistill{0.0f, 0.0f, 0.0f, 0.0f, 0.0, 0.0, 0.0f}};
 }
 
 __device__ __forceinline__ void write_row(const DistillArgs& a, int64_t r, const RowLoss& x) {
@@ -335,7 +348,9 @@ __device__ DistillPart row_part(const DistillArgs& a, int64_t r, int g, int G, f
   // A probability of 0 adds nothing, whatever the student makes of its token.
   const double w = e.id >= 0 ? exp(static_cast<double>(e.logq)) : 0.0;
   EntrySums s{w, 0.0};
-  if (w > 0.0) s.cross = w * (static_cast<double>(e.logq) - static_cast<double>(z) / static_cast<double>(T));
+  if (w > 0.0)
+    s.cross = w * (static_cast<double>(e.logq) -
+                   (static_cast<double>(z) - static_cast<double>(entry_ref(p.in))) / static_cast<double>(T));
   p.entries = sum_entries<kStatsBlock>(s);
   p.bad = sh_bad;
   p.pad = 0;
@@ -376,10 +391,9 @@ __global__ __launch_bounds__(kStatsBlock) void distill_parts_kernel(DistillArgs 
 }
 
 __device__ __forceinline__ RowSum merge_two(const RowSum& p, const RowSum& q, float c) {
-  RowSum s{fmaxf(p.m, q.m), 0.0f};
-  if (p.m != -INFINITY || p.S != p.S) s.S += p.S * fast_exp2(fmaxf(p.m * c - s.m * c, -kBig));
-  if (q.m != -INFINITY || q.S != q.S) s.S += q.S * fast_exp2(fmaxf(q.m * c - s.m * c, -kBig));
-  return s;
+  const float m = fmaxf(p.m, q.m);
+  auto part = [&](const RowSum& e) { return e.m == -INFINITY ? e.S : e.S * fast_exp2(ref_shift(e.m, m, c)); };
+  return RowSum{m, part(p) + part(q)};
 }
 
 // A row's loss from its parts, by one thread,
@@ -391,10 +405,11 @@ __device__ __forceinline__ RowLoss loss_from_parts(const DistillArgs& a, int64_t
 #pragma unroll 4
   for (int g = 1; g < G; ++g) {
     const DistillPart p = part[r * G + g];
-    s.in = merge_two(s.in, p.in, c);
-    s.out = merge_two(s.out, p.out, c);
+    const RowSum in = merge_two(s.in, p.in, c);
+    s.entries.cross = cross_from(s.entries, s.in, in.m, T) + cross_from(p.entries, p.in, in.m, T);
     s.entries.Q += p.entries.Q;
-    s.entries.cross += p.entries.cross;
+    s.in = in;
+    s.out = merge_two(s.out, p.out, c);
     s.bad |= p.bad;
   }
   return row_loss(a, s.in, s.out, s.entries, s.bad, T, c, w);
@@ -410,8 +425,9 @@ __device__ __forceinline__ RowLoss loss_from_lanes(const DistillArgs& a, int64_t
   if (lane < G) p = part[r * G + lane];
   const uint32_t bad = (__any(p.bad & PR_FLAG_BAD_ID) ? PR_FLAG_BAD_ID : 0u) |
                        (__any(p.bad & PR_FLAG_NONFINITE) ? PR_FLAG_NONFINITE : 0u);
-  const EntrySums s{wave_sum_d(p.entries.Q), wave_sum_d(p.entries.cross)};
-  return row_loss(a, merge_lanes(p.in, c), merge_lanes(p.out, c), s, bad, T, c, w);
+  const RowSum in = merge_lanes(p.in, c);
+  const EntrySums s{wave_sum_d(p.entries.Q), wave_sum_d(cross_from(p.entries, p.in, in.m, T))};
+  return row_loss(a, in, merge_lanes(p.out, c), s, bad, T, c, w);
 }
 
 // All split rows' outputs, gradient factors (rd NULL: not wanted) and the loss,
@@ -592,7 +608,7 @@ __device__ __forceinline__ uint32_t group_slot(const Group& g, int32_t nvec) {
 // to 1,980 us; 512 rows of 32,000 float32 logits with 20 entries 24.7. With up to 64 entries
 // the extra wave keeps pace with the others; with 65 to 256 a lane has up to 4
 // and the row waits for them (4,096 rows of 151,936: 64 entries 534 us, 65 581,
-// 256 706), the more so as 9 to 34 of its registers are spilled to scratch. Two of the smaller workgroups then share a compute unit only where
+// 256 706), the more so as 12 to 41 of its registers are spilled to scratch. Two of the smaller workgroups then share a compute unit only where
 // the launch bound asks for it: 512 rows of 50,257 bfloat16 logits with 256
 // entries 34.6 us, without it 41.6.
 template <typename Tin, int DW, int NR, int KE>
@@ -706,9 +722,13 @@ __global__ __launch_bounds__((DW + 1) * kWave, 4) void distill_row_kernel(Distil
         // A probability of 0 adds nothing, whatever the student makes of its token.
         q_of[i] = e.id[i] >= 0 ? exp(static_cast<double>(e.logq[i])) : 0.0;
         sums.Q += q_of[i];
-        if (q_of[i] > 0.0)
-          sums.cross += q_of[i] * (static_cast<double>(e.logq[i]) - static_cast<double>(z[i]) / static_cast<double>(T));
       }
+      const float from = entry_ref(RowSum{in.mw, 0.0f});
+#pragma unroll
+      for (int i = 0; i < KE; ++i)
+        if (q_of[i] > 0.0)
+          sums.cross += q_of[i] * (static_cast<double>(e.logq[i]) -
+                                   (static_cast<double>(z[i]) - static_cast<double>(from)) / static_cast<double>(T));
       sums.Q = wave_sum_d(sums.Q);
       sums.cross = wave_sum_d(sums.cross);
       const RowSum sum_in{in.mw, wave_sum(in.s)}, own{out.mw, wave_sum(out.s)};

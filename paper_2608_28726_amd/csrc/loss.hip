@@ -14,8 +14,9 @@
 // the device (parts_kernel and what follows it). All are bound by memory.
 //
 // Exponents are in base 2: with c = log2(e) / T and the row's reference
-// A = round(m c), m its largest logit, x_v = fma(z_v, c, -A) and
-// S = sum 2^x_v, softmax(u)_v = 2^x_v / S. A row's sums over the vocabulary
+// A = round(m c), m its largest logit (row_ref, which gives c and A also where m
+// is far from zero), x_v = fma(z_v, c, -A) and S = sum 2^x_v,
+// softmax(u)_v = 2^x_v / S. A row's sums over the vocabulary
 // are float32 per lane, all terms positive: at most 160 of them in a held row;
 // elsewhere a lane takes V / (256 G) and compensates its sum. What follows per
 // row (l, the loss's term, the coefficient) and the sums over rows are in 64
@@ -40,15 +41,17 @@ struct alignas(16) RowGrad {
 
 struct RowValue {
   double l;
-  float A;
+  float A, c;      // of the row's reference
   uint32_t flags;  // 0 or the reasons why l is NaN
 };
 
-// l of a row from its sum of exps, in 64 bits. S is relative to A = round(m c),
-// whose exact residual goes off its logarithm.
+// l of a row from its sum of exps, in 64 bits. S is relative to A, the rounded
+// product of m and the reference's c, whose exact residual goes off its logarithm.
 __device__ __forceinline__ RowValue row_value(const RowSum& p, float T, float c, int32_t y, int32_t V, float zy) {
   RowValue v;
-  v.A = p.m * c;
+  const RowRef ref = row_ref(p.m, c);
+  v.A = ref.A;
+  v.c = ref.c;
   v.flags = 0;
   if (!temperature_ok(T)) v.flags |= PR_FLAG_BAD_TP;
   if (!(fabsf(p.S) < INFINITY) || p.m == INFINITY || p.m == -INFINITY) v.flags |= PR_FLAG_NONFINITE;
@@ -58,7 +61,7 @@ __device__ __forceinline__ RowValue row_value(const RowSum& p, float T, float c,
     v.l = __longlong_as_double(0x7ff8000000000000ll);
     return v;
   }
-  const double delta = static_cast<double>(fmaf(p.m, c, -v.A));
+  const double delta = static_cast<double>(fmaf(p.m, v.c, -v.A));
   const double lnS = log(static_cast<double>(p.S)) - delta * 0.69314718055994530942;
   v.l = (static_cast<double>(zy) - static_cast<double>(p.m)) / static_cast<double>(T) - lnS;
   return v;
@@ -96,8 +99,8 @@ struct PolicyRow {
   RowGrad grad;
 };
 
-__device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, int64_t r, const RowValue& v, float T, float c,
-                                                float S, float w) {
+__device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, int64_t r, const RowValue& v, float T, float S,
+                                                float w) {
   const double A = a.advantage[r], ratio = exp_wide(v.l - static_cast<double>(a.old_logprob[r]));
   const double free = ratio * A, held = fmin(fmax(ratio, a.clip_lo), a.clip_hi) * A;
   const bool clipped = free > held;
@@ -116,7 +119,7 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, int64_t r, 
   p.ratio = static_cast<float>(ratio);
   p.kl = static_cast<float>(kl);
   p.flags = v.flags | (!v.flags && clipped ? PR_FLAG_CLIPPED : 0u);
-  p.grad = row_grad(v.flags ? v.l : a.grad_scale * dl / static_cast<double>(T), v.l, v.A, c, S);
+  p.grad = row_grad(v.flags ? v.l : a.grad_scale * dl / static_cast<double>(T), v.l, v.A, v.c, S);
   return p;
 }
 
@@ -186,7 +189,7 @@ __global__ __launch_bounds__(kStatsBlock) void policy_stats_kernel(PolicyArgs a,
     const float zy = token_logit<Tin>(a.rows, r, y);
     const RowSum s = stretch_sum<Tin, kStatsBlock>(row_ptr<Tin>(a.rows, r), a.rows.V, 0, 1, c);
     if (threadIdx.x != 0) return;
-    p = policy_row(a, r, row_value(s, T, c, y, a.rows.V, zy), T, c, s.S, w);
+    p = policy_row(a, r, row_value(s, T, c, y, a.rows.V, zy), T, s.S, w);
   } else if (threadIdx.x != 0) {
     return;
   }
@@ -261,7 +264,7 @@ __device__ __forceinline__ PolicyRow policy_from_parts(const PolicyArgs& a, int6
   const float T = a.rows.temperature[r], c = scale_of(T), z = zy[r];
   const int32_t y = a.rows.ids[r];
   const RowSum s = merge_parts(part + r * a.G, a.G, c);
-  return policy_row(a, r, row_value(s, T, c, y, a.rows.V, z), T, c, s.S, w);
+  return policy_row(a, r, row_value(s, T, c, y, a.rows.V, z), T, s.S, w);
 }
 
 // All split rows' outputs, gradient factors (rg NULL: not wanted) and the
@@ -356,7 +359,7 @@ __global__ __launch_bounds__((DW + 1) * kWave) void policy_row_kernel(PolicyArgs
       if (lane < DW) part = sh_sum[lane];
       if (lane == DW) part = RowSum{own.mw, S};
       const RowSum sum = merge_lanes(part, c);
-      const PolicyRow p = policy_row(a, r, row_value(sum, T, c, y, V, zy), T, c, sum.S, w);
+      const PolicyRow p = policy_row(a, r, row_value(sum, T, c, y, V, zy), T, sum.S, w);
       const RowGrad q = p.grad;
       if (lane == 0) sh_q = q;
       __syncthreads();
@@ -485,7 +488,7 @@ __device__ __forceinline__ double preference_row(const PreferenceArgs& a, int64_
                                                  int32_t y, float zy, double* l, RowGrad* rg) {
   const RowValue v = row_value(p, T, c, y, a.rows.V, zy);
   l[r] = v.l;
-  rg[r] = RowGrad{v.A, c, p.S, T};
+  rg[r] = RowGrad{v.A, v.c, p.S, T};
   if (a.out.logprob) a.out.logprob[r] = static_cast<float>(v.l);
   if (a.out.flags) a.out.flags[r] = v.flags;
   return v.l;

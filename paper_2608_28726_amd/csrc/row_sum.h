@@ -9,23 +9,49 @@ namespace pr {
 using scan::head_elems;
 using scan::neg_inf_vec;
 
-// A row's sum of exps: its largest logit and, relative to round(m c), S.
+// A row's sum of exps: its largest logit and, relative to that one's reference, S.
 struct RowSum {
   float m, S;
 };
+
+// The reference that exps are relative to beside a largest logit m: they are
+// 2^fma(z, c, -A), with A = round(m c). The product's rounding is at most 2^-25 of
+// it, and from kFar on (logits of about 7e8 T: masks of -1e10, of a type's lowest
+// value) more than an exp can hold. There two logits that differ lie at least 64
+// binary orders apart, so that any scale tells them: c is the power of two that
+// takes m to 2^31 .. 2^32, and A exact.
+constexpr float kFar = 0x1p30f;
+struct RowRef {
+  float c, A;
+  bool far;
+};
+__device__ __forceinline__ RowRef row_ref(float m, float c) {
+  const float A = m * c;
+  if (fabsf(A) < kFar) return RowRef{c, A, false};
+  const uint32_t exponent = __float_as_uint(m) >> 23 & 255u;
+  const float p = __uint_as_float((31u + 254u - exponent) << 23);
+  return RowRef{p, m * p, true};
+}
+
+// Binary orders from m up to top (m <= top), as their references have them: at least -kBig.
+__device__ __forceinline__ float ref_shift(float m, float top, float c) {
+  const float A = top * c;
+  if (!(fabsf(A) < kFar)) return m == top ? 0.0f : -kBig;
+  return fmaxf(m * c - A, -kBig);
+}
 
 // A rejected temperature still gets a finite scale, so that what else is
 // wrong with a row is seen.
 __device__ __forceinline__ float scale_of(float T) { return temperature_ok(T) ? kLog2e / T : kLog2e; }
 
-// Running state of a lane: the wave's largest logit so far and the lane's sum
-// relative to round(mw c). Every lane of the wave calls add() together. LONG:
+// Running state of a lane: the wave's largest logit so far, its reference (cw, a)
+// and the lane's sum relative to that. Every lane of the wave calls add() together. LONG:
 // for rows of any length, the sum's roundings so far are held beside it
 // (Kahan's sum); without, a row of 4 million logits was off by 5.5e-6 of its
 // sum, and the error grows with the row.
 template <bool LONG>
 struct LaneSum {
-  float mw = -INFINITY, a = kNegSentinel, s = 0.0f, over = 0.0f;
+  float mw = -INFINITY, a = kNegSentinel, cw = 1.0f, s = 0.0f, over = 0.0f;
 
   template <int N>
   __device__ __forceinline__ void add(const float (&z)[N], float c) {
@@ -39,19 +65,18 @@ struct LaneSum {
   __device__ __forceinline__ void add_top(const float (&z)[N], float top, float c) {
     if (__any(top > mw)) {
       mw = fmaxf(mw, wave_max(top));
-      // A mask of the type's lowest value may overflow here: it adds nothing
-      // either way, and a row of nothing else is beyond the logits' bounds.
-      const float now = fmaxf(mw * c, kNegSentinel);
-      const float f = fast_exp2(fmaxf(a - now, -kBig));
+      const RowRef now = row_ref(mw, c);
+      const float f = now.far ? 0.0f : fast_exp2(fmaxf(a - now.A, -kBig));
       s *= f;
       if (LONG) over *= f;
-      a = now;
+      a = now.A;
+      cw = now.c;
     }
     float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
     for (int k = 0; k < N; k += 2) {
-      s0 += fast_exp2(fmaf(z[k], c, -a));
-      if (k + 1 < N) s1 += fast_exp2(fmaf(z[k + 1 < N ? k + 1 : k], c, -a));
+      s0 += fast_exp2(fmaf(z[k], cw, -a));
+      if (k + 1 < N) s1 += fast_exp2(fmaf(z[k + 1 < N ? k + 1 : k], cw, -a));
     }
     if (LONG) {
       const float x = (s0 + s1) - over, t = s + x;
@@ -67,13 +92,13 @@ struct LaneSum {
   }
 };
 
-// Merge of the states held by the lanes of a wave (each relative to
-// round(m c)); every lane gets the result. A state with m = -inf adds
+// Merge of the states held by the lanes of a wave (each relative to its own
+// largest logit's reference); every lane gets the result. A state with m = -inf adds
 // nothing but a NaN sum, which stays one.
 __device__ __forceinline__ RowSum merge_lanes(RowSum e, float c) {
   RowSum r;
   r.m = wave_max(e.m);
-  const float s = e.m == -INFINITY ? 0.0f : fast_exp2(fmaxf(e.m * c - r.m * c, -kBig));
+  const float s = e.m == -INFINITY ? 0.0f : fast_exp2(ref_shift(e.m, r.m, c));
   r.S = wave_sum(e.S * s);
   return r;
 }
@@ -126,7 +151,7 @@ __device__ __forceinline__ RowSum merge_parts(const RowSum* part, int G, float c
   for (int g = 0; g < kMaxSplit; ++g) s.m = fmaxf(s.m, e[g].m);
 #pragma unroll
   for (int g = 0; g < kMaxSplit; ++g)
-    s.S += e[g].S * (e[g].m == -INFINITY ? 0.0f : fast_exp2(fmaxf(e[g].m * c - s.m * c, -kBig)));
+    s.S += e[g].S * (e[g].m == -INFINITY ? 0.0f : fast_exp2(ref_shift(e[g].m, s.m, c)));
   return s;
 }
 

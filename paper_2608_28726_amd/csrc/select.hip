@@ -579,8 +579,8 @@ __device__ __forceinline__ RowNorm row_norm(const RowSum& p, float T) {
   if (!temperature_ok(T)) x.flags |= PR_FLAG_BAD_TP;
   if (!(fabsf(p.S) < INFINITY) || p.m == INFINITY || p.m == -INFINITY) x.flags |= PR_FLAG_NONFINITE;
   if (!x.flags && fabsf(p.m) > ldexpf(T, 100)) x.flags |= PR_FLAG_BAD_TP;
-  const float c = scale_of(T), A = p.m * c;
-  x.lnS = log(static_cast<double>(p.S)) - static_cast<double>(fmaf(p.m, c, -A)) * 0.69314718055994530942;
+  const RowRef ref = row_ref(p.m, scale_of(T));
+  x.lnS = log(static_cast<double>(p.S)) - static_cast<double>(fmaf(p.m, ref.c, -ref.A)) * 0.69314718055994530942;
   return x;
 }
 
