@@ -166,10 +166,9 @@ def token_features(raw_row, dtype: str, y: int, T: float, P: float | None = None
     if bad_id:
         logprob = math.nan
     elif rank <= k:
-        # log p(y) = (u_y - u_a) - log S_N: finite even where p(y) underflows
-        # float64, and exact however far u_a is; -inf only for a masked logit
-        # (u_y = -inf).
-        logprob = (u[y] - u[a]) - math.log(S_N)
+        # log p(y) = u_y - lse: finite even where p(y) underflows float64;
+        # -inf only for a masked logit (u_y = -inf).
+        logprob = u[y] - lse
     else:
         logprob = -math.inf
         flags |= FLAG_OUTSIDE_NUCLEUS
