@@ -70,10 +70,36 @@ struct Elem<uint16_t> {  // bfloat16 bit patterns
   }
 };
 
+// The reference that exps are relative to beside a largest logit m: they are
+// 2^fma(z, c, -A), with A = round(m c). The product's rounding is at most 2^-25 of
+// it, and from kFar on (logits of about 7e8 T: masks of -1e10, of a type's lowest
+// value) more than an exp can hold. There two logits that differ lie at least 64
+// binary orders apart, so that any scale tells them: c is the power of two that
+// takes m to 2^31 .. 2^32, and A exact.
+constexpr float kFar = 0x1p30f;
+struct RowRef {
+  float c, A;
+  bool far;
+};
+__device__ __forceinline__ RowRef row_ref(float m, float c) {
+  const float A = m * c;
+  if (fabsf(A) < kFar) return RowRef{c, A, false};
+  const uint32_t exponent = __float_as_uint(m) >> 23 & 255u;
+  const float p = __uint_as_float((31u + 254u - exponent) << 23);
+  return RowRef{p, m * p, true};
+}
+
+// Binary orders from m up to top (m <= top), as their references have them: at least -kBig.
+__device__ __forceinline__ float ref_shift(float m, float top, float c) {
+  const float A = top * c;
+  if (!(fabsf(A) < kFar)) return m == top ? 0.0f : -kBig;
+  return fmaxf(m * c - A, -kBig);
+}
+
 // Reduction state of a stretch of one row. S and E are relative to the
-// reference a = round(m * c) (c = log2(e) / T, the float32 product):
-// S = sum 2^x, E = sum 2^x * x with x = fma(z, c, -a). References are always
-// such rounded products and are compared by plain subtraction; the library is
+// reference (c, A) of its largest logit m, c = log2(e) / T:
+// S = sum 2^x, E = sum 2^x * x with x = fma(z, c, -A). References are
+// rounded products and are compared by plain subtraction (ref_shift); the library is
 // built with floating-point contraction off so that this stays so. t1/t1i/t2: largest value, its lowest index, second value.
 // cnt: tokens of the stretch that precede the sampled token in the order.
 struct Partial {
@@ -258,17 +284,15 @@ __device__ __forceinline__ void wave_top2(float& t1, int32_t& t1i, float& t2) {
   t2 = dpp::lane63(t2);
 }
 
-// Rescale factor from a stretch's reference a_l to the row reference A.
-// A stretch that saw no finite logit contributes nothing (but NaN sums stay
-// NaN); its reference may be a sentinel while A is -inf, so no exponent is
-// formed for it.
-__device__ __forceinline__ void rebase(bool no_finite, float a_l, float A, float& S, float& E) {
+// Moves a stretch's sums to the row's reference, d binary orders away
+// (ref_shift). A stretch that saw no finite logit contributes nothing (but NaN
+// sums stay NaN), and no exponent is formed for it.
+__device__ __forceinline__ void rebase(bool no_finite, float d, float& S, float& E) {
   if (no_finite) {
     S *= 0.0f;
     E *= 0.0f;
     return;
   }
-  const float d = fmaxf(a_l - A, -kBig);
   const float s = fast_exp2(d);
   E = s * E + (s * d) * S;
   S = s * S;

@@ -61,14 +61,14 @@ __device__ __forceinline__ void finish_drawn(const RowArgs& a, int64_t r, const 
     // The token drawn for the row; its rank is not counted (that needs its
     // value before the pass), and is written as -1, "not available".
     __shared__ sample::Shared ssh;
-    __shared__ float sh_ref;
+    __shared__ float sh_m;
     __shared__ uint32_t sh_def;
     if (threadIdx.x == 0) {  // the merged state p is valid in the first wave
-      sh_ref = p.m * cx.c;
+      sh_m = p.m;
       sh_def = (row_flags(a, r, p, cx.T) & (PR_FLAG_NONFINITE | PR_FLAG_BAD_TP)) == 0 ? 1u : 0u;
     }
     __syncthreads();
-    sample::pick<Tin, BLOCK, U>(row, nvec, cx, L, hook.a, sh_ref, sh_def != 0, ssh, cf.y, cf.zy);
+    sample::pick<Tin, BLOCK, U>(row, nvec, cx, L, hook.a, sh_m, sh_def != 0, ssh, cf.y, cf.zy);
   }
   if constexpr (SEQ) {
     __shared__ topk::Store<BLOCK> ts;
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(kWave) void lane_scan_kernel(RowArgs a) {
   auto put = [&](uint32_t x) { lane_word<SEQ, SAMPLE>(a, r, k++)[lane0] = x; };
   if constexpr (SAMPLE) {
     put(__float_as_uint(L.S0 + L.S1));
-    put(__float_as_uint(L.a));
+    put(__float_as_uint(L.mw));
     put(static_cast<uint32_t>(hook.a.win));
   }
   if constexpr (SEQ) {
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(kLaneBlock) void lane_finish_kernel(RowArgs a) {
   auto get = [&]() { return lane_word<SEQ, SAMPLE>(a, r, k++)[threadIdx.x]; };
   if constexpr (SAMPLE) {
     L.S0 = __uint_as_float(get());
-    L.a = __uint_as_float(get());
+    L.mw = __uint_as_float(get());
     hook.a.win = static_cast<int32_t>(get());
   }
   if constexpr (SEQ) {
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(kWave) void row_merge_kernel(RowArgs a) {
   cx.thr_lo = 0.0f;
   Partial p;
   p.m = wave_max(q.m);
-  rebase(q.m == -INFINITY, q.m * cx.c, p.m * cx.c, q.S, q.E);
+  rebase(q.m == -INFINITY, ref_shift(q.m, p.m, cx.c), q.S, q.E);
   p.S = wave_sum(q.S);
   p.E = wave_sum(q.E);
   wave_top2(q.t1, q.t1i, q.t2);

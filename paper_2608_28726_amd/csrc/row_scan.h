@@ -10,7 +10,7 @@ namespace scan {
 
 struct Lane {
   float mw;        // running max of the wave's logits (wave-uniform in the vector loop)
-  float a;         // reference of S and E: mw * c, or kNegSentinel
+  float a, c;      // reference of S and E (row_ref of mw), or kNegSentinel and any scale
   float S0, S1;    // two accumulators of sum 2^x (alternating elements)
   float E0, E1;    // two accumulators of sum 2^x * x
   float t1, t2;    // largest and second largest maximum of the lane's buckets (a
@@ -34,6 +34,7 @@ struct RowCtx {
 __device__ __forceinline__ void lane_init(Lane& L) {
   L.mw = -INFINITY;
   L.a = kNegSentinel;
+  L.c = 1.0f;
   L.S0 = L.S1 = L.E0 = L.E1 = 0.0f;
   L.t1 = -INFINITY;
   L.t2 = -INFINITY;
@@ -42,18 +43,19 @@ __device__ __forceinline__ void lane_init(Lane& L) {
   L.cnt = 0;
 }
 
-// Moves the lane's reference up to a_new = m_new * c (m_new >= the old max).
+// Moves the lane's reference up to that of m_new (>= the old max).
 __device__ __forceinline__ void lane_rescale(Lane& L, float m_new, float c) {
   L.mw = m_new;
-  const float a_new = m_new * c;
-  const float d = fmaxf(L.a - a_new, -kBig);
+  const RowRef now = row_ref(m_new, c);
+  const float d = now.far ? -kBig : fmaxf(L.a - now.A, -kBig);
   const float s = fast_exp2(d);
   const float sd = s * d;
   L.E0 = fmaf(sd, L.S0, s * L.E0);
   L.E1 = fmaf(sd, L.S1, s * L.E1);
   L.S0 *= s;
   L.S1 *= s;
-  L.a = a_new;
+  L.a = now.A;
+  L.c = now.c;
 }
 
 // Per-element hook of the scan: step() is called once per step with the
@@ -134,8 +136,8 @@ __device__ __forceinline__ void consume(const vec4u* v, int64_t i, const RowCtx&
     float s0 = 0.0f, s1 = 0.0f, q0 = 0.0f, q1 = 0.0f;
 #pragma unroll
     for (int k = 0; k < NV * VEC; k += 2) {
-      const float x0 = fmaf(z[k], cx.c, na);
-      const float x1 = fmaf(z[k + 1], cx.c, na);
+      const float x0 = fmaf(z[k], L.c, na);
+      const float x1 = fmaf(z[k + 1], L.c, na);
       const float e0 = fast_exp2(x0);
       const float e1 = fast_exp2(x1);
       ev[k] = e0;
@@ -196,7 +198,7 @@ __device__ __forceinline__ void consume_scalar(float z, int64_t idx, const RowCt
   if (cx.y >= 0) L.cnt += (z > cx.zy || (z == cx.zy && idx < cx.y)) ? 1u : 0u;
   if constexpr (SOFT) {
     if (z > L.mw) lane_rescale(L, z, cx.c);
-    const float x = fmaf(z, cx.c, -L.a);
+    const float x = fmaf(z, L.c, -L.a);
     const float e = fast_exp2(x);
     L.S0 += e;
     L.E0 = fmaf(e, fmaxf(x, -kBig), L.E0);
@@ -221,7 +223,7 @@ __device__ __forceinline__ Partial wave_partial(Lane& L, float c) {
   Partial q;
   q.m = wave_max(L.t1);
   float S = L.S0 + L.S1, E = L.E0 + L.E1;
-  rebase(L.a == kNegSentinel, L.a, q.m * c, S, E);
+  rebase(L.a == kNegSentinel, ref_shift(L.mw, q.m, c), S, E);
   q.S = wave_sum(S);
   q.E = wave_sum(E);
   q.t1 = L.t1;
@@ -247,7 +249,7 @@ __device__ __forceinline__ Partial merge_waves(Partial e, int n, float c) {
   }
   Partial p;
   p.m = wave_max(e.m);
-  rebase(e.m == -INFINITY, e.m * c, p.m * c, e.S, e.E);
+  rebase(e.m == -INFINITY, ref_shift(e.m, p.m, c), e.S, e.E);
   p.S = wave_sum(e.S);
   p.E = wave_sum(e.E);
   wave_top2(e.t1, e.t1i, e.t2);
@@ -568,8 +570,9 @@ __device__ __forceinline__ uint32_t finalize_row(const RowArgs& a, int64_t r, co
       // S and E are relative to A = round(M * c). The exact residual
       // delta = M * c - A moves them to the exact reference M * c, so that
       // the largest logit contributes exactly 2^0 (matters for large |M|/T).
-      const float A = p.m * cx.c;
-      const float delta = fmaf(p.m, cx.c, -A);
+      const RowRef ref = row_ref(p.m, cx.c);
+      const float A = ref.A;
+      const float delta = fmaf(p.m, ref.c, -A);
       const float sc = fast_exp2(-delta);
       const float S = p.S * sc;
       const float E = sc * fmaf(-delta, p.S, p.E);
@@ -580,7 +583,9 @@ __device__ __forceinline__ uint32_t finalize_row(const RowArgs& a, int64_t r, co
       cutoff = a.V;
       if (cx.y >= 0) {
         const float xy = fmaf(cx.zy, cx.c, -A) - delta;
-        logprob = kLn2 * xy - lnS;
+        // (Of a far reference the scale is not the temperature's.)
+        logprob = (ref.far ? static_cast<float>((static_cast<double>(cx.zy) - static_cast<double>(p.m)) / static_cast<double>(T))
+                           : kLn2 * xy) - lnS;
       }
     }
   }

@@ -14,32 +14,6 @@ struct RowSum {
   float m, S;
 };
 
-// The reference that exps are relative to beside a largest logit m: they are
-// 2^fma(z, c, -A), with A = round(m c). The product's rounding is at most 2^-25 of
-// it, and from kFar on (logits of about 7e8 T: masks of -1e10, of a type's lowest
-// value) more than an exp can hold. There two logits that differ lie at least 64
-// binary orders apart, so that any scale tells them: c is the power of two that
-// takes m to 2^31 .. 2^32, and A exact.
-constexpr float kFar = 0x1p30f;
-struct RowRef {
-  float c, A;
-  bool far;
-};
-__device__ __forceinline__ RowRef row_ref(float m, float c) {
-  const float A = m * c;
-  if (fabsf(A) < kFar) return RowRef{c, A, false};
-  const uint32_t exponent = __float_as_uint(m) >> 23 & 255u;
-  const float p = __uint_as_float((31u + 254u - exponent) << 23);
-  return RowRef{p, m * p, true};
-}
-
-// Binary orders from m up to top (m <= top), as their references have them: at least -kBig.
-__device__ __forceinline__ float ref_shift(float m, float top, float c) {
-  const float A = top * c;
-  if (!(fabsf(A) < kFar)) return m == top ? 0.0f : -kBig;
-  return fmaxf(m * c - A, -kBig);
-}
-
 // A rejected temperature still gets a finite scale, so that what else is
 // wrong with a row is seen.
 __device__ __forceinline__ float scale_of(float T) { return temperature_ok(T) ? kLog2e / T : kLog2e; }

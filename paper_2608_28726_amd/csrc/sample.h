@@ -94,7 +94,8 @@ struct Hook {
   }
   __device__ __forceinline__ void rebase(const scan::Lane& L) {
     if (L.a != ar) {
-      const float f = ar == kNegSentinel ? 0.0f : fast_exp2(ar - L.a);
+      // (Beside a far largest logit nothing before it counts.)
+      const float f = ar == kNegSentinel || !(fabsf(L.a) < kFar) ? 0.0f : fast_exp2(ar - L.a);
       Wb *= f;
       Wl *= f;
       ar = L.a;
@@ -152,19 +153,19 @@ struct Shared {
 };
 
 // The row's token, after the scan: a lane by inverse CDF over the lanes'
-// totals (relative to A = M * c), then a token of that lane's bucket.
+// totals (relative to the row's largest logit M), then a token of that lane's bucket.
 // Every thread of the block calls this and gets the same (y, zy); y = -1
 // when the row's distribution is undefined.
 template <typename Tin, int BLOCK, int U>
 __device__ __forceinline__ void pick(const void* row, int64_t nvec, const scan::RowCtx& cx, const scan::Lane& L, const Hook& hk,
-                     float A, bool defined, Shared& sh, int32_t& y, float& zy) {
+                     float M, bool defined, Shared& sh, int32_t& y, float& zy) {
   constexpr int VEC = Elem<Tin>::kVec;
   constexpr int NW = BLOCK / kWave;
   const int t = threadIdx.x;
   const int w = t / kWave;
   const int lane = t % kWave;
   float W = 0.0f;
-  if (defined && L.a != kNegSentinel && hk.win != kNone) W = (L.S0 + L.S1) * fast_exp2(L.a - A);
+  if (defined && L.mw > -INFINITY && hk.win != kNone) W = (L.S0 + L.S1) * fast_exp2(ref_shift(L.mw, M, cx.c));
   float incl = W;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
@@ -215,12 +216,13 @@ __device__ __forceinline__ void pick(const void* row, int64_t nvec, const scan::
       const vec4u v = (lane < NB && j < nvec) ? vp[j] : scan::neg_inf_vec<Tin>();
       float z[VEC];
       Elem<Tin>::unpack(v, z);
+      const RowRef ref = row_ref(M, cx.c);
       float ev[VEC];
       float part = 0.0f, zm = z[0];
       int km = 0;
 #pragma unroll
       for (int k = 0; k < VEC; ++k) {
-        ev[k] = fast_exp2(fmaf(z[k], cx.c, -A));
+        ev[k] = fast_exp2(fmaf(z[k], ref.c, -ref.A));
         part += ev[k];
         if (z[k] > zm) {
           zm = z[k];

@@ -405,12 +405,13 @@ __device__ void select_topk(const void* row, int32_t V, int64_t h, int64_t vb, i
 
 // -sum over the j largest logits top[0..j) of p log p with
 // p = 2^x / S, x = (z - M) * log2(e) / T in the row state's reference
-// (A = round(M c), delta = M c - A, S relative to M c): the float32 path of
+// (A = round(M c), delta = M c - A, S relative to M c; where M is far, x is 0 or so
+// low that p is 0): the float32 path of
 // a row without a nucleus. Called by the 64 lanes of one wave (j <= 64);
 // every lane gets the sum.
 __device__ __forceinline__ float topk_entropy_f32(const float* top, int j, float M, float c, float S_raw) {
-  const float A = M * c;
-  const float delta = fmaf(M, c, -A);
+  const RowRef ref = row_ref(M, c);
+  const float delta = fmaf(M, ref.c, -ref.A);
   const float S = S_raw * fast_exp2(-delta);
   const float lnS = ln_sum(S);
   float term = 0.0f;
@@ -418,7 +419,7 @@ __device__ __forceinline__ float topk_entropy_f32(const float* top, int j, float
   if (l < j) {
     const float z = top[l];
     if (z != -INFINITY) {
-      const float x = fmaf(z, c, -A) - delta;
+      const float x = fmaxf(fmaf(z, ref.c, -ref.A) - delta, -kBig);  // (a mask's product may overflow)
       const float p = fast_exp2(x) / S;
       term = p * (kLn2 * x - lnS);
     }
