@@ -145,6 +145,7 @@ size_t pr_token_features_workspace(pr_dtype dtype, int64_t n_rows, int32_t vocab
  *                truncation off; 0 < P < 1 keeps the shortest prefix of the
  *                order whose mass reaches P of the total. With top_p, vocab
  *                must be below 2^24 (PR_ERR_UNSUPPORTED otherwise).
+ *   n_rows       below 2^24, with top_p below 2^23 (PR_ERR_UNSUPPORTED otherwise).
  *   out          host pointer to a struct of device output arrays, all
  *                required.
  *   workspace    device scratch of at least
@@ -342,7 +343,8 @@ pr_status pr_verifier_head(const float* X, int64_t n_rows, const int32_t* offset
  *             and margin are read.
  *   offsets   int32 [n_req + 1], device. Request i owns rows
  *             offsets[i] .. offsets[i+1]-1. Precondition (not checked here,
- *             see pr_validate_offsets): offsets[0] >= 0, non-decreasing.
+ *             see pr_validate_offsets): offsets[0] >= 0, non-decreasing. n_req
+ *             must be below 2^24 (PR_ERR_UNSUPPORTED otherwise).
  *   params    host pointer, or NULL for the defaults.
  *   out       host pointer to a struct of device output arrays.
  */

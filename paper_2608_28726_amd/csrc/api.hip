@@ -70,6 +70,11 @@ pr_status check_rows(const void* logits, pr_dtype dtype, int64_t n_rows, int32_t
   return PR_OK;
 }
 
+// Whether the one launch of the row kernels takes n rows, or that of the request
+// kernels n requests: it has fewer than 2^32 threads (more are cut off without an
+// error), 256 a row or request, 512 a row with top-p.
+bool launch_fits(int64_t n, bool top_p = false) { return n < (int64_t{1} << (top_p ? 23 : 24)); }
+
 pr_status hip_status(hipError_t e) {
   if (e == hipSuccess) return PR_OK;
   if (e == hipErrorOutOfMemory) return PR_ERR_NO_MEMORY;
@@ -250,7 +255,7 @@ pr_status pr_token_features_ws(const void* logits, pr_dtype dtype, int64_t n_row
   a.temperature = temperature;
   a.top_p = top_p;
   a.out = *out;
-  if (top_p && vocab >= kTopPMaxVocab) return PR_ERR_UNSUPPORTED;
+  if ((top_p && vocab >= kTopPMaxVocab) || !launch_fits(n_rows, top_p)) return PR_ERR_UNSUPPORTED;
   if (top_p) return hip_status(launch_topp(a, dtype, workspace, workspace_bytes, as_stream(stream)));
   a.G = row_split(n_rows, vocab, dtype);
   a.ws = static_cast<Partial*>(workspace);
@@ -313,7 +318,7 @@ pr_status pr_feature_sequence_ws(const void* logits, pr_dtype dtype, int64_t n_r
   a.offsets = offsets;
   a.n_req = n_req;
   a.top_k = top_k;
-  if (top_p && vocab >= kTopPMaxVocab) return PR_ERR_UNSUPPORTED;
+  if ((top_p && vocab >= kTopPMaxVocab) || !launch_fits(n_rows, top_p)) return PR_ERR_UNSUPPORTED;
   if (workspace && !aligned(workspace, 16)) return PR_ERR_INVALID_ARG;
   if (top_p) return hip_status(launch_topp(a, dtype, workspace, workspace_bytes, as_stream(stream)));
   const size_t need = lane_workspace_bytes(n_rows, vocab, dtype, true, false);
@@ -343,7 +348,7 @@ pr_status pr_sample_features_ws(const void* logits, pr_dtype dtype, int64_t n_ro
                                 void* stream) {
   if (dtype != PR_F32 && dtype != PR_BF16) return PR_ERR_INVALID_ARG;
   if (n_rows < 0 || vocab < 2 || row_stride < vocab) return PR_ERR_INVALID_ARG;
-  if (n_rows > (int64_t{1} << 26)) return PR_ERR_UNSUPPORTED;
+  if (!launch_fits(n_rows)) return PR_ERR_UNSUPPORTED;
   if (features && !features_complete(features)) return PR_ERR_INVALID_ARG;
   if (X && (top_k < 1 || top_k > PR_MAX_TOP_K || n_req < 0)) return PR_ERR_INVALID_ARG;
   if (n_rows == 0) return PR_OK;
@@ -412,6 +417,7 @@ pr_status pr_request_aggregate(const pr_token_features_t* feats, const int32_t* 
     return PR_ERR_INVALID_ARG;
   const pr_agg_params p = params ? *params : default_params();
   if (!params_ok(p)) return PR_ERR_INVALID_ARG;
+  if (!launch_fits(n_req)) return PR_ERR_UNSUPPORTED;
   return hip_status(launch_aggregate(*feats, offsets, n_req, p, *out, as_stream(stream)));
 }
 
@@ -531,7 +537,7 @@ pr_status pr_stream_step_ws(pr_stream* state, const void* logits, pr_dtype dtype
   if (st != PR_OK) return st;
   if (n_active > state->dev.max_slots) return PR_ERR_INVALID_ARG;
   if (n_active > 0 && !slot_ids) return PR_ERR_INVALID_ARG;
-  if (top_p && vocab >= kTopPMaxVocab) return PR_ERR_UNSUPPORTED;
+  if ((top_p && vocab >= kTopPMaxVocab) || !launch_fits(n_active, top_p)) return PR_ERR_UNSUPPORTED;
   if (out && !features_complete(out)) return PR_ERR_INVALID_ARG;
   if (workspace && !aligned(workspace, 16)) return PR_ERR_INVALID_ARG;
   if (n_active == 0) return PR_OK;
@@ -559,6 +565,7 @@ pr_status pr_stream_finish(pr_stream* state, const int32_t* slots, int32_t n, fl
   if (!state || n < 0) return PR_ERR_INVALID_ARG;
   if (n == 0) return PR_OK;
   if (!slots) return PR_ERR_INVALID_ARG;
+  if (!launch_fits(n)) return PR_ERR_UNSUPPORTED;
   pr_request_agg_t o{};
   if (out) o = *out;
   return hip_status(
