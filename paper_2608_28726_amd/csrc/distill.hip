@@ -66,10 +66,11 @@ struct EntrySums {
   double Q, cross;  // sum q, sum q (log q - u)
 };
 __device__ __forceinline__ float entry_ref(const RowSum& in) { return in.m > -INFINITY ? in.m : 0.0f; }
-// cross relative to `top`, the largest logit of the entries of all parts, from one part's.
-__device__ __forceinline__ double cross_from(const EntrySums& e, const RowSum& in, float top, float T) {
+// cross relative to `top`, the largest logit of the entries of all parts, from one
+// part's. over_T: 1 / T.
+__device__ __forceinline__ double cross_from(const EntrySums& e, const RowSum& in, float top, double over_T) {
   if (in.m == -INFINITY || in.m == top) return e.cross;
-  return e.cross - e.Q * ((static_cast<double>(in.m) - static_cast<double>(top)) / static_cast<double>(T));
+  return e.cross - e.Q * ((static_cast<double>(in.m) - static_cast<double>(top)) * over_T);
 }
 
 // What a row comes to: `in` are the tokens of the entries, `out` the others.
@@ -390,29 +391,33 @@ __global__ __launch_bounds__(kStatsBlock) void distill_parts_kernel(DistillArgs 
   if (threadIdx.x == 0) part[blockIdx.x] = p;
 }
 
-__device__ __forceinline__ RowSum merge_two(const RowSum& p, const RowSum& q, float c) {
-  const float m = fmaxf(p.m, q.m);
-  auto part = [&](const RowSum& e) { return e.m == -INFINITY ? e.S : e.S * fast_exp2(ref_shift(e.m, m, c)); };
-  return RowSum{m, part(p) + part(q)};
-}
-
 // A row's loss from its parts, by one thread,
 __device__ __forceinline__ RowLoss loss_from_parts(const DistillArgs& a, int64_t r, const DistillPart* part, int G) {
   const float w = a.rows.weight[r];
   if (w == 0.0f) return masked_row();
   const float T = a.rows.temperature[r], c = scale_of(T);
-  DistillPart s = part[r * G];
+  const double over_T = 1.0 / static_cast<double>(T);
+  RowSum in{-INFINITY, 0.0f}, out{-INFINITY, 0.0f};
 #pragma unroll 4
-  for (int g = 1; g < G; ++g) {
-    const DistillPart p = part[r * G + g];
-    const RowSum in = merge_two(s.in, p.in, c);
-    s.entries.cross = cross_from(s.entries, s.in, in.m, T) + cross_from(p.entries, p.in, in.m, T);
-    s.entries.Q += p.entries.Q;
-    s.in = in;
-    s.out = merge_two(s.out, p.out, c);
-    s.bad |= p.bad;
+  for (int g = 0; g < G; ++g) {
+    in.m = fmaxf(in.m, part[r * G + g].in.m);
+    out.m = fmaxf(out.m, part[r * G + g].out.m);
   }
-  return row_loss(a, s.in, s.out, s.entries, s.bad, T, c, w);
+  EntrySums e{0.0, 0.0};
+  uint32_t bad = 0;
+  auto add = [&](RowSum& s, const RowSum& p) {
+    s.S += p.m == -INFINITY ? p.S : p.S * fast_exp2(ref_shift(p.m, s.m, c));
+  };
+#pragma unroll 4
+  for (int g = 0; g < G; ++g) {
+    const DistillPart p = part[r * G + g];
+    add(in, p.in);
+    add(out, p.out);
+    e.Q += p.entries.Q;
+    e.cross += cross_from(p.entries, p.in, in.m, over_T);
+    bad |= p.bad;
+  }
+  return row_loss(a, in, out, e, bad, T, c, w);
 }
 
 // and by every wave of a workgroup, a lane a part.
@@ -426,7 +431,7 @@ __device__ __forceinline__ RowLoss loss_from_lanes(const DistillArgs& a, int64_t
   const uint32_t bad = (__any(p.bad & PR_FLAG_BAD_ID) ? PR_FLAG_BAD_ID : 0u) |
                        (__any(p.bad & PR_FLAG_NONFINITE) ? PR_FLAG_NONFINITE : 0u);
   const RowSum in = merge_lanes(p.in, c);
-  const EntrySums s{wave_sum_d(p.entries.Q), wave_sum_d(cross_from(p.entries, p.in, in.m, T))};
+  const EntrySums s{wave_sum_d(p.entries.Q), wave_sum_d(cross_from(p.entries, p.in, in.m, 1.0 / static_cast<double>(T)))};
   return row_loss(a, in, merge_lanes(p.out, c), s, bad, T, c, w);
 }
 

@@ -123,9 +123,15 @@ __device__ __forceinline__ RowSum merge_parts(const RowSum* part, int G, float c
   for (int g = 0; g < kMaxSplit; ++g) e[g] = g < G ? part[g] : RowSum{-INFINITY, 0.0f};
 #pragma unroll
   for (int g = 0; g < kMaxSplit; ++g) s.m = fmaxf(s.m, e[g].m);
+  const float A = s.m * c;
+  if (fabsf(A) < kFar) {
 #pragma unroll
-  for (int g = 0; g < kMaxSplit; ++g)
-    s.S += e[g].S * (e[g].m == -INFINITY ? 0.0f : fast_exp2(ref_shift(e[g].m, s.m, c)));
+    for (int g = 0; g < kMaxSplit; ++g)
+      s.S += e[g].S * (e[g].m == -INFINITY ? 0.0f : fast_exp2(fmaxf(e[g].m * c - A, -kBig)));
+  } else {  // as ref_shift: equal ones count alike
+#pragma unroll
+    for (int g = 0; g < kMaxSplit; ++g) s.S += e[g].m == s.m || e[g].S != e[g].S ? e[g].S : 0.0f;
+  }
   return s;
 }
 
