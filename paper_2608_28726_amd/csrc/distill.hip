@@ -34,9 +34,9 @@ static_assert(kStatsBlock >= kMaxTop && kGradBlock >= kMaxTop, "a thread for eac
 
 // What the gradient pass needs of a row: dz_v = k 2^fma(z_v, c, -A) outside the
 // entries, in_k 2^fma(z_v, in_c, -in_A) - q_k q_i in them (either part relative to
-// its own largest logit), the products in 64 bits:
-// where student and teacher agree little is left of the two. All factors 0: the
-// gradient is zero and the row is not read.
+// its own largest logit), the products in 64 bits: where student and teacher agree
+// little is left of the two. All factors 0: the gradient is zero and the row is not
+// read.
 struct alignas(16) RowDistill {
   float A, k, c, in_A;
   double in_k, q_k;
@@ -613,9 +613,10 @@ __device__ __forceinline__ uint32_t group_slot(const Group& g, int32_t nvec) {
 // to 1,980 us; 512 rows of 32,000 float32 logits with 20 entries 24.7. With up to 64 entries
 // the extra wave keeps pace with the others; with 65 to 256 a lane has up to 4
 // and the row waits for them (4,096 rows of 151,936: 64 entries 534 us, 65 581,
-// 256 706), the more so as 12 to 41 of its registers are spilled to scratch. Two of the smaller workgroups then share a compute unit only where
-// the launch bound asks for it: 512 rows of 50,257 bfloat16 logits with 256
-// entries 34.6 us, without it 41.6.
+// 256 706), the more so as 12 to 41 of its registers are spilled to scratch. Two of
+// the smaller workgroups then share a compute unit only where the launch bound asks
+// for it: 512 rows of 50,257 bfloat16 logits with 256 entries 34.6 us, without it
+// 41.6.
 template <typename Tin, int DW, int NR, int KE>
 __global__ __launch_bounds__((DW + 1) * kWave, 4) void distill_row_kernel(DistillArgs a, double* term) {
   constexpr int VEC = Elem<Tin>::kVec, NT = DW * kWave, MOST = NR * NT;  // vectors

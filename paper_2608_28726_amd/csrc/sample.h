@@ -64,7 +64,7 @@ __device__ __forceinline__ void threefry2x32(uint32_t c0, uint32_t c1, uint32_t 
 __device__ __forceinline__ float unit(uint32_t w) { return static_cast<float>(w >> 8) * 0x1p-24f; }
 
 // Per-lane reservoir over the lane's buckets (a scan hook). Every mass is
-// relative to the lane's reference L.a; when the reference moves up, the
+// relative to the lane's reference, that of L.mw; when it moves up, the
 // stored totals are moved with it. The key, the row and the step count are
 // the same in every lane of a wave (the vector loop's trip counts are
 // wave-uniform), so they stay in scalar registers.
@@ -75,7 +75,7 @@ struct Hook {
   int32_t s;          // vector steps taken (bucket s / kBucketSteps)
   float Wb;           // lane total before the current bucket
   float Wl;           // lane total after the last element taken in
-  float ar;           // reference of Wb and Wl
+  float mr;           // largest logit that Wb and Wl are relative to
   int32_t bfirst;     // first vector index of the current bucket
   uint32_t spare;     // second random word of the current pair of buckets
   int32_t win;        // chosen bucket: its first vector index (>= 0), -(element + 2) for a scalar, or kNone
@@ -87,18 +87,18 @@ struct Hook {
     row = static_cast<uint32_t>(r);
     s = 0;
     Wb = Wl = 0.0f;
-    ar = kNegSentinel;
+    mr = -INFINITY;
     bfirst = 0;
     spare = 0;
     win = kNone;
   }
   __device__ __forceinline__ void rebase(const scan::Lane& L) {
-    if (L.a != ar) {
+    if (L.mw != mr) {
       // (Beside a far largest logit nothing before it counts.)
-      const float f = ar == kNegSentinel || !(fabsf(L.a) < kFar) ? 0.0f : fast_exp2(ar - L.a);
+      const float f = fabsf(L.a) < kFar ? fast_exp2(mr * L.c - L.a) : 0.0f;
       Wb *= f;
       Wl *= f;
-      ar = L.a;
+      mr = L.mw;
     }
   }
   // Keeps bucket b (mass Wl - Wb) with probability (Wl - Wb) / Wl. Buckets

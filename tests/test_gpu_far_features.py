@@ -129,3 +129,20 @@ def test_streamed_tokens(V, dtype, max_len):
     compare_features({k: v.cpu().numpy() for k, v in f.items()}, o)
     assert_floats("score", score.cpu().numpy(), o["maxprob"])  # the mean of maxprob, which the second step leaves
     state.close()
+
+
+@pytest.mark.parametrize("n", [6, 300, 2100])
+@pytest.mark.parametrize("low,high", [(3 * 2.0 ** 39, 3 * 2.0 ** 40), (-3 * 2.0 ** 41, -3 * 2.0 ** 40), (-3e38, -1e10), (1e9, 3e12)])
+def test_the_one_token_that_is_larger_is_drawn(n, low, high):
+    """Rows of one far value but for a larger one, which has all the probability (pairs a power of two apart among them,
+    whose references look alike)."""
+    V = 33000
+    rng = np.random.default_rng(n)
+    at = rng.integers(0, V, n)
+    at[:3] = 0, V // 2, V - 1
+    z = torch.full((n, V), low, device="cuda")
+    z[torch.arange(n), cuda(at)] = high
+    ids, f, _ = pr.sample_features(z, torch.ones(n, device="cuda"), 9)
+    torch.cuda.synchronize()
+    assert np.array_equal(ids.cpu().numpy(), at)
+    assert (f["logprob"] == 0).all() and (f["maxprob"] == 1).all()
